@@ -17,6 +17,12 @@
  *                          device by the variant id (Sec. II-A, II-C)
  *   damoe_router           gating logits, top-k experts and softmax gates of
  *                          each token: the routing input above (Sec. II-A)
+ *   damoe_router_loss      balance loss per sequence, z-loss, per-expert counts and
+ *                          mean probabilities of a routed batch; its gradient and
+ *                          that of the gates: damoe_router_loss_grad
+ *   damoe_mxfp4_quantise   bf16 or fp32 rows to MXFP4, in the expert layer's layouts
+ *                          or as an operand of damoe_mxfp4_linear, the product of
+ *                          MXFP4 weights with activations quantised in the call
  *   damoe_tune             offline auto-tuning: Alg. 1, ddist:X sweep,
  *                          benchmark every variant, exemplar centroids
  *                          (Sec. III-A, IV-A)
@@ -101,8 +107,15 @@ typedef enum damoe_wdtype {
  * access.  damoe_pack_weights converts once, at load time. */
 typedef enum damoe_wlayout {
   DAMOE_LAYOUT_ROWMAJOR = 0,
-  DAMOE_LAYOUT_FRAG16 = 1
+  DAMOE_LAYOUT_FRAG16 = 1,
+  DAMOE_LAYOUT_TILE32 = 2 /* MXFP4 operands of damoe_mxfp4_linear only (below), not a layer's weights */
 } damoe_wlayout;
+
+/* Element types of the matrices that the MXFP4 calls and the router's loss take. */
+typedef enum damoe_dtype {
+  DAMOE_BF16 = 0,
+  DAMOE_F32 = 1
+} damoe_dtype;
 
 /* One MoE layer of E SwiGLU experts, FFN_e(x) = W2_e (silu(W1_e x) * (W3_e x))
  * (Sec. II-A).  Weights of expert e are contiguous slabs:
@@ -433,6 +446,104 @@ size_t damoe_router_workspace_size(int32_t E, int32_t H, int32_t T_max);
 damoe_status damoe_router(const uint16_t* x, const uint16_t* wg, const float* bias, int32_t T,
                           int32_t H, int32_t E, int32_t k, float* logits, int32_t* topk_ids,
                           float* topk_w, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Score of an expert in damoe_router_loss. */
+typedef enum damoe_score {
+  DAMOE_SCORE_SOFTMAX = 0, /* p_te = exp(l_te) / sum_j exp(l_tj)                  */
+  DAMOE_SCORE_SIGMOID = 1  /* p_te = sigmoid(l_te) / sum_j sigmoid(l_tj)          */
+} damoe_score;
+
+/* Loss of a routed batch: what a router is trained with besides the task's loss.
+ * Sequence s is the tokens [seq_offsets[s], seq_offsets[s + 1]); its valid tokens V_s are those
+ * whose mask byte is not 0, n_s of them; S' sequences have n_s > 0 and N = sum n_s.
+ *   c_se = #{(t, j): t in V_s, topk_ids[t][j] = e}   f_se = E c_se / (k n_s)
+ *   P_se = sum over V_s of p_te / n_s                (0 where n_s = 0)
+ *   balance = sum_s sum_e f_se P_se / S'   z = sum over valid t of (log sum_e exp l_te)^2 / N
+ *   loss[0] = alpha balance + z_coef z     loss[1] = balance     loss[2] = z
+ * (a term whose coefficient is 0 is left out of loss[0]; without a valid token all three are 0).
+ *   logits      bf16 or fp32 (dtype) [T][ld], ld >= E; -inf is an expert that is switched off.  A
+ *               valid row of -inf alone has p = 0 and adds nothing to z; a valid row with a NaN or
+ *               +inf gives NaN.  Rows of tokens that are not valid are not read
+ *   topk_ids    int32 [T][k]; a negative id is a masked slot, an id >= E is dropped and
+ *               flagged (DAMOE_DEVERR_EXPERT_ID); an id that a token holds twice counts twice
+ *   mask        uint8 [T], or NULL: every token of a sequence is valid
+ *   seq_offsets int32 [S + 1], non-decreasing, from 0 to at most T (otherwise the results are
+ *               unspecified), or NULL with S = 1: one sequence of T tokens
+ *   counts      int32 [S][E] output c_se
+ *   probs       fp32 [S][E] output P_se, or NULL
+ *   tokens      int32 [S + 2] output: n_s of each sequence, then S' and N
+ *   loss        fp32 [3] output
+ *   ws          at least damoe_router_loss_workspace_size(T, E, S) bytes; its first word is the
+ *               sticky device error (damoe_read_device_error), so it is cleared once by the
+ *               caller; nothing else is kept between calls
+ * Sums run in a fixed order: equal inputs give equal bits.  T = 0 is valid.  1 <= S <= DAMOE_MAX_T.
+ * Stream-ordered, allocates nothing, capturable. */
+size_t damoe_router_loss_workspace_size(int32_t T_max, int32_t E, int32_t S);
+damoe_status damoe_router_loss(const void* logits, int32_t dtype, int64_t ld, const int32_t* topk_ids,
+                               const uint8_t* mask, const int32_t* seq_offsets, int32_t T, int32_t E, int32_t k,
+                               int32_t S, int32_t score, float alpha, float z_coef, float* loss, int32_t* counts,
+                               float* probs, int32_t* tokens, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradient with respect to the logits of g loss[0], g = *dloss (fp32, NULL = 1; counts are constants),
+ * plus that of the gates topk_w = softmax over the chosen logits for dtopk_w (both fp32 [T][k], or both NULL):
+ *   dlogits[t][e] = g alpha / (S' n_s) p_te (1 - sigmoid(l_te) | 1 for softmax) (f_se - sum_j f_sj p_tj)
+ *                 + g z_coef 2 / N log(sum_j exp l_tj) exp(l_te) / sum_j exp(l_tj)
+ *                 + sum over the slots j with topk_ids[t][j] = e of w_tj (dw_tj - sum_i w_ti dw_ti)
+ * (sums over slots skip ids outside [0, E)).  dlogits has the logits' type, [T][ldd], ldd >= E; the row of
+ * a token that is not valid, or in no sequence, is 0.  dlogits may be logits itself (ldd = ld).  counts and
+ * tokens are damoe_router_loss's of the same inputs.  Stream-ordered, no workspace, capturable. */
+damoe_status damoe_router_loss_grad(const void* logits, int32_t dtype, int64_t ld, const int32_t* topk_ids,
+                                    const float* topk_w, const float* dtopk_w, const uint8_t* mask,
+                                    const int32_t* seq_offsets, const int32_t* counts, const int32_t* tokens,
+                                    int32_t T, int32_t E, int32_t k, int32_t S, int32_t score, float alpha,
+                                    float z_coef, const float* dloss, void* dlogits, int64_t ldd,
+                                    hipStream_t stream);
+
+/* MXFP4 (DAMOE_W_MXFP4's element format) of the rows x cols matrix x, cols a multiple of 32: a block of 32
+ * consecutive values of a row with largest magnitude m takes the scale 2^e, e = max(floor(log2 m) - 2, -127)
+ * (m = 0: e = 0), and each value v the e2m1 code nearest to v / 2^e, ties to the even code, magnitudes
+ * above 6 to 6.  A block with an infinity or a NaN takes the scale byte 255: all its values are NaN.
+ *   x       bf16 or fp32 (dtype) [rows][ldx], ldx >= cols, any alignment of the element
+ *   layout  where codes and scales go (damoe_mxfp4_bytes: the bytes of `codes`)
+ *     DAMOE_LAYOUT_ROWMAJOR  codes [rows][cols / 2], scales [rows][cols / 32]
+ *     DAMOE_LAYOUT_FRAG16    the packed slab of an MXFP4 layer (E matrices of r rows are E r rows);
+ *                            rows a multiple of 16, cols of 128; scales lie in it (NULL here)
+ *     DAMOE_LAYOUT_TILE32    an operand of damoe_mxfp4_linear; scales lie in it (NULL here).  Tile
+ *                            (rb, cb) of 32 rows x 256 columns is 4352 bytes at (rb ceil(cols / 256) + cb) 4352:
+ *                            codes of row 32 rb + r, columns 256 cb + 64 j + 32 h .. + 31, as 16 bytes at
+ *                            1024 j + 16 (32 h + r), then the block's scale byte at 4096 + 4 (32 h + r) + j.
+ *                            Rows and columns past the matrix hold code 0 and scale 127
+ * codes must be 16-byte aligned; cols <= 2^20 and rows cols <= 2^36, else DAMOE_ERR_UNSUPPORTED.  rows = 0
+ * is a no-op.  Stream-ordered, capturable. */
+size_t damoe_mxfp4_bytes(int64_t rows, int32_t cols, int32_t layout); /* 0: not a valid shape */
+damoe_status damoe_mxfp4_quantise(const void* x, int32_t dtype, int64_t rows, int32_t cols, int64_t ldx,
+                                  int32_t layout, uint8_t* codes, uint8_t* scales, hipStream_t stream);
+
+/* The values that codes and scales of such a matrix stand for, as bf16 or fp32 [rows][ldx]: code value
+ * times 2^(s - 127), exact, infinity past the type's range, NaN where s = 255.  x aliases neither input. */
+damoe_status damoe_mxfp4_dequantise(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t cols,
+                                    int32_t layout, void* x, int32_t dtype, int64_t ldx, hipStream_t stream);
+
+/* Row-major codes [rows][cols / 2] and scales [rows][cols / 32], a checkpoint's, into DAMOE_LAYOUT_TILE32
+ * (damoe_mxfp4_bytes; codes and tiles 16-byte aligned).  The packed layout of the expert layers has
+ * damoe_pack_weights. */
+damoe_status damoe_mxfp4_pack(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t cols,
+                              uint8_t* tiles, hipStream_t stream);
+
+/* y = add + Q(x) W^T: the dense product next to the experts (a shared expert, a dense layer).
+ *   x    bf16 or fp32 (xdtype) [T][ldx], quantised in the call as damoe_mxfp4_quantise does
+ *   w    DAMOE_LAYOUT_TILE32 of the N x K weights, K a multiple of 32
+ *   add  NULL, or [T][ld_add] of y's type; it may be y itself (ld_add = ldy)
+ *   y    bf16 or fp32 (ydtype) [T][ldy], ldy >= N; columns past N are left as they were
+ *   ws   16-byte aligned, at least damoe_mxfp4_linear_workspace_size(T, N, K) bytes; nothing is kept in it.
+ * Products and scales are exact, sums fp32 in a fixed order; a NaN block makes its row (x) or column (w) of y
+ * NaN.  T = 0 is a no-op; T <= DAMOE_MAX_T, N and K <= 2^20, and T ceil(K / 256) 136, N ceil(K / 256) 136
+ * below 2^31 (32-bit offsets in an operand), else DAMOE_ERR_UNSUPPORTED.  Stream-ordered, capturable;
+ * concurrent calls need workspaces of their own, and so does every captured graph that may run beside another. */
+size_t damoe_mxfp4_linear_workspace_size(int32_t T_max, int32_t N, int32_t K);
+damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int32_t T, int32_t K, const uint8_t* w,
+                                int32_t N, const void* add, int64_t ld_add, void* y, int32_t ydtype, int64_t ldy,
+                                void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Alg. 1 (Sec. III-A): the Dirichlet concentration alpha in [1e-6, 1e6] whose
  * mean Effective Experts over `samples` draws equals `target`, by bisection on

@@ -19,7 +19,9 @@ LIB_PATH = os.path.join(_HERE, "libdamoe.so")
 N_TILE_SIZES = 5
 W_BF16, W_FP8_B128, W_MXFP4 = 0, 1, 2
 DEVERR_EXPERT_ID, DEVERR_TILES, DEVERR_VARIANT, DEVERR_COUNTS = 1, 2, 4, 8
-LAYOUT_ROWMAJOR, LAYOUT_FRAG16 = 0, 1
+LAYOUT_ROWMAJOR, LAYOUT_FRAG16, LAYOUT_TILE32 = 0, 1, 2
+BF16, F32 = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 
 STATUS = {0: "ok", -1: "invalid argument", -2: "unsupported", -3: "workspace too small",
           -4: "table mismatch", -5: "hip error", -6: "out of memory", -7: "io error"}
@@ -32,7 +34,9 @@ EXPORTED = [
     "damoe_read_device_error", "damoe_fused_moe_stage", "damoe_route_dispatch", "damoe_pack_weights",
     "damoe_table_candidates", "damoe_router", "damoe_router_workspace_size", "damoe_route_dispatch_effexp",
     "damoe_table_effexp_map", "damoe_table_effexp_candidates", "damoe_noalloc_scratch_bytes",
-    "damoe_moe_layer_noalloc",
+    "damoe_moe_layer_noalloc", "damoe_router_loss_workspace_size", "damoe_router_loss", "damoe_router_loss_grad",
+    "damoe_mxfp4_bytes", "damoe_mxfp4_quantise", "damoe_mxfp4_dequantise", "damoe_mxfp4_pack",
+    "damoe_mxfp4_linear_workspace_size", "damoe_mxfp4_linear",
 ]
 
 
@@ -84,6 +88,7 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, u32, u64, sz, f64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_uint64,
                                       ctypes.c_size_t, ctypes.c_double)
+        i64, f32 = ctypes.c_int64, ctypes.c_float
         sigs = {
             "damoe_status_string": ([i32], ctypes.c_char_p),
             "damoe_workspace_layout": ([i32, i32, i32, i32, i32, vp], i32),
@@ -114,6 +119,17 @@ def lib() -> ctypes.CDLL:
             "damoe_table_effexp_candidates": ([vp, i32], u32),
             "damoe_noalloc_scratch_bytes": ([], sz),
             "damoe_moe_layer_noalloc": ([vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp], i32),
+            "damoe_router_loss_workspace_size": ([i32, i32, i32], sz),
+            "damoe_router_loss": ([vp, i32, i64, vp, vp, vp, i32, i32, i32, i32, i32, f32, f32, vp, vp, vp, vp, vp, sz,
+                                   vp], i32),
+            "damoe_router_loss_grad": ([vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, f32, vp,
+                                        vp, i64, vp], i32),
+            "damoe_mxfp4_bytes": ([i64, i32, i32], sz),
+            "damoe_mxfp4_quantise": ([vp, i32, i64, i32, i64, i32, vp, vp, vp], i32),
+            "damoe_mxfp4_dequantise": ([vp, vp, i64, i32, i32, vp, i32, i64, vp], i32),
+            "damoe_mxfp4_pack": ([vp, vp, i64, i32, vp, vp], i32),
+            "damoe_mxfp4_linear_workspace_size": ([i32, i32, i32], sz),
+            "damoe_mxfp4_linear": ([vp, i32, i64, i32, i32, vp, i32, vp, i64, vp, i32, i64, vp, sz, vp], i32),
         }
         for name, (args, res) in sigs.items():
             fn = getattr(L, name)
@@ -251,6 +267,80 @@ def router_workspace_size(E: int, H: int, T_max: int) -> int:
 def router(x, wg, bias, T, H, E, k, logits, ids, w, ws, stream=None):
     _check("damoe_router", lib().damoe_router(_p(x), _p(wg), _p(bias), T, H, E, k, _p(logits), _p(ids), _p(w),
                                               _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def _dtype(t) -> int:
+    """BF16 or F32 of a tensor; anything else gets a code that the library refuses."""
+    name = str(t.dtype)
+    return BF16 if name == "torch.bfloat16" else F32 if name == "torch.float32" else -1
+
+
+def _ld(t, cols: int, ld) -> int:
+    """Row stride of a matrix in elements: as given, the tensor's own (2-D), or `cols`.  The elements of a row
+    lie side by side; a tensor of any other form is refused."""
+    if ld is not None:
+        return int(ld)
+    if t.dim() != 2:
+        return cols
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("the elements of a row must lie side by side")
+    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
+
+
+def router_loss_workspace_size(T_max: int, E: int, S: int = 1) -> int:
+    return int(lib().damoe_router_loss_workspace_size(T_max, E, S))
+
+
+def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, seq_offsets=None, S=1,
+                score=SCORE_SOFTMAX, alpha=0.0, z_coef=0.0, probs=None, ld=None, stream=None):
+    """Balance loss, z-loss, counts and mean probabilities of a routed batch (damoe_router_loss)."""
+    _check("damoe_router_loss", lib().damoe_router_loss(
+        _p(logits), _dtype(logits), _ld(logits, E, ld), _p(ids), _p(mask), _p(seq_offsets), T, E, k, S, score, alpha,
+        z_coef, _p(loss), _p(counts), _p(probs), _p(tokens), _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None, seq_offsets=None, S=1,
+                     score=SCORE_SOFTMAX, alpha=0.0, z_coef=0.0, dloss=None, w=None, dw=None, ld=None, ldd=None,
+                     stream=None):
+    """Gradient of the loss and of the gates w with respect to the logits (damoe_router_loss_grad)."""
+    if dlogits.dtype != logits.dtype:
+        raise ValueError("dlogits has the logits' type")
+    _check("damoe_router_loss_grad", lib().damoe_router_loss_grad(
+        _p(logits), _dtype(logits), _ld(logits, E, ld), _p(ids), _p(w), _p(dw), _p(mask), _p(seq_offsets), _p(counts),
+        _p(tokens), T, E, k, S, score, alpha, z_coef, _p(dloss), _p(dlogits), _ld(dlogits, E, ldd), _stream(stream)))
+
+
+def mxfp4_bytes(rows: int, cols: int, layout: int = LAYOUT_TILE32) -> int:
+    """Bytes of the codes of a rows x cols matrix (scales included but for the row-major layout); 0 if invalid."""
+    return int(lib().damoe_mxfp4_bytes(rows, cols, layout))
+
+
+def mxfp4_quantise(x, rows, cols, codes, scales=None, layout=LAYOUT_TILE32, ldx=None, stream=None):
+    _check("damoe_mxfp4_quantise", lib().damoe_mxfp4_quantise(
+        _p(x), _dtype(x), rows, cols, _ld(x, cols, ldx), layout, _p(codes), _p(scales), _stream(stream)))
+
+
+def mxfp4_dequantise(codes, scales, rows, cols, x, layout=LAYOUT_TILE32, ldx=None, stream=None):
+    _check("damoe_mxfp4_dequantise", lib().damoe_mxfp4_dequantise(
+        _p(codes), _p(scales), rows, cols, layout, _p(x), _dtype(x), _ld(x, cols, ldx), _stream(stream)))
+
+
+def mxfp4_pack(codes, scales, rows, cols, tiles, stream=None):
+    """Row-major codes and scales into the operand layout of mxfp4_linear."""
+    _check("damoe_mxfp4_pack", lib().damoe_mxfp4_pack(_p(codes), _p(scales), rows, cols, _p(tiles), _stream(stream)))
+
+
+def mxfp4_linear_workspace_size(T_max: int, N: int, K: int) -> int:
+    return int(lib().damoe_mxfp4_linear_workspace_size(T_max, N, K))
+
+
+def mxfp4_linear(x, T, K, w_tiles, N, y, ws, add=None, ldx=None, ldy=None, ld_add=None, stream=None):
+    """y = add + Q(x) W^T with W in tiles (damoe_mxfp4_linear); add has y's type."""
+    if add is not None and add.dtype != y.dtype:
+        raise ValueError("add has y's type")
+    _check("damoe_mxfp4_linear", lib().damoe_mxfp4_linear(
+        _p(x), _dtype(x), _ld(x, K, ldx), T, K, _p(w_tiles), N, _p(add), 0 if add is None else _ld(add, N, ld_add),
+        _p(y), _dtype(y), _ld(y, N, ldy), _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def read_device_error(ws, stream=None) -> int:

@@ -70,6 +70,57 @@ class DeviceLayer:
         return 3 * sh.H * sh.I + 3 * (sh.H // 128) * (sh.I // 128) * 4
 
 
+class QuantisedLayer:
+    """An MXFP4 layer's packed weights and its descriptor (what DeviceLayer holds for generated ones)."""
+
+    def __init__(self, shape: synth.Shape, w: dict):
+        self.shape, self.w, self.s = shape, w, {}
+        self.wdtype, self.packed = damoe.W_MXFP4, True
+        self.layer = damoe.make_layer(shape.E, shape.k, shape.H, shape.I, damoe.W_MXFP4, w["w1"], w["w3"], w["w2"],
+                                      layout=damoe.LAYOUT_FRAG16)
+
+
+def quantise_layer(shape: synth.Shape, w1, w3, w2, stream=None) -> QuantisedLayer:
+    """MXFP4 layer of bf16 or fp32 weights on the device (w1, w3 [E][I][H], w2 [E][H][I], contiguous): one pass
+    over each into the packed layout, no row-major copy."""
+    packed = {}
+    for name, t in (("w1", w1), ("w3", w3), ("w2", w2)):
+        _, r, c = synth.weight_dims(shape, name)
+        if tuple(t.shape) != (shape.E, r, c) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous [{shape.E}][{r}][{c}] tensor")
+        n = damoe.mxfp4_bytes(shape.E * r, c, damoe.LAYOUT_FRAG16)
+        packed[name] = torch.empty((shape.E, n // shape.E), dtype=torch.uint8, device=t.device)
+        damoe.mxfp4_quantise(t, shape.E * r, c, packed[name], None, damoe.LAYOUT_FRAG16, ldx=c, stream=stream)
+    return QuantisedLayer(shape, packed)
+
+
+class MxLinear:
+    """A dense MXFP4 product next to the experts (a shared expert's projections, a dense layer): the weights
+    [N][K] quantised once into the product's layout, and a workspace for up to T_max tokens.  Calls of one object
+    share its workspace, so they belong on one stream (and in one graph) at a time."""
+
+    def __init__(self, weight, T_max: int):
+        self.N, self.K = weight.shape
+        self.T_max = T_max
+        n = damoe.mxfp4_bytes(self.N, self.K)
+        if n == 0:
+            raise ValueError("the weight's columns must be a multiple of 32")
+        self.tiles = torch.empty(n, dtype=torch.uint8, device=weight.device)
+        damoe.mxfp4_quantise(weight, self.N, self.K, self.tiles)
+        self.ws = torch.empty(damoe.mxfp4_linear_workspace_size(T_max, self.N, self.K), dtype=torch.uint8,
+                              device=weight.device)
+
+    def __call__(self, x, y=None, add=None, stream=None):
+        """add + Q(x) W^T of the rows of x [T][K], into y (by default new, of x's type)."""
+        T = x.shape[0]
+        if T > self.T_max:
+            raise ValueError("more rows than T_max")
+        if y is None:
+            y = torch.empty((T, self.N), dtype=x.dtype if add is None else add.dtype, device=x.device)
+        damoe.mxfp4_linear(x, T, self.K, self.tiles, self.N, y, self.ws, add=add, stream=stream)
+        return y
+
+
 class RankLayer:
     """Expert-parallel rank `rank` of `ep`: a layer over the full layer's experts
     [rank E / ep, (rank + 1) E / ep), as views into its weight tensors (no copy)."""
@@ -151,6 +202,35 @@ class Path:
         sh = self.dl.shape
         damoe.router(self.x, gate.wg, gate.bias, T, sh.H, sh.E, sh.k, self.logits if logits else None, self.ids,
                      self.w, self.router_ws, stream)
+
+    def prepare_loss(self, S: int = 1):
+        """Buffers of router_loss and router_loss_grad for batches of S sequences (allocates; call it once)."""
+        sh, dev = self.dl.shape, self.logits.device
+        self.loss_S = S
+        self.loss = torch.zeros(3, device=dev)
+        self.loss_counts = torch.zeros((S, sh.E), dtype=torch.int32, device=dev)
+        self.loss_probs = torch.zeros((S, sh.E), device=dev)
+        self.loss_tokens = torch.zeros(S + 2, dtype=torch.int32, device=dev)
+        self.loss_ws = torch.zeros(damoe.router_loss_workspace_size(self.T_max, sh.E, S), dtype=torch.uint8, device=dev)
+        self.dlogits = torch.zeros_like(self.logits)
+
+    def router_loss(self, T: int, alpha: float, z_coef: float = 0.0, *, mask=None, seq_offsets=None,
+                    score: int = damoe.SCORE_SOFTMAX, stream=None):
+        """Balance and z-loss of the router's last call on T tokens (its logits and ids) into loss; counts, mean
+        probabilities and token counts into loss_counts, loss_probs and loss_tokens."""
+        sh = self.dl.shape
+        damoe.router_loss(self.logits, self.ids, T, sh.E, sh.k, self.loss, self.loss_counts, self.loss_tokens,
+                          self.loss_ws, mask=mask, seq_offsets=seq_offsets, S=self.loss_S, score=score, alpha=alpha,
+                          z_coef=z_coef, probs=self.loss_probs, stream=stream)
+
+    def router_loss_grad(self, T: int, alpha: float, z_coef: float = 0.0, *, dloss=None, dw=None, mask=None,
+                         seq_offsets=None, score: int = damoe.SCORE_SOFTMAX, stream=None):
+        """Gradient of router_loss (same arguments) and of the gates (dw [T][k]), with respect to the logits, into
+        the first T rows of dlogits."""
+        sh = self.dl.shape
+        damoe.router_loss_grad(self.logits, self.ids, T, sh.E, sh.k, self.loss_counts, self.loss_tokens, self.dlogits,
+                               mask=mask, seq_offsets=seq_offsets, S=self.loss_S, score=score, alpha=alpha,
+                               z_coef=z_coef, dloss=dloss, w=self.w if dw is not None else None, dw=dw, stream=stream)
 
     def route(self, T: int, ids=None, stream=None):
         sh = self.dl.shape
