@@ -46,7 +46,8 @@ damoe_status device_info(DeviceInfo** out) {
         cus <= 0)
       return DAMOE_ERR_HIP;
     if (gemm_set_lds_limits() != hipSuccess || big_set_lds_limits() != hipSuccess ||
-        big8_set_lds_limits() != hipSuccess || router_set_lds_limits() != hipSuccess)
+        big8_set_lds_limits() != hipSuccess || router_set_lds_limits() != hipSuccess ||
+        mxfp4_set_lds_limits() != hipSuccess)
       return DAMOE_ERR_HIP;
     // With this device current: the address of its copy of the allocation-free workspace.  A
     // failed lookup only disables damoe_moe_layer_noalloc.
@@ -116,6 +117,13 @@ damoe_status layout(int32_t E, int32_t k, int32_t H, int32_t I, int32_t T, damoe
 damoe_status damoe::device_setup() {
   DeviceInfo* d = nullptr;
   return device_info(&d);
+}
+
+damoe_status damoe::device_cus(int* cus) {
+  DeviceInfo* d = nullptr;
+  const damoe_status st = device_info(&d);
+  if (st == DAMOE_OK) *cus = d->cus;
+  return st;
 }
 
 

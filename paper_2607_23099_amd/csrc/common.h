@@ -166,8 +166,11 @@ hipError_t big8_set_lds_limits();
 hipError_t launch_reduce(const ReduceArgs& a, hipStream_t stream);
 hipError_t gemm_set_lds_limits();
 hipError_t router_set_lds_limits();
+hipError_t mxfp4_set_lds_limits();
 // Once per device (thread-safe): the CU count and the LDS limits of every kernel above 64 KB.
 damoe_status device_setup();
+// The same, and the current device's CU count.
+damoe_status device_cus(int* cus);
 // elem_bytes 0: MXFP4 codes, packed with their row-major E8M0 `scales` into quad fragments.
 hipError_t launch_pack(const void* src, void* dst, int32_t slabs, int32_t rows, int32_t cols, int32_t elem_bytes,
                        hipStream_t stream, const void* scales = nullptr);

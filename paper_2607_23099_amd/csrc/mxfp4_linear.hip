@@ -21,6 +21,8 @@ struct LinearArgs {
   int64_t ld_add, ldy;
   int32_t T, N, nk;   // nk: tiles along K
   int32_t y_bf;
+  int32_t vec;        // rows of y and add start at 16 bytes, N is whole eights, 32 rows lie within 2^31 bytes
+  int32_t tiles_r;    // 256-row tiles of W (the kernel of many tokens)
 };
 
 // Both operands' fp4 codes fill the lower half of the instruction's 8-register operands.
@@ -70,6 +72,370 @@ __device__ __forceinline__ void store_block(const LinearArgs& a, const floatx16&
     }
 }
 
+// ---------------------------------------------------------------- many tokens
+//
+// A workgroup of four waves takes tiles of 256 rows of W x 32 NB tokens, one after the other: wave w has 64 rows (two
+// blocks) and all the tokens, 2 NB accumulator blocks.  A stage, 256 columns, is 8 NB MFMAs a wave.
+//   W      straight into registers, every fragment read by one wave: the registers of a step are loaded for the
+//          stage after next as soon as its MFMAs have read them.
+//   tokens through LDS, which the four waves share: global -> registers (two stages ahead) -> LDS (the wave's quarter
+//          of the stage), in a ring of three stages.  The operand layout makes every LDS access one contiguous 1 KB.
+// One barrier a stage, in its middle: it makes the next stage's tokens visible, so that the first operands of
+// the next stage can be read before this one's last MFMAs, and with three buffers the one being filled is
+// that of the stage before last.  Reads, writes and loads stand one at a time behind pairs of MFMAs.  The stages of a
+// workgroup's tiles run on without a gap: the last stages of a tile load the first of the next one, whose results
+// leave while those loads are in flight.
+constexpr int kRowBlocks = 8;  // 32-row blocks of W a workgroup
+constexpr int kAhead = 4;      // token operands read ahead of their MFMAs
+
+constexpr int wait_lgkm(int n) { return 15 | (7 << 4) | (n << 8) | (3 << 14); }
+
+typedef __attribute__((address_space(3))) uint8_t lds_t;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint4 lds_read16(const lds_t* p) {
+  return __builtin_bit_cast(uint4, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(p));
+}
+__device__ __forceinline__ uint32_t lds_read4(const lds_t* p) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) uint32_t*>(p);
+}
+__device__ __forceinline__ void lds_write16(lds_t* p, uint4 v) {
+  *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(p) = __builtin_bit_cast(u32x4, v);
+}
+__device__ __forceinline__ void lds_write4(lds_t* p, uint32_t v) {
+  *reinterpret_cast<__attribute__((address_space(3))) uint32_t*>(p) = v;
+}
+
+// Tiles of a workgroup.  Workgroups b, b + 8, ... share an XCD and its L2: each XCD takes a run of the tiles in bands of
+// kBand row tiles, so that the 32 tiles it works on at a time are about 4 x 8 and read 12 rows of tiles, not 18 or 33.
+constexpr int kBand = 4;
+
+struct TileWalk {
+  int n, per, first, step, tiles_r, tiles_t;
+
+  __device__ __forceinline__ TileWalk(const LinearArgs& a, int tiles_t_) : tiles_r(a.tiles_r), tiles_t(tiles_t_) {
+    n = tiles_r * tiles_t;
+    per = (n + 7) / 8;
+    first = blockIdx.x >> 3;
+    step = gridDim.x >> 3;
+  }
+
+  // The workgroup's tile number `turn`; false past its last.
+  __device__ __forceinline__ bool tile(int turn, int& rt, int& tt) const {
+    const int i = first + turn * step, l = (blockIdx.x & 7) * per + i;
+    if (i >= per || l >= n) return false;
+    const int band = l / (kBand * tiles_t), in = l - band * kBand * tiles_t;
+    const int width = min(kBand, tiles_r - band * kBand);
+    rt = band * kBand + in % width;
+    tt = in / width;
+    return true;
+  }
+};
+
+// A wave's 32 tokens x 64 columns of results on their way through LDS, so that stores fill whole 128-byte lines (a lane
+// of the accumulators holds four columns of one token): rows of bf16 where nothing is added, of fp32 otherwise, 16
+// bytes apart.  LDS carries out a wave's accesses in order, so only the compiler is held back between them.
+constexpr uint32_t kOutBytes = 32 * (64 * 4 + 16);
+
+__device__ __forceinline__ void wave_lds_fence() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
+template <bool YBF, bool ADD>
+struct Out {
+  static constexpr bool kHalf = YBF && !ADD;             // bf16 rows in LDS
+  static constexpr uint32_t kElem = kHalf ? 2 : 4, kPitch = 64 * kElem + 16;
+  static constexpr int kLanes = 64 * kElem / 16;         // lanes of a row, 16 bytes each
+  static constexpr int kRowsAt = 64 / kLanes, kTrips = 32 / kRowsAt;
+  uint4 v[kTrips];
+
+  // Register 4 q + i of lane 32 g + r of block m is column 32 m + 8 q + 4 g + i of token r.
+  static __device__ __forceinline__ void put(lds_t* out, floatx16 c, int m, int lane) {
+    if constexpr (kHalf) asm volatile("" : "+v"(c));  // converted here and not, all blocks at once, ahead of the loop
+    lds_t* p = out + (uint32_t)(lane & 31) * kPitch + (32u * m + 4u * (lane >> 5)) * kElem;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (kHalf) {
+        const u32x2 h = {pack_bf16x2(c[4 * q], c[4 * q + 1]), pack_bf16x2(c[4 * q + 2], c[4 * q + 3])};
+        *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(p + 16 * q) = h;
+      } else {
+        lds_write16(p + 32 * q, make_uint4(__float_as_uint(c[4 * q]), __float_as_uint(c[4 * q + 1]),
+                                           __float_as_uint(c[4 * q + 2]), __float_as_uint(c[4 * q + 3])));
+      }
+    }
+  }
+
+  __device__ __forceinline__ void get(const lds_t* out, int lane) {
+    const lds_t* p = out + (uint32_t)(lane / kLanes) * kPitch + 16u * (lane % kLanes);
+#pragma unroll
+    for (int i = 0; i < kTrips; ++i) v[i] = lds_read16(p + i * kRowsAt * kPitch);
+  }
+
+  // The rows of tokens t0 .. t0 + 31, columns n0 .. + 63, where a.vec: whole lanes in or out of range, rows within 32-bit
+  // offsets of the block's first.
+  __device__ __forceinline__ void store(const LinearArgs& a, int64_t t0, int n0, int lane) const {
+    constexpr uint32_t es = YBF ? 2 : 4;
+    const int n = 16 / (int)kElem * (lane % kLanes), r0 = lane / kLanes;
+    const int rows = n0 + n < a.N ? (int)min((int64_t)32, a.T - t0) - r0 : 0;
+    const __amdgpu_buffer_rsrc_t ry = make_rsrc(static_cast<char*>(a.y) + (t0 * a.ldy + n0) * es, kOobOffset);
+    const uint32_t ldy = (uint32_t)a.ldy * es, yo = (uint32_t)r0 * ldy + (uint32_t)n * es;
+#pragma unroll
+    for (int i = 0; i < kTrips; ++i) {
+      const bool in = i * kRowsAt < rows;
+      const uint32_t o = in ? yo : kOobOffset, so = (uint32_t)(i * kRowsAt) * ldy;
+      if constexpr (kHalf) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v[i]), ry, o, so, 0);
+        continue;
+      }
+      float f[4] = {__uint_as_float(v[i].x), __uint_as_float(v[i].y), __uint_as_float(v[i].z), __uint_as_float(v[i].w)};
+      if constexpr (ADD) {
+        const __amdgpu_buffer_rsrc_t ra = make_rsrc(static_cast<const char*>(a.add) + (t0 * a.ld_add + n0) * es, kOobOffset);
+        const uint32_t lda = (uint32_t)a.ld_add * es;
+        const uint32_t p = in ? (uint32_t)r0 * lda + (uint32_t)n * es : kOobOffset, sp = (uint32_t)(i * kRowsAt) * lda;
+        if constexpr (YBF) {
+          const uint2 d = buf_load<uint2, 0>(ra, p, sp);
+          f[0] += __uint_as_float(d.x << 16), f[1] += __uint_as_float(d.x & 0xFFFF0000u);
+          f[2] += __uint_as_float(d.y << 16), f[3] += __uint_as_float(d.y & 0xFFFF0000u);
+        } else {
+          const uint4 d = buf_load<uint4, 0>(ra, p, sp);
+          f[0] += __uint_as_float(d.x), f[1] += __uint_as_float(d.y);
+          f[2] += __uint_as_float(d.z), f[3] += __uint_as_float(d.w);
+        }
+      }
+      if constexpr (YBF) {
+        const u32x2 h = {pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+        __builtin_amdgcn_raw_buffer_store_b64(h, ry, o, so, 0);
+      } else {
+        const u32x4 h = {__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+        __builtin_amdgcn_raw_buffer_store_b128(h, ry, o, so, 0);
+      }
+    }
+  }
+
+  // The same for any strides and alignment, from LDS: a column a lane, a row at a time.
+  static __device__ __forceinline__ void store_any(const LinearArgs& a, const lds_t* out, int64_t t0, int n0, int lane) {
+    const int n = n0 + lane;
+    const int rows = n < a.N ? (int)min((int64_t)32, a.T - t0) : 0;
+#pragma unroll 1
+    for (int r = 0; r < rows; ++r) {
+      const lds_t* p = out + (uint32_t)r * kPitch + (uint32_t)lane * kElem;
+      if constexpr (kHalf) {
+        static_cast<uint16_t*>(a.y)[(t0 + r) * a.ldy + n] = *reinterpret_cast<const __attribute__((address_space(3))) uint16_t*>(p);
+      } else {
+        float f = __uint_as_float(lds_read4(p));
+        if constexpr (ADD) f += load_elem(a.add, (t0 + r) * a.ld_add + n, YBF);
+        if constexpr (YBF) static_cast<uint16_t*>(a.y)[(t0 + r) * a.ldy + n] = __builtin_bit_cast(uint16_t, (__bf16)f);
+        else static_cast<float*>(a.y)[(t0 + r) * a.ldy + n] = f;
+      }
+    }
+  }
+};
+
+template <int NB, bool YBF, bool ADD>
+__global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
+  constexpr uint32_t kStage = NB * kTileBytes;
+  constexpr int kScaleMoves = (NB + 3) / 4;  // a wave's 256 B pieces of a stage (its 1 KB pieces: NB)
+  extern __shared__ __attribute__((aligned(1024))) uint8_t gemm_smem[];
+  lds_t* const lds = (lds_t*)gemm_smem;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  lds_t* const mine = lds + 3 * kStage + w * kOutBytes;
+  const int nrb = (a.N + 31) / 32, ntb = (a.T + 31) / 32, nk = a.nk;
+  // Stages of a tile: even (the sets of registers alternate) and at least 4 (a stage's loads reach into the next tile
+  // at most); stages past nk multiply zero weights.
+  const int ns = max(4, (nk + 1) & ~1);
+  const TileWalk walk(a, (ntb + NB - 1) / NB);
+  int rt, tt, turn = 0;
+  if (!walk.tile(0, rt, tt)) return;
+
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.w, (uint32_t)nrb * (uint32_t)nk * kTileBytes);
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.x, (uint32_t)ntb * (uint32_t)nk * kTileBytes);
+  const uint32_t row_bytes = (uint32_t)nk * kTileBytes;  // of a row of tiles
+  const uint32_t l16 = 16u * lane, l4 = 4u * lane;
+
+  // Where a tile's weights and tokens start: row and token blocks past the last repeat it, and their results are not
+  // stored.
+  struct Base {
+    uint32_t w[2], x[NB], xs[kScaleMoves];
+  };
+  auto base_of = [&](int rt_, int tt_) __attribute__((always_inline)) {
+    Base b;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) b.w[m] = (uint32_t)min(rt_ * kRowBlocks + 2 * w + m, nrb - 1) * row_bytes;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int piece = w * NB + i;
+      b.x[i] = (uint32_t)min(tt_ * NB + (piece >> 2), ntb - 1) * row_bytes + 1024u * (piece & 3);
+    }
+#pragma unroll
+    for (int i = 0; i < kScaleMoves; ++i)
+      b.xs[i] = (uint32_t)min(tt_ * NB + min(w * kScaleMoves + i, NB - 1), ntb - 1) * row_bytes + kTileCodes;
+    return b;
+  };
+  Base cur = base_of(rt, tt), nxt = cur;
+
+  // Sets by the parity of the stage.
+  uint4 wq[2][2][4], st[2][NB], xr[kAhead];
+  uint32_t wsc[2][2], sts[2][kScaleMoves], xs[2][NB];
+  floatx16 acc[2][NB];
+
+  // Loads of stage t of the current tile, or t - ns of the next.
+  auto at = [&](int t) __attribute__((always_inline)) { return (uint32_t)min(t < ns ? t : t - ns, nk - 1) * kTileBytes; };
+  auto load_w = [&](int t, int p, int j, int m) __attribute__((always_inline)) {
+    const uint32_t o = (t < ns ? t : t - ns) < nk ? l16 : kOobOffset;  // out of range: zero codes
+    wq[p][m][j] = buf_load<uint4, 0>(rw, o + 1024u * j, (t < ns ? cur.w[m] : nxt.w[m]) + at(t));
+  };
+  auto load_ws = [&](int t, int p, int m) __attribute__((always_inline)) {
+    wsc[p][m] = buf_load<uint32_t, 0>(rw, l4, (t < ns ? cur.w[m] : nxt.w[m]) + at(t) + kTileCodes);
+  };
+  auto load_x = [&](int t, int p, int i) __attribute__((always_inline)) {
+    st[p][i] = buf_load<uint4, 0>(rx, l16, (t < ns ? cur.x[i] : nxt.x[i]) + at(t));
+  };
+  auto load_xs = [&](int t, int p, int i) __attribute__((always_inline)) {
+    sts[p][i] = buf_load<uint32_t, 0>(rx, l4, (t < ns ? cur.xs[i] : nxt.xs[i]) + at(t));
+  };
+  auto write_x = [&](lds_t* buf, int p, int i) __attribute__((always_inline)) {
+    const int piece = w * NB + i;
+    lds_write16(buf + (piece >> 2) * kTileBytes + 1024 * (piece & 3) + l16, st[p][i]);
+  };
+  auto write_xs = [&](lds_t* buf, int p, int i) __attribute__((always_inline)) {
+    lds_write4(buf + min(w * kScaleMoves + i, NB - 1) * kTileBytes + kTileCodes + l4, sts[p][i]);
+  };
+  // Token operand i of a stage: step i / NB, token block i % NB.
+  auto read_x = [&](const lds_t* buf, int i) __attribute__((always_inline)) {
+    return lds_read16(buf + (i % NB) * kTileBytes + 1024 * (i / NB) + l16);
+  };
+  auto read_xs = [&](const lds_t* buf, int p, int n) __attribute__((always_inline)) {
+    xs[p][n] = lds_read4(buf + n * kTileBytes + kTileCodes + l4);
+  };
+  // MFMAs of step J of stage t in buf (next: the buffer of the stage after it), and behind each pair one or two of the
+  // stage's other accesses: step 0 writes the next stage's tokens, step 1 loads those of stage t + 3 into the registers
+  // that became free, step 2 reads the next stage's scales; every step loads the weights of the step before it again,
+  // for two stages on.
+  auto step = [&](const lds_t* buf, lds_t* next, int t, auto p, auto j) __attribute__((always_inline)) {
+    constexpr int P = decltype(p)::value, J = decltype(j)::value;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int i = J * NB + n, f = i + kAhead;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) acc[m][n] = mfma_fp4<J>(wq[P][m][J], wsc[P][m], xr[i % kAhead], xs[P][n], acc[m][n]);
+      xr[i % kAhead] = f < 4 * NB ? read_x(buf, f) : read_x(next, f - 4 * NB);
+      if constexpr (J == 0) {
+        write_x(next, 1 - P, n);
+        if (n < kScaleMoves) write_xs(next, 1 - P, n);
+      } else if constexpr (J == 1) {
+        load_x(t + 3, 1 - P, n);
+        if (n < kScaleMoves) load_xs(t + 3, 1 - P, n);
+      } else if constexpr (J == 2) {
+        read_xs(next, 1 - P, n);
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        if (n != (m + 1) * NB / 3) continue;
+        if constexpr (J == 0) {
+          load_w(t + 1, 1 - P, 3, m);
+          load_ws(t + 1, 1 - P, m);
+        } else {
+          load_w(t + 2, P, J - 1, m);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  using std::integral_constant;
+  auto barrier = [&]() __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto stage = [&](int t, const lds_t* buf, lds_t* next, auto p) __attribute__((always_inline)) {
+    step(buf, next, t, p, integral_constant<int, 0>{});
+    step(buf, next, t, p, integral_constant<int, 1>{});
+    // Step 0's writes are older than step 1's NB operand reads, and LDS answers a wave in order.
+    __builtin_amdgcn_s_waitcnt(wait_lgkm(NB < kAhead ? 0 : kAhead - 1));
+    barrier();
+    step(buf, next, t, p, integral_constant<int, 2>{});
+    step(buf, next, t, p, integral_constant<int, 3>{});
+  };
+
+#pragma unroll
+  for (int i = 0; i < NB; ++i) load_x(0, 0, i);
+#pragma unroll
+  for (int i = 0; i < kScaleMoves; ++i) load_xs(0, 0, i);
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_w(p, p, j, m);
+      load_ws(p, p, m);
+    }
+  }
+#pragma unroll
+  for (int p = 1; p >= 0; --p) {
+    if (p == 0) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) write_x(lds, 0, i);
+#pragma unroll
+      for (int i = 0; i < kScaleMoves; ++i) write_xs(lds, 0, i);
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) load_x(2 - p, p, i);
+#pragma unroll
+    for (int i = 0; i < kScaleMoves; ++i) load_xs(2 - p, p, i);
+  }
+  __builtin_amdgcn_s_waitcnt(wait_lgkm(0));
+  barrier();
+#pragma unroll
+  for (int n = 0; n < NB; ++n) read_xs(lds, 0, n);
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) xr[i] = read_x(lds, i);
+  uint32_t b0 = 0, b1 = kStage, b2 = 2 * kStage;
+  for (;;) {
+    int rt1 = rt, tt1 = tt;
+    const bool more = walk.tile(++turn, rt1, tt1);
+    nxt = base_of(rt1, tt1);  // with no next tile, the loads repeat this one's
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.f;
+    for (int t = 0; t < ns; t += 2) {
+      stage(t, lds + b0, lds + b1, integral_constant<int, 0>{});
+      stage(t + 1, lds + b1, lds + b2, integral_constant<int, 1>{});
+      const uint32_t o = b0;
+      b0 = b2, b2 = b1, b1 = o;
+    }
+    // Results, a token block at a time through LDS of the wave's own; a block's stores go out while the next one's
+    // values come back from LDS.
+    using O = Out<YBF, ADD>;
+    O o[2];
+    const int nb = min(NB, ntb - tt * NB), n0 = (rt * kRowBlocks + 2 * w) * 32;
+#pragma unroll
+    for (int n = 0; n <= NB; ++n) {
+      if (n < NB && n < nb) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) O::put(mine, acc[m][n], m, lane);
+        wave_lds_fence();
+        if (a.vec) o[n & 1].get(mine, lane);
+        else O::store_any(a, mine, (int64_t)(tt * NB + n) * 32, n0, lane);
+        wave_lds_fence();
+      }
+      if (a.vec && n > 0 && n <= nb) o[(n - 1) & 1].store(a, (int64_t)(tt * NB + n - 1) * 32, n0, lane);
+    }
+    if (!more) break;
+    rt = rt1, tt = tt1;
+    cur = nxt;
+  }
+}
+
+template <int NB>
+constexpr size_t gemm_lds() {
+  return 3 * NB * kTileBytes + 4 * kOutBytes;
+}
+
 // A wave: 32 rows of W x 32 NT tokens.
 template <int NT>
 __global__ void __launch_bounds__(256) k_mxfp4_linear(LinearArgs a) {
@@ -110,6 +476,16 @@ size_t x_tiles_bytes(int32_t T, int32_t K) {
 }
 
 }  // namespace
+
+hipError_t mxfp4_set_lds_limits() {
+  for (auto f : {k_mxfp4_gemm<8, false, false>, k_mxfp4_gemm<8, false, true>, k_mxfp4_gemm<8, true, false>,
+                 k_mxfp4_gemm<8, true, true>}) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, gemm_lds<8>());
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 }  // namespace damoe
 
 using namespace damoe;
@@ -138,7 +514,23 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
   if (ws_bytes < x_tiles_bytes(T, K)) return DAMOE_ERR_WORKSPACE;
   uint8_t* xt = static_cast<uint8_t*>(ws);
   if (launch_quantise_tiles(x, xdtype == DAMOE_BF16, T, K, ldx, xt, stream) != hipSuccess) return DAMOE_ERR_HIP;
-  const LinearArgs a{w, xt, add, y, ld_add, ldy, T, N, (int32_t)tiles_of(K, kTileCols), ydtype == DAMOE_BF16};
+  const auto rows_ok = [&](const void* p, int64_t ld) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)ys % 16 == 0 && ld * (int64_t)ys * 32 < (int64_t)1 << 31;
+  };
+  const bool vec = N % 8 == 0 && rows_ok(y, ldy) && (!add || rows_ok(add, ld_add));
+  const LinearArgs a{w, xt, add, y, ld_add, ldy, T, N, (int32_t)tiles_of(K, kTileCols), ydtype == DAMOE_BF16, vec,
+                     (int32_t)tiles_of(N, 256)};
+  if (T > 512) {
+    int cus = 0;
+    const damoe_status st = device_cus(&cus);
+    if (st != DAMOE_OK) return st;
+    const int64_t tiles = a.tiles_r * tiles_of(T, 256);
+    const dim3 grid((unsigned)std::min<int64_t>(tiles_of(tiles, 8), cus / 8) * 8);
+    void (*const f[4])(LinearArgs) = {k_mxfp4_gemm<8, false, false>, k_mxfp4_gemm<8, false, true>,
+                                      k_mxfp4_gemm<8, true, false>, k_mxfp4_gemm<8, true, true>};
+    hipLaunchKernelGGL(f[2 * a.y_bf + (a.add != nullptr)], grid, dim3(256), gemm_lds<8>(), stream, a);
+    return hipGetLastError() == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
+  }
   const int nt = T <= 32 ? 1 : 4;
   const dim3 grid((unsigned)tiles_of(N, 128), (unsigned)tiles_of(T, 32 * nt));
   if (nt == 1) hipLaunchKernelGGL(k_mxfp4_linear<1>, grid, dim3(256), 0, stream, a);
