@@ -24,9 +24,6 @@ __device__ __forceinline__ uint32_t fp4_scale_byte(uint32_t amax_bits) {
   return amax_bits == 0 ? kScaleOne : e == 255u ? 255u : e > 2u ? e - 2u : 0u;
 }
 
-// The same in bf16 bits.
-__device__ __forceinline__ uint32_t fp4_scale_byte_bf16(uint32_t amax16) { return fp4_scale_byte(amax16 << 16); }
-
 // 2^(s - 127), a number for s = 255 too (the codes of such a block are set to 0 by the caller).
 __device__ __forceinline__ float fp4_scale(uint32_t s) { return __uint_as_float(s == 0u ? 0x00400000u : s << 23); }
 
@@ -79,21 +76,24 @@ struct Eight {
     for (uint32_t& v : q) v = 0;
   }
 
-  // Scale byte of the block of a quad's 32 values.  Magnitudes compare as integers.
-  __device__ __forceinline__ uint32_t scale_byte() const {
+  // Largest magnitude of the eight, as the bits of an fp32 value: magnitudes compare as integers.
+  __device__ __forceinline__ uint32_t amax() const {
     if constexpr (BF) {
       u16x2_t m = __builtin_bit_cast(u16x2_t, q[0] & 0x7FFF7FFFu);
 #pragma unroll
       for (int j = 1; j < 4; ++j)
         m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, q[j] & 0x7FFF7FFFu));
-      return fp4_scale_byte_bf16(quad_max(max((uint32_t)m[0], (uint32_t)m[1])));
+      return max((uint32_t)m[0], (uint32_t)m[1]) << 16;
     } else {
       uint32_t m = q[0] & 0x7FFFFFFFu;
 #pragma unroll
       for (int j = 1; j < 8; ++j) m = max(m, q[j] & 0x7FFFFFFFu);
-      return fp4_scale_byte(quad_max(m));
+      return m;
     }
   }
+
+  // Scale byte of the block of a quad's 32 values.
+  __device__ __forceinline__ uint32_t scale_byte() const { return fp4_scale_byte(quad_max(amax())); }
 
   // The eight codes, the first in the low nibble.  The conversion divides by the scale exactly and rounds to
   // nearest even with saturation, subnormal inputs and scales included (checked on the device against the

@@ -33,52 +33,17 @@ __device__ __forceinline__ floatx16 mfma_fp4(const uint4& a, uint32_t sa, const 
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bv, c, 4, 4, J, (int)sa, J, (int)sb);
 }
 
-// A tile's operand registers of one lane: four steps and their scales.
-struct Frag {
-  uint4 q[4];
-  uint32_t s;
-
-  __device__ __forceinline__ void load(const uint8_t* tile, int lane) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = *reinterpret_cast<const uint4*>(tile + 1024 * j + 16 * lane);
-    s = *reinterpret_cast<const uint32_t*>(tile + kTileCodes + 4 * lane);
-  }
-};
-
-__device__ __forceinline__ void mfma_tile(const Frag& a, const Frag& b, floatx16& c) {
-  c = mfma_fp4<0>(a.q[0], a.s, b.q[0], b.s, c);
-  c = mfma_fp4<1>(a.q[1], a.s, b.q[1], b.s, c);
-  c = mfma_fp4<2>(a.q[2], a.s, b.q[2], b.s, c);
-  c = mfma_fp4<3>(a.q[3], a.s, b.q[3], b.s, c);
-}
-
 __device__ __forceinline__ float load_elem(const void* p, int64_t i, bool bf) {
   return bf ? bf16_to_f32(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
-}
-
-// Rows of W of a block of results: register 4 q + i of lane (r, g) is W row 8 q + 4 g + i, token r.
-__device__ __forceinline__ void store_block(const LinearArgs& a, const floatx16& c, int64_t t, int n0, int g) {
-  if (t >= a.T) return;
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = n0 + 8 * q + 4 * g + i;
-      if (n >= a.N) continue;
-      float v = c[4 * q + i];
-      if (a.add) v += load_elem(a.add, t * a.ld_add + n, a.y_bf);
-      if (a.y_bf) static_cast<uint16_t*>(a.y)[t * a.ldy + n] = __builtin_bit_cast(uint16_t, (__bf16)v);
-      else static_cast<float*>(a.y)[t * a.ldy + n] = v;
-    }
 }
 
 // ---------------------------------------------------------------- many tokens
 //
 // A workgroup of four waves takes tiles of 256 rows of W x 32 NB tokens, one after the other: wave w has 64 rows (two
 // blocks) and all the tokens, 2 NB accumulator blocks.  A stage, 256 columns, is 8 NB MFMAs a wave.
-//   W      straight into registers, every fragment read by one wave: the registers of a step are loaded for the
-//          stage after next as soon as its MFMAs have read them.
-//   tokens through LDS, which the four waves share: global -> registers (two stages ahead) -> LDS (the wave's quarter
+//   W      straight into registers, every fragment read by one wave: the registers of a step are loaded for a
+//          stage D ahead as soon as its MFMAs have read them.
+//   tokens through LDS, which the four waves share: global -> registers (D stages ahead) -> LDS (the wave's quarter
 //          of the stage), in a ring of three stages.  The operand layout makes every LDS access one contiguous 1 KB.
 // One barrier a stage, in its middle: it makes the next stage's tokens visible, so that the first operands of
 // the next stage can be read before this one's last MFMAs, and with three buffers the one being filled is
@@ -86,7 +51,6 @@ __device__ __forceinline__ void store_block(const LinearArgs& a, const floatx16&
 // workgroup's tiles run on without a gap: the last stages of a tile load the first of the next one, whose results
 // leave while those loads are in flight.
 constexpr int kRowBlocks = 8;  // 32-row blocks of W a workgroup
-constexpr int kAhead = 4;      // token operands read ahead of their MFMAs
 
 constexpr int wait_lgkm(int n) { return 15 | (7 << 4) | (n << 8) | (3 << 14); }
 
@@ -236,15 +200,18 @@ struct Out {
 template <int NB, bool YBF, bool ADD>
 __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
   constexpr uint32_t kStage = NB * kTileBytes;
+  // Token operands read ahead of their MFMAs; reads of the next stage's start behind the barrier, in step 2.
+  constexpr int kAhead = NB >= 2 ? 4 : 2;
+  constexpr int D = 2;  // stages ahead that weights and tokens are loaded (4 is no faster, and its code starts colder)
   constexpr int kScaleMoves = (NB + 3) / 4;  // a wave's 256 B pieces of a stage (its 1 KB pieces: NB)
   extern __shared__ __attribute__((aligned(1024))) uint8_t gemm_smem[];
   lds_t* const lds = (lds_t*)gemm_smem;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   lds_t* const mine = lds + 3 * kStage + w * kOutBytes;
   const int nrb = (a.N + 31) / 32, ntb = (a.T + 31) / 32, nk = a.nk;
-  // Stages of a tile: even (the sets of registers alternate) and at least 4 (a stage's loads reach into the next tile
-  // at most); stages past nk multiply zero weights.
-  const int ns = max(4, (nk + 1) & ~1);
+  // Stages of a tile: whole turns of the D sets of registers, and two at least (a stage's loads reach into the next
+  // tile at most); stages past nk multiply zero weights.
+  const int ns = max(2 * D, (nk + D - 1) / D * D);
   const TileWalk walk(a, (ntb + NB - 1) / NB);
   int rt, tt, turn = 0;
   if (!walk.tile(0, rt, tt)) return;
@@ -275,9 +242,9 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
   };
   Base cur = base_of(rt, tt), nxt = cur;
 
-  // Sets by the parity of the stage.
-  uint4 wq[2][2][4], st[2][NB], xr[kAhead];
-  uint32_t wsc[2][2], sts[2][kScaleMoves], xs[2][NB];
+  // Sets by the stage modulo D, of scales from LDS modulo 2.
+  uint4 wq[D][2][4], st[D][NB], xr[kAhead];
+  uint32_t wsc[D][2], sts[D][kScaleMoves], xs[2][NB];
   floatx16 acc[2][NB];
 
   // Loads of stage t of the current tile, or t - ns of the next.
@@ -310,34 +277,35 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
     xs[p][n] = lds_read4(buf + n * kTileBytes + kTileCodes + l4);
   };
   // MFMAs of step J of stage t in buf (next: the buffer of the stage after it), and behind each pair one or two of the
-  // stage's other accesses: step 0 writes the next stage's tokens, step 1 loads those of stage t + 3 into the registers
-  // that became free, step 2 reads the next stage's scales; every step loads the weights of the step before it again,
-  // for two stages on.
+  // stage's other accesses: step 0 writes the next stage's tokens, step 1 loads those of stage t + 1 + D into the
+  // registers that became free, step 2 reads the next stage's scales; every step loads the weights of the step before
+  // it again, for D stages on.
   auto step = [&](const lds_t* buf, lds_t* next, int t, auto p, auto j) __attribute__((always_inline)) {
-    constexpr int P = decltype(p)::value, J = decltype(j)::value;
+    constexpr int P = decltype(p)::value, J = decltype(j)::value;  // P: t modulo D
+    constexpr int Q = (P + 1) % D, R = (P + D - 1) % D;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const int i = J * NB + n, f = i + kAhead;
 #pragma unroll
-      for (int m = 0; m < 2; ++m) acc[m][n] = mfma_fp4<J>(wq[P][m][J], wsc[P][m], xr[i % kAhead], xs[P][n], acc[m][n]);
+      for (int m = 0; m < 2; ++m) acc[m][n] = mfma_fp4<J>(wq[P][m][J], wsc[P][m], xr[i % kAhead], xs[P % 2][n], acc[m][n]);
       xr[i % kAhead] = f < 4 * NB ? read_x(buf, f) : read_x(next, f - 4 * NB);
       if constexpr (J == 0) {
-        write_x(next, 1 - P, n);
-        if (n < kScaleMoves) write_xs(next, 1 - P, n);
+        write_x(next, Q, n);
+        if (n < kScaleMoves) write_xs(next, Q, n);
       } else if constexpr (J == 1) {
-        load_x(t + 3, 1 - P, n);
-        if (n < kScaleMoves) load_xs(t + 3, 1 - P, n);
+        load_x(t + 1 + D, Q, n);
+        if (n < kScaleMoves) load_xs(t + 1 + D, Q, n);
       } else if constexpr (J == 2) {
-        read_xs(next, 1 - P, n);
+        read_xs(next, 1 - P % 2, n);
       }
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         if (n != (m + 1) * NB / 3) continue;
         if constexpr (J == 0) {
-          load_w(t + 1, 1 - P, 3, m);
-          load_ws(t + 1, 1 - P, m);
+          load_w(t - 1 + D, R, 3, m);
+          load_ws(t - 1 + D, R, m);
         } else {
-          load_w(t + 2, P, J - 1, m);
+          load_w(t + D, P, J - 1, m);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -360,11 +328,11 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
   };
 
 #pragma unroll
-  for (int i = 0; i < NB; ++i) load_x(0, 0, i);
+  for (int p = 0; p < D; ++p) {
 #pragma unroll
-  for (int i = 0; i < kScaleMoves; ++i) load_xs(0, 0, i);
+    for (int i = 0; i < NB; ++i) load_x(p, p, i);
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
+    for (int i = 0; i < kScaleMoves; ++i) load_xs(p, p, i);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
 #pragma unroll
@@ -373,18 +341,13 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
     }
   }
 #pragma unroll
-  for (int p = 1; p >= 0; --p) {
-    if (p == 0) {
+  for (int i = 0; i < NB; ++i) write_x(lds, 0, i);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) write_x(lds, 0, i);
+  for (int i = 0; i < kScaleMoves; ++i) write_xs(lds, 0, i);
 #pragma unroll
-      for (int i = 0; i < kScaleMoves; ++i) write_xs(lds, 0, i);
-    }
+  for (int i = 0; i < NB; ++i) load_x(D, 0, i);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) load_x(2 - p, p, i);
-#pragma unroll
-    for (int i = 0; i < kScaleMoves; ++i) load_xs(2 - p, p, i);
-  }
+  for (int i = 0; i < kScaleMoves; ++i) load_xs(D, 0, i);
   __builtin_amdgcn_s_waitcnt(wait_lgkm(0));
   barrier();
 #pragma unroll
@@ -402,11 +365,14 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.f;
-    for (int t = 0; t < ns; t += 2) {
-      stage(t, lds + b0, lds + b1, integral_constant<int, 0>{});
-      stage(t + 1, lds + b1, lds + b2, integral_constant<int, 1>{});
+    const auto turn_of = [&](int t, auto p) __attribute__((always_inline)) {
+      stage(t + decltype(p)::value, lds + b0, lds + b1, p);
       const uint32_t o = b0;
-      b0 = b2, b2 = b1, b1 = o;
+      b0 = b1, b1 = b2, b2 = o;
+    };
+    for (int t = 0; t < ns; t += D) {
+      turn_of(t, integral_constant<int, 0>{});
+      turn_of(t, integral_constant<int, 1>{});
     }
     // Results, a token block at a time through LDS of the wave's own; a block's stores go out while the next one's
     // values come back from LDS.
@@ -436,29 +402,218 @@ constexpr size_t gemm_lds() {
   return 3 * NB * kTileBytes + 4 * kOutBytes;
 }
 
-// A wave: 32 rows of W x 32 NT tokens.
-template <int NT>
-__global__ void __launch_bounds__(256) k_mxfp4_linear(LinearArgs a) {
+// ---------------------------------------------------------------- few tokens
+//
+// A workgroup of eight waves takes 16 MR rows of W and 16 NT tokens, and its waves the tiles of 256 columns in turn, so
+// that even a short row keeps every wave's loads in flight at once; the waves' sums meet in LDS and are added in
+// order.  The weight stream is the traffic (latency at few rows), so nothing is staged: a wave reads both operands
+// straight into registers.
+//
+// v_mfma_scale_f32_16x16x128_f8f6f4: lane 16 b + i holds row i, columns 32 b .. + 31, one scale block.  In a tile that is
+// the piece of step b / 2 (+ 2 for the second 128 columns), half b % 2, and byte b / 2 (+ 2) of its scales.  The
+// result has D[4 (l / 16) + i][l % 16] in register i.
+constexpr int kRowsThreads = 512, kRowsWaves = kRowsThreads / kWave;
+
+struct RowsArgs {
+  LinearArgs l;
+  const void* x;  // rows to quantise here (XT: bf16 or fp32), 16-byte aligned; or unused
+  int64_t ldx;
+  int32_t K;
+};
+
+// 16 rows of a tile in operand form.
+struct Half {
+  uint4 q[2];
+  uint32_t s;
+
+  // off: the lane's offset in the tile, soff its scales'.
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t tile, uint32_t off, uint32_t soff) {
+    q[0] = buf_load<uint4, 0>(r, off, tile);
+    q[1] = buf_load<uint4, 0>(r, off + 2048u, tile);
+    s = buf_load<uint32_t, 0>(r, soff, tile);
+  }
+  __device__ __forceinline__ void align(int lane) { s >>= 8 * (lane >> 5); }  // byte b / 2 to the front
+};
+
+// The same from 32 values a lane and 128 columns, quantised in the lane.
+template <bool BF>
+struct Raw {
+  Eight<BF> e[2][4];
+
+  __device__ __forceinline__ void load(const void* x, int64_t row, int c, int K) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (row >= 0 && c + 128 * h < K) e[h][i].template load<true>(x, row + c + 128 * h + 8 * i);
+        else e[h][i].zero();
+      }
+  }
+  __device__ __forceinline__ void quantise(Half& o) const {
+    o.s = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t m = e[h][0].amax();
+#pragma unroll
+      for (int i = 1; i < 4; ++i) m = max(m, e[h][i].amax());
+      const uint32_t s = fp4_scale_byte(m);
+      o.q[h] = make_uint4(e[h][0].codes(s), e[h][1].codes(s), e[h][2].codes(s), e[h][3].codes(s));
+      o.s |= s << (16 * h);
+    }
+  }
+};
+
+template <int H>
+__device__ __forceinline__ floatx4 mfma_half(const Half& a, const Half& b, const floatx4& c) {
+  const v8i av = {(int)a.q[H].x, (int)a.q[H].y, (int)a.q[H].z, (int)a.q[H].w, 0, 0, 0, 0};
+  const v8i bv = {(int)b.q[H].x, (int)b.q[H].y, (int)b.q[H].z, (int)b.q[H].w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4, 4, 2 * H, (int)a.s, 2 * H, (int)b.s);
+}
+
+// XT: 0 tokens quantised in the workspace, 1 bf16 and 2 fp32 rows quantised here (NT = 1).
+template <int MR, int NT, int XT>
+__global__ void __launch_bounds__(kRowsThreads, NT > 2 ? 2 : 4) k_mxfp4_rows(RowsArgs ra) {
+  static_assert(MR * NT <= kRowsWaves, "a thread sums one lane's four values");
+  const LinearArgs& a = ra.l;
+  __shared__ floatx4 red[kRowsWaves][MR * NT][kWave];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rb = blockIdx.x * 4 + w, tb0 = blockIdx.y * NT;
-  const int nrb = (a.N + 31) / 32, ntb = (a.T + 31) / 32;
-  if (rb >= nrb) return;
-  floatx16 c[NT];
+  const int i16 = lane & 15, b = lane >> 4;
+  const int nrb = (a.N + 31) / 32, ntb = (a.T + 31) / 32, nk = a.nk;
+  const int row0 = blockIdx.x * 16 * MR, tok0 = blockIdx.y * 16 * NT;
+  const uint32_t row_bytes = (uint32_t)nk * kTileBytes;
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.w, (uint32_t)nrb * row_bytes);
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.x, (uint32_t)ntb * row_bytes);
+  // Lane offsets in a tile, of rows 0 .. 15 of it; the upper sixteen rows are 256 (scales: 64) bytes on.
+  const uint32_t off = 1024u * (b >> 1) + 16u * (32 * (b & 1) + i16), soff = kTileCodes + 4u * (32 * (b & 1) + i16);
+  uint32_t wbase[MR], xbase[NT], wup[MR], xup[NT];
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) c[n][i] = 0.f;
-  for (int k = 0; k < a.nk; ++k) {
-    Frag wf, xf[NT];
-    wf.load(a.w + ((int64_t)rb * a.nk + k) * kTileBytes, lane);
-#pragma unroll
-    for (int n = 0; n < NT; ++n)  // blocks past the last repeat it; their results are not stored
-      xf[n].load(a.x + ((int64_t)min(tb0 + n, ntb - 1) * a.nk + k) * kTileBytes, lane);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) mfma_tile(wf, xf[n], c[n]);
+  for (int m = 0; m < MR; ++m) {  // row blocks past the last repeat it; their results are not stored
+    const int r = row0 + 16 * m;
+    wbase[m] = (uint32_t)min(r >> 5, nrb - 1) * row_bytes;
+    wup[m] = (r >> 4) & 1;
   }
 #pragma unroll
-  for (int n = 0; n < NT; ++n) store_block(a, c[n], (int64_t)(tb0 + n) * 32 + (lane & 31), rb * 32, lane >> 5);
+  for (int n = 0; n < NT; ++n) {
+    const int t = tok0 + 16 * n;
+    xbase[n] = (uint32_t)min(t >> 5, ntb - 1) * row_bytes;
+    xup[n] = (t >> 4) & 1;
+  }
+  floatx4 acc[MR][NT];
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  // Tiles whose weights a wave loads together, and tiles of raw tokens it holds at a time.
+  constexpr int U = NT > 2 ? 2 : 4, UX = XT == 1 ? 2 : 1;
+  for (int k0 = w; k0 < nk; k0 += U * kRowsWaves) {
+    Half wf[U][MR], xf[U][NT];
+    Raw<XT != 2> raw[UX];
+    const auto load_raw = [&](int u) __attribute__((always_inline)) {
+      const int k = k0 + u * kRowsWaves;
+      if (k < nk) raw[u % UX].load(ra.x, tok0 + i16 < a.T ? (tok0 + i16) * ra.ldx : -1, 256 * k + 32 * b, ra.K);
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * kRowsWaves;
+      if (XT != 0 && u < UX) load_raw(u);
+      if (k >= nk) continue;
+      const uint32_t tile = (uint32_t)k * kTileBytes;
+#pragma unroll
+      for (int m = 0; m < MR; ++m) wf[u][m].load(rw, wbase[m] + tile, off + 256u * wup[m], soff + 64u * wup[m]);
+      if constexpr (XT == 0) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) xf[u][n].load(rx, xbase[n] + tile, off + 256u * xup[n], soff + 64u * xup[n]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k0 + u * kRowsWaves >= nk) continue;
+#pragma unroll
+      for (int m = 0; m < MR; ++m) wf[u][m].align(lane);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        if constexpr (XT == 0) {
+          xf[u][n].align(lane);
+        } else {
+          raw[u % UX].quantise(xf[u][n]);
+          if (u + UX < U) load_raw(u + UX);
+        }
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+          acc[m][n] = mfma_half<0>(wf[u][m], xf[u][n], acc[m][n]);
+          acc[m][n] = mfma_half<1>(wf[u][m], xf[u][n], acc[m][n]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) red[w][m * NT + n][lane] = acc[m][n];
+  __syncthreads();
+  if (w >= MR * NT) return;
+  floatx4 v = red[0][w][lane];
+#pragma unroll
+  for (int i = 1; i < kRowsWaves; ++i) v += red[i][w][lane];
+  const int64_t t = tok0 + 16 * (w % NT) + i16;
+  const int n0 = row0 + 16 * (w / NT) + 4 * b;
+  if (t >= a.T) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (n0 + i >= a.N) continue;
+    float f = v[i];
+    if (a.add) f += load_elem(a.add, t * a.ld_add + n0 + i, a.y_bf);
+    if (a.y_bf) static_cast<uint16_t*>(a.y)[t * a.ldy + n0 + i] = __builtin_bit_cast(uint16_t, (__bf16)f);
+    else static_cast<float*>(a.y)[t * a.ldy + n0 + i] = f;
+  }
+}
+
+// Which kernel a call of more than 32 tokens takes: the one with the least estimated time, in us, fitted to measured
+// calls (N x K of 4096 x 7168, 7168 x 2048, 8192 x 8192 and 512 x 1024, T = 33 to 8192; at most 15% over the fastest).
+// k_mxfp4_rows<2, 4> runs rounds of a workgroup a CU, each a start and its waves' tiles.  k_mxfp4_gemm<NB> runs rounds
+// of tiles, each a fixed part and stages, which take the longer the more CUs share L2 (and, at NB = 8, the card's power).
+// Fastest at T = 64 / 300 / 1000 / 4096: 4096 x 7168 rows 6.1, gemm<1> 15.0 (rows 16.3), <2> 20.8 (<4> 27.3),
+// <8> 57.3 (<4> 62.2); 7168 x 2048 rows 4.3, <2> 7.6 (<1> 8.6), <4> 12.6 (<8> 18.1), <4> 38.8 (<8> 40.0).
+enum Path { kRows, kGemm1, kGemm2, kGemm4, kGemm8 };
+
+Path path_of(int32_t T, int32_t N, int32_t K, int cus) {
+  const double nk = (double)tiles_of(K, kTileCols);
+  const auto rounds = [&](int64_t n) { return (double)((n + cus - 1) / cus); };
+  double best = 2.8 + rounds(tiles_of(N, 32) * tiles_of(T, 64)) * (1.0 + 0.13 * nk);
+  Path path = kRows;
+  constexpr struct {
+    Path path;
+    int nb;
+    double stage, shared, fixed;
+  } gemms[] = {{kGemm1, 1, 0.33, 0.14, 0.3}, {kGemm2, 2, 0.40, 0.24, 0.6}, {kGemm4, 4, 0.60, 0.45, 1.2}, {kGemm8, 8, 1.10, 0.85, 4.0}};
+  for (const auto& g : gemms) {
+    const int64_t tiles = tiles_of(N, 256) * tiles_of(T, 32 * g.nb);
+    const double t = 2.7 + rounds(tiles) * (nk * (g.stage + g.shared * std::min(1.0, (double)tiles / cus)) + g.fixed);
+    if (t < best) best = t, path = g.path;
+  }
+  return path;
+}
+
+template <int NB>
+hipError_t launch_gemm(const LinearArgs& a, int cus, hipStream_t stream) {
+  const int64_t tiles = a.tiles_r * tiles_of(a.T, 32 * NB);
+  const dim3 grid((unsigned)std::min<int64_t>(tiles_of(tiles, 8), cus * (NB <= 2 ? 2 : 1) / 8) * 8);  // 1 or 2 a CU
+  const auto go = [&](void (*f)(LinearArgs)) { hipLaunchKernelGGL(f, grid, dim3(256), gemm_lds<NB>(), stream, a); };
+  if (a.y_bf) go(a.add ? k_mxfp4_gemm<NB, true, true> : k_mxfp4_gemm<NB, true, false>);
+  else go(a.add ? k_mxfp4_gemm<NB, false, true> : k_mxfp4_gemm<NB, false, false>);
+  return hipGetLastError();
+}
+
+template <int NB>
+hipError_t gemm_limits() {
+  for (auto f : {k_mxfp4_gemm<NB, false, false>, k_mxfp4_gemm<NB, false, true>, k_mxfp4_gemm<NB, true, false>,
+                 k_mxfp4_gemm<NB, true, true>}) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             gemm_lds<NB>());
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 constexpr int32_t kMaxDim = 1 << 20;
@@ -478,11 +633,8 @@ size_t x_tiles_bytes(int32_t T, int32_t K) {
 }  // namespace
 
 hipError_t mxfp4_set_lds_limits() {
-  for (auto f : {k_mxfp4_gemm<8, false, false>, k_mxfp4_gemm<8, false, true>, k_mxfp4_gemm<8, true, false>,
-                 k_mxfp4_gemm<8, true, true>}) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, gemm_lds<8>());
+  for (const hipError_t e : {gemm_limits<1>(), gemm_limits<2>(), gemm_limits<4>(), gemm_limits<8>()})
     if (e != hipSuccess) return e;
-  }
   return hipSuccess;
 }
 
@@ -513,29 +665,37 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
     return DAMOE_ERR_INVALID_ARG;
   if (ws_bytes < x_tiles_bytes(T, K)) return DAMOE_ERR_WORKSPACE;
   uint8_t* xt = static_cast<uint8_t*>(ws);
-  if (launch_quantise_tiles(x, xdtype == DAMOE_BF16, T, K, ldx, xt, stream) != hipSuccess) return DAMOE_ERR_HIP;
+  const bool x_bf = xdtype == DAMOE_BF16;
   const auto rows_ok = [&](const void* p, int64_t ld) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)ys % 16 == 0 && ld * (int64_t)ys * 32 < (int64_t)1 << 31;
   };
   const bool vec = N % 8 == 0 && rows_ok(y, ldy) && (!add || rows_ok(add, ld_add));
   const LinearArgs a{w, xt, add, y, ld_add, ldy, T, N, (int32_t)tiles_of(K, kTileCols), ydtype == DAMOE_BF16, vec,
                      (int32_t)tiles_of(N, 256)};
-  if (T > 512) {
-    int cus = 0;
-    const damoe_status st = device_cus(&cus);
-    if (st != DAMOE_OK) return st;
-    const int64_t tiles = a.tiles_r * tiles_of(T, 256);
-    const dim3 grid((unsigned)std::min<int64_t>(tiles_of(tiles, 8), cus / 8) * 8);
-    void (*const f[4])(LinearArgs) = {k_mxfp4_gemm<8, false, false>, k_mxfp4_gemm<8, false, true>,
-                                      k_mxfp4_gemm<8, true, false>, k_mxfp4_gemm<8, true, true>};
-    hipLaunchKernelGGL(f[2 * a.y_bf + (a.add != nullptr)], grid, dim3(256), gemm_lds<8>(), stream, a);
-    return hipGetLastError() == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
+  // Up to four tokens are quantised where they are used, which saves a launch (4096 x 7168, T = 1: 5.8 us against 3.6 and
+  // 2.9; from T = 8 on the workgroups' reads of x cost more, 7.5 us).
+  const bool fused = T <= 4 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * (int64_t)xs % 16 == 0;
+  if (!fused && launch_quantise_tiles(x, x_bf, T, K, ldx, xt, stream) != hipSuccess) return DAMOE_ERR_HIP;
+  int cus = 0;
+  const damoe_status st = device_cus(&cus);
+  if (st != DAMOE_OK) return st;
+  const RowsArgs r{a, x, ldx, K};
+  const auto rows = [&](void (*f)(RowsArgs), int mr, int nt) {
+    hipLaunchKernelGGL(f, dim3((unsigned)tiles_of(N, 16 * mr), (unsigned)tiles_of(T, 16 * nt)), dim3(kRowsThreads), 0, stream, r);
+    return hipGetLastError();
+  };
+  hipError_t e;
+  if (fused) e = rows(x_bf ? k_mxfp4_rows<1, 1, 1> : k_mxfp4_rows<1, 1, 2>, 1, 1);
+  else if (T <= 16) e = rows(k_mxfp4_rows<1, 1, 0>, 1, 1);
+  else if (T <= 32) e = rows(k_mxfp4_rows<1, 2, 0>, 1, 2);
+  else switch (path_of(T, N, K, cus)) {
+    case kRows: e = rows(k_mxfp4_rows<2, 4, 0>, 2, 4); break;
+    case kGemm1: e = launch_gemm<1>(a, cus, stream); break;
+    case kGemm2: e = launch_gemm<2>(a, cus, stream); break;
+    case kGemm4: e = launch_gemm<4>(a, cus, stream); break;
+    default: e = launch_gemm<8>(a, cus, stream);
   }
-  const int nt = T <= 32 ? 1 : 4;
-  const dim3 grid((unsigned)tiles_of(N, 128), (unsigned)tiles_of(T, 32 * nt));
-  if (nt == 1) hipLaunchKernelGGL(k_mxfp4_linear<1>, grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL(k_mxfp4_linear<4>, grid, dim3(256), 0, stream, a);
-  return hipGetLastError() == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
+  return e == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
 }
 
 }  // extern "C"

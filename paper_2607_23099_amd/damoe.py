@@ -154,9 +154,9 @@ def _p(t) -> int:
 
 
 def _stream(stream) -> int:
-    if stream is None:
+    if stream is None:  # the handle alone: torch.cuda.current_stream() builds a Stream object, 2.7 us a call
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -269,10 +269,15 @@ def router(x, wg, bias, T, H, E, k, logits, ids, w, ws, stream=None):
                                               _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
+_DTYPES = {}
+
+
 def _dtype(t) -> int:
     """BF16 or F32 of a tensor; anything else gets a code that the library refuses."""
-    name = str(t.dtype)
-    return BF16 if name == "torch.bfloat16" else F32 if name == "torch.float32" else -1
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: BF16, torch.float32: F32})
+    return _DTYPES.get(t.dtype, -1)
 
 
 def _ld(t, cols: int, ld) -> int:
@@ -280,11 +285,12 @@ def _ld(t, cols: int, ld) -> int:
     lie side by side; a tensor of any other form is refused."""
     if ld is not None:
         return int(ld)
-    if t.dim() != 2:
+    stride = t.stride()
+    if len(stride) != 2:
         return cols
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if stride[1] != 1 and t.shape[1] > 1:
         raise ValueError("the elements of a row must lie side by side")
-    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
+    return max(cols, stride[0]) if t.shape[0] == 1 else stride[0]
 
 
 def router_loss_workspace_size(T_max: int, E: int, S: int = 1) -> int:

@@ -17,11 +17,11 @@ def quantise(x):
     _, ex = np.frexp(m)  # m = mant 2^ex, mant in [0.5, 1): floor(log2 m) = ex - 1
     e = np.where(m > 0, np.maximum(ex - 3, -127), 0)
     a = np.abs(b) * np.exp2(-e.astype(np.float64))[:, :, None]
-    d = np.abs(a[..., None] - LEVELS)
-    best = d.min(axis=-1)
     # Nearest level; of two at one distance the even code; past the last level, the last.
-    even_first = np.array([0, 2, 4, 6, 1, 3, 5, 7])
-    code = even_first[np.argmax(d[..., even_first] == best[..., None], axis=-1)]
+    hi = np.clip(np.searchsorted(LEVELS, a, side="left"), 1, 7)
+    lo = hi - 1
+    d_hi, d_lo = LEVELS[hi] - a, a - LEVELS[lo]
+    code = np.where((d_hi < d_lo) | ((d_hi == d_lo) & (hi % 2 == 0)), hi, lo)
     code = code | np.where(np.signbit(b), 8, 0)
     code = np.where(bad[:, :, None], 0, code)
     return code.reshape(R, C).astype(np.uint8), np.where(bad, 255, e + 127).astype(np.uint8)

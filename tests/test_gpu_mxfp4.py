@@ -159,7 +159,10 @@ def _check(got, want, tol):
 
 TNK = [(1, 1, 32), (1, 7168, 2048), (2, 100, 96), (5, 33, 256), (16, 512, 7168), (31, 31, 288), (32, 256, 512),
        (33, 1000, 544), (37, 4096, 1024), (64, 64, 4096), (65, 257, 768), (100, 130, 2048), (129, 96, 256),
-       (200, 2048, 1024), (255, 384, 1280), (300, 7168, 512), (513, 300, 2304), (1000, 513, 320), (2049, 1025, 1056)]
+       (200, 2048, 1024), (255, 384, 1280), (300, 7168, 512), (513, 300, 2304), (1000, 513, 320), (2049, 1025, 1056),
+       # every kernel of many tokens, with whole and with odd rows of y
+       (129, 4100, 544), (300, 4104, 800), (513, 7001, 288), (700, 4096, 1056), (1100, 5000, 800), (600, 7169, 320),
+       (2300, 4001, 1568), (2300, 4000, 1568)]
 
 
 @pytest.mark.parametrize("T,N,K", TNK)
@@ -177,14 +180,16 @@ def test_linear(T, N, K):
         assert torch.equal(again, y)  # a fixed order of sums
 
 
-@pytest.mark.parametrize("T,N,K", [(3, 100, 320), (40, 77, 2048), (300, 301, 512)])
+@pytest.mark.parametrize("T,N,K", [(3, 100, 320), (40, 77, 2048), (300, 301, 512), (150, 4096, 544), (513, 7001, 288),
+                                   (600, 7168, 320), (2300, 4001, 1568), (2300, 4008, 1568)])
 @pytest.mark.parametrize("yd", ["bf16", "f32"])
 def test_linear_add_and_strides(T, N, K, yd):
     torch = torch_cuda()
     log(f"linear with add T={T} N={N} K={K} {yd}")
     dt = torch.bfloat16 if yd == "bf16" else torch.float32
     p = Linear(torch, T, N, K, seed=1)
-    ldx, ldy, lda = K + 5, N + 3, N + 1
+    # Rows of y and add that start at 16 bytes take wide accesses where N allows it.
+    ldx, ldy, lda = (K + 5, N + 3, N + 1) if N % 8 else (K + 5, N + 16, N + 8)
     x = torch.full((T, ldx), float("nan"), dtype=torch.bfloat16, device="cuda")
     x[:, :K] = p.x
     add = torch.randn(T, lda, generator=torch.Generator().manual_seed(2)).to(dt).cuda()
