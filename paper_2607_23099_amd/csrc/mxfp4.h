@@ -41,18 +41,33 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+template <bool NT>
+__device__ __forceinline__ uint4 load16(const void* p) {
+  const u32x4_t* q = static_cast<const u32x4_t*>(p);
+  return __builtin_bit_cast(uint4, NT ? __builtin_nontemporal_load(q) : *q);
+}
+
+template <bool NT>
+__device__ __forceinline__ void store16(void* p, uint4 v) {
+  u32x4_t* q = static_cast<u32x4_t*>(p);
+  if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), q);
+  else *q = __builtin_bit_cast(u32x4_t, v);
+}
+
 // Eight values of a lane, as loaded.
 template <bool BF>
 struct Eight {
   uint32_t q[BF ? 4 : 8];
 
-  // V: 16-byte loads (the address is 16-byte aligned).
-  template <bool V>
+  // V: 16-byte loads (the address is 16-byte aligned); NT: with the nontemporal hint.
+  template <bool V, bool NT = false>
   __device__ __forceinline__ void load(const void* base, int64_t i) {
     if constexpr (BF) {
       const uint16_t* p = static_cast<const uint16_t*>(base) + i;
       if constexpr (V) {
-        const uint4 a = *reinterpret_cast<const uint4*>(p);
+        const uint4 a = load16<NT>(p);
         q[0] = a.x, q[1] = a.y, q[2] = a.z, q[3] = a.w;
       } else {
 #pragma unroll
@@ -61,7 +76,7 @@ struct Eight {
     } else {
       const uint32_t* p = static_cast<const uint32_t*>(base) + i;
       if constexpr (V) {
-        const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+        const uint4 a = load16<NT>(p), b = load16<NT>(p + 4);
         q[0] = a.x, q[1] = a.y, q[2] = a.z, q[3] = a.w;
         q[4] = b.x, q[5] = b.y, q[6] = b.z, q[7] = b.w;
       } else {

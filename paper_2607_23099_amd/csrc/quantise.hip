@@ -26,7 +26,7 @@ struct QuantArgs {
 // ---------------------------------------------------------------- quantise
 
 // Row-major.  Rows without a gap (ld = cols) are one long row.
-template <bool BF, bool V>
+template <bool BF, bool V, bool NT>
 __global__ void __launch_bounds__(kThreads) k_quantise_rows(QuantArgs a, int64_t n8) {
   for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
     const int64_t first = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(kThreads) k_quantise_rows(QuantArgs a, int64_t
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int64_t i = first + u * kThreads;
-      if (i < n8) e[u].template load<V>(a.x, row * a.ld + i * 8);
+      if (i < n8) e[u].template load<V, NT>(a.x, row * a.ld + i * 8);
       else e[u].zero();
     }
 #pragma unroll
@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kThreads) k_quantise_rows(QuantArgs a, int64_t
 
 // FRAG16: a wave a quad fragment.  Lane 16 r4 + 4 b + g has row 4 u + r4, columns 32 b + 8 g .. + 7, whose codes
 // are bytes 4 b .. + 3 of the fragment's lane 16 g + row.
-template <bool BF, bool V>
+template <bool BF, bool V, bool NT>
 __global__ void __launch_bounds__(kThreads) k_quantise_frag(QuantArgs a, int64_t quads, int32_t per_row) {
   const int lane = threadIdx.x & 63;
   const int64_t q = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kThreads) k_quantise_frag(QuantArgs a, int64_t
   Eight<BF> e[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u)
-    e[u].template load<V>(a.x, (rb * 16 + 4 * u + r4) * a.ld + (int64_t)kq * 128 + 32 * b + 8 * g);
+    e[u].template load<V, NT>(a.x, (rb * 16 + 4 * u + r4) * a.ld + (int64_t)kq * 128 + 32 * b + 8 * g);
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int row = 4 * u + r4;
@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kThreads) k_quantise_frag(QuantArgs a, int64_t
 
 // TILE32: a block a tile, a wave 8 of its rows.  Lane 8 r + 4 h + q has row 8 w + r, columns
 // 64 j + 32 h + 8 q .. + 7.
-template <bool BF, bool V>
+template <bool BF, bool V, bool NT>
 __global__ void __launch_bounds__(kThreads) k_quantise_tile(QuantArgs a, int64_t tiles, int32_t per_row) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int r = 8 * w + (lane >> 3), h = (lane >> 2) & 1, q = lane & 3;
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kThreads) k_quantise_tile(QuantArgs a, int64_t
     Eight<BF> e[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (row < a.rows && c0 + 64 * j < a.cols) e[j].template load<V>(a.x, row * a.ld + c0 + 64 * j);
+      if (row < a.rows && c0 + 64 * j < a.cols) e[j].template load<V, NT>(a.x, row * a.ld + c0 + 64 * j);
       else e[j].zero();
     }
     uint8_t* out = a.codes + tile * kTileBytes;
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kThreads) k_quantise_tile(QuantArgs a, int64_t
 
 // Eight values of the codes c and the scale byte s: an e2m1 value times 2^(s - 127) from integer and exact
 // fp32 steps (twice the value, an integer up to 12, then a power of two that may be below the normal range).
-template <bool BF, bool V>
+template <bool BF, bool V, bool NT>
 __device__ __forceinline__ void store8(void* base, int64_t i, uint32_t c, uint32_t s) {
   float v[8];
 #pragma unroll
@@ -120,7 +120,7 @@ __device__ __forceinline__ void store8(void* base, int64_t i, uint32_t c, uint32
 #pragma unroll
     for (int j = 0; j < 4; ++j) q[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
     if constexpr (V) {
-      *reinterpret_cast<uint4*>(p) = make_uint4(q[0], q[1], q[2], q[3]);
+      store16<NT>(p, make_uint4(q[0], q[1], q[2], q[3]));
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) p[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
@@ -128,8 +128,8 @@ __device__ __forceinline__ void store8(void* base, int64_t i, uint32_t c, uint32
   } else {
     float* p = static_cast<float*>(base) + i;
     if constexpr (V) {
-      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      store16<NT>(p, __builtin_bit_cast(uint4, make_float4(v[0], v[1], v[2], v[3])));
+      store16<NT>(p + 4, __builtin_bit_cast(uint4, make_float4(v[4], v[5], v[6], v[7])));
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) p[j] = v[j];
@@ -137,7 +137,7 @@ __device__ __forceinline__ void store8(void* base, int64_t i, uint32_t c, uint32
   }
 }
 
-template <bool BF, bool V>
+template <bool BF, bool V, bool NT>
 __global__ void __launch_bounds__(kThreads) k_dequantise_rows(QuantArgs a, int64_t n8) {
   for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
     const int64_t first = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
@@ -145,13 +145,13 @@ __global__ void __launch_bounds__(kThreads) k_dequantise_rows(QuantArgs a, int64
     for (int u = 0; u < kUnroll; ++u) {
       const int64_t i = first + u * kThreads;
       if (i >= n8) continue;
-      store8<BF, V>(a.x, row * a.ld + i * 8, reinterpret_cast<const uint32_t*>(a.codes)[row * n8 + i],
+      store8<BF, V, NT>(a.x, row * a.ld + i * 8, reinterpret_cast<const uint32_t*>(a.codes)[row * n8 + i],
                     a.scales[(row * n8 + i) >> 2]);
     }
   }
 }
 
-template <bool BF, bool V>
+template <bool BF, bool V, bool NT>
 __global__ void __launch_bounds__(kThreads) k_dequantise_frag(QuantArgs a, int64_t quads, int32_t per_row) {
   const int lane = threadIdx.x & 63;
   const int64_t q = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -163,12 +163,12 @@ __global__ void __launch_bounds__(kThreads) k_dequantise_frag(QuantArgs a, int64
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int row = 4 * u + r4;
-    store8<BF, V>(a.x, (rb * 16 + row) * a.ld + (int64_t)kq * 128 + 32 * b + 8 * g,
+    store8<BF, V, NT>(a.x, (rb * 16 + row) * a.ld + (int64_t)kq * 128 + 32 * b + 8 * g,
                   *reinterpret_cast<const uint32_t*>(in + (row + 16 * g) * 16 + 4 * b), in[1024 + 4 * row + b]);
   }
 }
 
-template <bool BF, bool V>
+template <bool BF, bool V, bool NT>
 __global__ void __launch_bounds__(kThreads) k_dequantise_tile(QuantArgs a, int64_t tiles, int32_t per_row) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int r = 8 * w + (lane >> 3), h = (lane >> 2) & 1, q = lane & 3;
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kThreads) k_dequantise_tile(QuantArgs a, int64
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (c0 + 64 * j < a.cols)
-        store8<BF, V>(a.x, row * a.ld + c0 + 64 * j,
+        store8<BF, V, NT>(a.x, row * a.ld + c0 + 64 * j,
                       *reinterpret_cast<const uint32_t*>(in + 1024 * j + 16 * (32 * h + r) + 4 * q),
                       (sc >> (8 * j)) & 255u);
   }
@@ -217,12 +217,20 @@ __global__ void __launch_bounds__(kThreads) k_pack_tile(const uint8_t* __restric
 
 constexpr int64_t kMaxGrid = 1 << 20;
 
+// Bytes of x from which its accesses carry the nontemporal hint: what no longer fits the 256 MB cache in front of HBM is
+// not worth keeping there.  bf16, quantise / dequantise over and over: 470 MiB 95 / 91 us with the hint, 111 / 126
+// without; 256 MiB 54 / 52 and 60 / 72; 128 MiB 28 / 28 and 25 / 29, there the next reader finds the values cached.
+constexpr int64_t kNontemporal = (int64_t)256 << 20;
+
 template <class F>
-hipError_t by_type(bool bf, bool vec, F f) {
+hipError_t by_type(bool bf, bool vec, bool nt, F f) {
   using std::false_type;
   using std::true_type;
-  if (bf) return vec ? f(true_type{}, true_type{}) : f(true_type{}, false_type{});
-  return vec ? f(false_type{}, true_type{}) : f(false_type{}, false_type{});
+  const auto typed = [&](auto b) {
+    if (!vec) return f(b, false_type{}, false_type{});
+    return nt ? f(b, true_type{}, true_type{}) : f(b, true_type{}, false_type{});
+  };
+  return bf ? typed(true_type{}) : typed(false_type{});
 }
 
 // 16-byte accesses of eights: rows start 16-byte aligned.
@@ -234,8 +242,9 @@ template <bool QUANT>
 hipError_t launch(QuantArgs a, bool bf, int32_t layout, hipStream_t stream) {
   if (a.rows == 0) return hipSuccess;
   const bool vec = vec_ok(a.x, a.ld, bf);
-  return by_type(bf, vec, [&](auto b, auto v) {
-    constexpr bool B = decltype(b)::value, V = decltype(v)::value;
+  const bool nt = a.rows * a.cols * (bf ? 2 : 4) >= kNontemporal;
+  return by_type(bf, vec, nt, [&](auto b, auto v, auto n) {
+    constexpr bool B = decltype(b)::value, V = decltype(v)::value, NT = decltype(n)::value;
     if (layout == DAMOE_LAYOUT_ROWMAJOR) {
       int64_t n8 = a.cols / 8;
       if (a.ld == a.cols) {  // one long row
@@ -243,20 +252,20 @@ hipError_t launch(QuantArgs a, bool bf, int32_t layout, hipStream_t stream) {
         a.rows = 1;
       }
       const dim3 grid((unsigned)tiles_of(n8, kThreads * kUnroll), (unsigned)std::min<int64_t>(a.rows, 65535));
-      if constexpr (QUANT) hipLaunchKernelGGL((k_quantise_rows<B, V>), grid, dim3(kThreads), 0, stream, a, n8);
-      else hipLaunchKernelGGL((k_dequantise_rows<B, V>), grid, dim3(kThreads), 0, stream, a, n8);
+      if constexpr (QUANT) hipLaunchKernelGGL((k_quantise_rows<B, V, NT>), grid, dim3(kThreads), 0, stream, a, n8);
+      else hipLaunchKernelGGL((k_dequantise_rows<B, V, NT>), grid, dim3(kThreads), 0, stream, a, n8);
     } else if (layout == DAMOE_LAYOUT_FRAG16) {
       const int32_t per_row = a.cols / 128;
       const int64_t quads = a.rows / 16 * per_row;
       const dim3 grid((unsigned)((quads + 3) / 4));
-      if constexpr (QUANT) hipLaunchKernelGGL((k_quantise_frag<B, V>), grid, dim3(kThreads), 0, stream, a, quads, per_row);
-      else hipLaunchKernelGGL((k_dequantise_frag<B, V>), grid, dim3(kThreads), 0, stream, a, quads, per_row);
+      if constexpr (QUANT) hipLaunchKernelGGL((k_quantise_frag<B, V, NT>), grid, dim3(kThreads), 0, stream, a, quads, per_row);
+      else hipLaunchKernelGGL((k_dequantise_frag<B, V, NT>), grid, dim3(kThreads), 0, stream, a, quads, per_row);
     } else {
       const int32_t per_row = (int32_t)tiles_of(a.cols, kTileCols);
       const int64_t tiles = tiles_of(a.rows, kTileRows) * per_row;
       const dim3 grid((unsigned)std::min(tiles, kMaxGrid));
-      if constexpr (QUANT) hipLaunchKernelGGL((k_quantise_tile<B, V>), grid, dim3(kThreads), 0, stream, a, tiles, per_row);
-      else hipLaunchKernelGGL((k_dequantise_tile<B, V>), grid, dim3(kThreads), 0, stream, a, tiles, per_row);
+      if constexpr (QUANT) hipLaunchKernelGGL((k_quantise_tile<B, V, NT>), grid, dim3(kThreads), 0, stream, a, tiles, per_row);
+      else hipLaunchKernelGGL((k_dequantise_tile<B, V, NT>), grid, dim3(kThreads), 0, stream, a, tiles, per_row);
     }
     return hipGetLastError();
   });

@@ -13,19 +13,25 @@
 // bound at few.
 //
 // Forward: a block takes a chunk of tokens and, for each sequence that it meets, writes one slot of partial
-// sums (probabilities, counts, z, tokens).  Block b's slot of sequence s is b + s: the slots of a walk over
-// the tokens, distinct while offsets do not decrease.  A block per sequence then adds its slots in order, so
-// the sums run in a fixed order, and a last block adds the sequences.
+// sums (probabilities and counts by expert, z, tokens).  Block b's slot of sequence s is b + s: the slots of a walk
+// over the tokens, distinct while offsets do not decrease.  The next launch adds the slots of each sequence, 32 experts
+// a block, in a fixed order, and a third one adds the sequences (the last block of the second could, found by an atomic
+// count, which takes as long as the launch).  One block adds the slots of a single sequence where they are few, and a
+// batch that fits one block takes one launch.
 #include "common.h"
 
 namespace damoe {
 namespace {
 
-constexpr int kRows = 4;          // rows of logits a wave holds at a time
-constexpr int kLossThreads = 256;
-constexpr int kLossWaves = kLossThreads / kWave;
-constexpr int kMaxChunks = 512;   // blocks of the forward pass: two per compute unit
-constexpr int kMinChunk = kRows * kLossWaves;
+constexpr int kLossThreads = 512;
+constexpr int kOneThreads = 1024;  // of the block that takes a small batch alone
+constexpr int kMaxChunks = 512;    // blocks of the forward pass: two per compute unit
+constexpr int kMinChunk = 4 * kLossThreads / kWave;
+constexpr int kGroup = 32;         // experts of a block that adds slots, where there are few sequences
+constexpr int kFewSeqs = 16;       // below this many sequences their blocks have 1024 threads, else 256
+constexpr int kManySeqs = 128;     // from here on a block adds all experts of a sequence
+constexpr int kGradThreads = 256;
+constexpr int kGradWaves = kGradThreads / kWave;
 
 // Tokens of a block of the forward pass.
 __host__ __device__ inline int32_t chunk_tokens(int32_t T) {
@@ -42,10 +48,12 @@ struct LossArgs {
   int32_t T, E, k, S;
   int32_t chunk, nb;   // tokens of a block, blocks
   int32_t* err;
-  float* part_p;       // [nb + S][E]
-  int32_t* part_c;     // [nb + S][E]
+  float2* part;        // [nb + S][Ep]: sum of p, bits of the count
+  int32_t Ep;          // E rounded up to kGroup
+  int32_t width;       // experts of a block that adds slots
   float2* part_zn;     // [nb + S]: sum of lse^2, bits of the valid tokens
-  float2* seq_lz;      // [S]: sum_e f P, sum of lse^2
+  double* seq_l;       // [S][Ep / width]: sum over the group's experts of f P
+  float* seq_z;        // [S]: sum of lse^2
   float alpha, z_coef;
   float* loss;
   int32_t* counts;
@@ -99,7 +107,9 @@ __device__ __forceinline__ float wave_sum(float x) {
   return wave_all(x, [](float a, float b) { return a + b; });
 }
 
-__device__ __forceinline__ float exp_f(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896f); }
+constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
+
+__device__ __forceinline__ float exp_f(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // LDS of a wave's own: what other lanes of the wave wrote before is read after it.
 __device__ __forceinline__ void wave_fence() {
@@ -109,9 +119,10 @@ __device__ __forceinline__ void wave_fence() {
 
 // ---------------------------------------------------------------- rows
 
-// A lane's V * NC values of a row: columns 64 V c + V lane + i.  V = 4 wants rows of whole aligned fours.
+// A lane's V * NC values of a row: columns 64 V c + V lane + i.  V = 4 and 2 want rows of whole aligned fours or twos.
 template <int V, int NC, bool BF>
 struct Row {
+  typedef float Vec __attribute__((ext_vector_type(V)));
   float v[V * NC];
 
   static __device__ __forceinline__ int col(int c, int lane) { return (c * kWave + lane) * V; }
@@ -123,32 +134,34 @@ struct Row {
       if (e < E) {
         if constexpr (BF) {
           const uint16_t* p = static_cast<const uint16_t*>(base) + row * ld + e;
-          if constexpr (V == 4) {
-            const uint2 q = *reinterpret_cast<const uint2*>(p);
-            v[4 * c] = __uint_as_float(q.x << 16);
-            v[4 * c + 1] = __uint_as_float(q.x & 0xFFFF0000u);
-            v[4 * c + 2] = __uint_as_float(q.y << 16);
-            v[4 * c + 3] = __uint_as_float(q.y & 0xFFFF0000u);
-          } else {
+          if constexpr (V == 1) {
             v[c] = bf16_to_f32(*p);
+          } else {
+            uint32_t q[V / 2];
+            if constexpr (V == 4) {
+              const uint2 u = *reinterpret_cast<const uint2*>(p);
+              q[0] = u.x, q[1] = u.y;
+            } else {
+              q[0] = *reinterpret_cast<const uint32_t*>(p);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[V * c + i] = __uint_as_float(i & 1 ? q[i / 2] & 0xFFFF0000u : q[i / 2] << 16);
           }
         } else {
-          const float* p = static_cast<const float*>(base) + row * ld + e;
-          if constexpr (V == 4) {
-            const float4 q = *reinterpret_cast<const float4*>(p);
-            v[4 * c] = q.x;
-            v[4 * c + 1] = q.y;
-            v[4 * c + 2] = q.z;
-            v[4 * c + 3] = q.w;
-          } else {
-            v[c] = *p;
-          }
+          const Vec q = *reinterpret_cast<const Vec*>(static_cast<const float*>(base) + row * ld + e);
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[V * c + i] = q[i];
         }
       } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[V * c + i] = fill;
       }
     }
+  }
+
+  __device__ __forceinline__ void fill(float x) {
+#pragma unroll
+    for (int i = 0; i < V * NC; ++i) v[i] = x;
   }
 
   __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int E, int lane) const {
@@ -158,21 +171,20 @@ struct Row {
       if (e >= E) continue;
       if constexpr (BF) {
         uint16_t* p = static_cast<uint16_t*>(base) + row * ld + e;
-        if constexpr (V == 4) {
-          uint2 q;
-          q.x = (uint32_t)bf16_of(v[4 * c]) | (uint32_t)bf16_of(v[4 * c + 1]) << 16;
-          q.y = (uint32_t)bf16_of(v[4 * c + 2]) | (uint32_t)bf16_of(v[4 * c + 3]) << 16;
-          *reinterpret_cast<uint2*>(p) = q;
-        } else {
+        if constexpr (V == 1) {
           *p = bf16_of(v[c]);
+        } else {
+          uint32_t q[V / 2];
+#pragma unroll
+          for (int i = 0; i < V / 2; ++i) q[i] = (uint32_t)bf16_of(v[V * c + 2 * i]) | (uint32_t)bf16_of(v[V * c + 2 * i + 1]) << 16;
+          if constexpr (V == 4) *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
+          else *reinterpret_cast<uint32_t*>(p) = q[0];
         }
       } else {
-        float* p = static_cast<float*>(base) + row * ld + e;
-        if constexpr (V == 4) {
-          *reinterpret_cast<float4*>(p) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-        } else {
-          *p = v[c];
-        }
+        Vec q;
+#pragma unroll
+        for (int i = 0; i < V; ++i) q[i] = v[V * c + i];
+        *reinterpret_cast<Vec*>(static_cast<float*>(base) + row * ld + e) = q;
       }
     }
   }
@@ -188,18 +200,19 @@ struct Row {
   }
 };
 
-// exp(l - m) of a row with maximum m; all 0 where the row is -inf throughout (-inf - -inf would be NaN).
+// exp(l - m), m the row's maximum.  (l log2 e - m log2 e in one fma would be an instruction less, but is off by the
+// rounding of m log2 e, which is anything at the type's largest magnitudes.)
 __device__ __forceinline__ float shifted_exp(float l, float m) { return exp_f(l - m); }
 
-// sigmoid(l) over a common factor of the row with maximum m: sigmoid(l) = e^min(l, 0) / (1 + e^-|l|), and the
-// row's largest keeps a numerator of 1, so that rows of very negative logits do not underflow.
-__device__ __forceinline__ float shifted_sigmoid(float l, float m) {
-  return exp_f(fminf(l, 0.f) - fminf(m, 0.f)) * __builtin_amdgcn_rcpf(1.f + exp_f(-fabsf(l)));
-}
+__device__ __forceinline__ float lse_of(float m, float sum) { return m + __builtin_amdgcn_logf(sum) * kLn2; }
 
-// 1 - sigmoid(l) = sigmoid(-l)
-__device__ __forceinline__ float one_minus_sigmoid(float l) {
-  return exp_f(fminf(-l, 0.f)) * __builtin_amdgcn_rcpf(1.f + exp_f(-fabsf(l)));
+// Sigmoids of a row with maximum m: with e = exp(-|l|) and r = 1 / (1 + e), sigmoid(l) is r or e r and 1 - sigmoid(l)
+// the other.  Where the whole row is negative, sigmoid(l) exp(-m) = exp(l - m) r takes its place: p is the same, and rows
+// of very negative logits do not underflow.  ex: shifted_exp of l.
+__device__ __forceinline__ float2 sigmoids(float l, float ex, float m) {
+  const float e = exp_f(-fabsf(l)), r = __builtin_amdgcn_rcpf(1.f + e);
+  const float big = r, small = e * r;
+  return make_float2(m < 0.f ? ex * r : l >= 0.f ? big : small, l >= 0.f ? small : big);
 }
 
 __device__ __forceinline__ int offset_at(const int32_t* off, int32_t s, int32_t T) {
@@ -208,131 +221,6 @@ __device__ __forceinline__ int offset_at(const int32_t* off, int32_t s, int32_t 
 }
 
 // ---------------------------------------------------------------- forward
-
-template <int V, int NC, bool BF, bool SIG>
-__global__ void __launch_bounds__(kLossThreads) k_router_loss(LossArgs a) {
-  extern __shared__ float loss_smem[];
-  float* const red = loss_smem;                                                // [waves][E]
-  int32_t* const hist = reinterpret_cast<int32_t*>(red + kLossWaves * a.E);    // [E]
-  __shared__ float z_red[kLossWaves];
-  __shared__ int32_t n_red[kLossWaves];
-  __shared__ int32_t first;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int E = a.E, k = a.k;
-  const int t0 = blockIdx.x * a.chunk, t1 = min(t0 + a.chunk, a.T);
-  const float kNegInf = -__builtin_huge_valf();
-
-  // The first sequence that may reach past t0: the number of ends at or before it.
-  if (tid == 0) first = 0;
-  for (int e = tid; e < E; e += kLossThreads) hist[e] = 0;
-  __syncthreads();
-  if (a.off) {
-    int n = 0;
-    for (int s = tid; s < a.S; s += kLossThreads) n += offset_at(a.off, s + 1, a.T) <= t0;
-    if (n) atomicAdd(&first, n);
-    __syncthreads();
-  }
-  for (int s = first; s < a.S; ++s) {
-    const int b0 = offset_at(a.off, s, a.T), b1 = offset_at(a.off, s + 1, a.T);
-    if (b0 >= t1) break;
-    const int lo = max(t0, b0), hi = min(t1, b1);
-    if (lo >= hi) continue;
-    float acc[V * NC];
-#pragma unroll
-    for (int i = 0; i < V * NC; ++i) acc[i] = 0.f;
-    float zsum = 0.f;
-    int n = 0;
-    for (int t = lo + w * kRows; t < hi; t += kLossWaves * kRows) {
-      Row<V, NC, BF> r[kRows];
-      bool ok[kRows];
-#pragma unroll
-      for (int u = 0; u < kRows; ++u) ok[u] = t + u < hi && (!a.mask || a.mask[t + u] != 0);
-#pragma unroll
-      for (int u = 0; u < kRows; ++u) {
-        if (ok[u]) {
-          r[u].load(a.logits, t + u, a.ld, E, lane, kNegInf);
-        } else {
-#pragma unroll
-          for (int i = 0; i < V * NC; ++i) r[u].v[i] = 0.f;
-        }
-      }
-      // The slots of the kRows tokens, one a lane (k <= 16).
-      if (lane < kRows * k) {
-        const int u = lane / k;
-        if (t + u < hi && (!a.mask || a.mask[t + u] != 0)) {
-          const int id = a.ids[(int64_t)t * k + lane];
-          if (id >= E) atomicOr(a.err, DAMOE_DEVERR_EXPERT_ID);
-          else if (id >= 0) atomicAdd(&hist[id], 1);
-        }
-      }
-      float m[kRows], sum[kRows], inv[kRows];
-#pragma unroll
-      for (int u = 0; u < kRows; ++u) m[u] = wave_max(r[u].max());
-#pragma unroll
-      for (int u = 0; u < kRows; ++u) {
-        const float mm = m[u] == kNegInf ? 0.f : m[u];  // a row of -inf alone: every term 0
-        sum[u] = 0.f;
-        float sg = 0.f;
-#pragma unroll
-        for (int i = 0; i < V * NC; ++i) {
-          const float l = r[u].v[i], x = shifted_exp(l, mm);
-          sum[u] += x;
-          if constexpr (SIG) {
-            r[u].v[i] = shifted_sigmoid(l, mm);
-            sg += r[u].v[i];
-          } else {
-            r[u].v[i] = x;
-          }
-        }
-        sum[u] = wave_sum(sum[u]);
-        inv[u] = SIG ? wave_sum(sg) : sum[u];
-      }
-#pragma unroll
-      for (int u = 0; u < kRows; ++u) {
-        if (!ok[u]) continue;
-        ++n;
-        if (m[u] == kNegInf) continue;
-        const float lse = m[u] + __logf(sum[u]);
-        zsum += lse * lse;
-        const float f = 1.f / inv[u];
-#pragma unroll
-        for (int i = 0; i < V * NC; ++i) acc[i] += r[u].v[i] * f;
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int e = Row<V, NC, BF>::col(c, lane) + i;
-        if (e < E) red[w * E + e] = acc[V * c + i];
-      }
-    if (lane == 0) {
-      z_red[w] = zsum;
-      n_red[w] = n;
-    }
-    __syncthreads();
-    const int64_t slot = (int64_t)blockIdx.x + s;
-    for (int e = tid; e < E; e += kLossThreads) {
-      float p = 0.f;
-#pragma unroll
-      for (int i = 0; i < kLossWaves; ++i) p += red[i * E + e];
-      a.part_p[slot * E + e] = p;
-      a.part_c[slot * E + e] = hist[e];
-      hist[e] = 0;
-    }
-    if (tid == 0) {
-      float z = 0.f;
-      int nn = 0;
-      for (int i = 0; i < kLossWaves; ++i) {
-        z += z_red[i];
-        nn += n_red[i];
-      }
-      a.part_zn[slot] = make_float2(z, __int_as_float(nn));
-    }
-    __syncthreads();
-  }
-}
 
 __device__ __forceinline__ void write_loss(const LossArgs& a, double balance, double z, int n_seq, int n_tok) {
   const float b = n_seq > 0 ? (float)(balance / n_seq) : 0.f;
@@ -344,16 +232,23 @@ __device__ __forceinline__ void write_loss(const LossArgs& a, double balance, do
   a.tokens[a.S + 1] = n_tok;
 }
 
-constexpr int kSeqThreads = 1024;
+constexpr int kAloneThreads = 1024;
 
-// A block per sequence: its slots added in order, f and P, and their product's sum.
-__global__ void __launch_bounds__(kSeqThreads) k_router_loss_seq(LossArgs a) {
-  __shared__ float p_red[kSeqThreads];
-  __shared__ int32_t c_red[kSeqThreads];
-  __shared__ double lz[kSeqThreads / kWave];
-  __shared__ float z_tot;
-  __shared__ int32_t n_tot;
-  const int tid = threadIdx.x, E = a.E, s = blockIdx.x;
+template <int THREADS>
+struct SeqSmem {
+  float4 p[THREADS];
+  double l[THREADS / kWave];
+  float z;
+  int32_t n;
+};
+
+// Sequence s, `width` experts (an even number) from e0 on: its slots added in order, f, P and their product's sum, which
+// thread 0 returns with z and n.  Thread lanes r + c adds every split-th slot from r on, two experts at a time (more
+// than 512 experts: a block of 256 threads goes over them in turn).
+template <int THREADS>
+__device__ __forceinline__ double add_slots(const LossArgs& a, SeqSmem<THREADS>& sm, int s, int e0, int width) {
+  const int tid = threadIdx.x, lanes = min(width / 2, THREADS), split = THREADS / lanes;
+  const int r = tid / lanes, c = tid - r * lanes;
   const int o0 = offset_at(a.off, s, a.T), o1 = offset_at(a.off, s + 1, a.T);
   const int b0 = o0 / a.chunk;
   const int nslot = o1 > o0 ? min((o1 - 1) / a.chunk, a.nb - 1) - b0 + 1 : 0;
@@ -369,67 +264,102 @@ __global__ void __launch_bounds__(kSeqThreads) k_router_loss_seq(LossArgs a) {
     z = wave_sum(z);
     for (int d = 1; d < kWave; d <<= 1) n += __shfl_xor(n, d);
     if (tid == 0) {
-      z_tot = z;
-      n_tot = n;
-      a.tokens[s] = n;
+      sm.z = z;
+      sm.n = n;
     }
   }
-  __syncthreads();
-  const int n = n_tot;
   double l = 0.0;
-  // Columns in passes of `cols`; the threads of a column share its slots.
-  const int cols = min((E + kWave - 1) / kWave * kWave, kSeqThreads), split = kSeqThreads / cols;
-  const int c = tid % cols, g = tid / cols;
-  for (int e0 = 0; e0 < E; e0 += cols) {
-    const int e = e0 + c;
-    float p = 0.f;
-    int cnt = 0;
-    if (e < E && g < split) {
-      for (int i = g; i < nslot; i += split) {
-        p += a.part_p[(base + i) * E + e];
-        cnt += a.part_c[(base + i) * E + e];
+  for (int w0 = 0; w0 < width; w0 += 2 * lanes) {
+    float p0 = 0.f, p1 = 0.f;
+    int c0 = 0, c1 = 0;
+    const bool in = r < split && w0 + 2 * c < width;
+    if (in) {
+      const float4* q = reinterpret_cast<const float4*>(a.part + base * a.Ep + e0 + w0) + c;
+#pragma unroll 8
+      for (int i = r; i < nslot; i += split) {
+        const float4 v = q[(int64_t)i * (a.Ep / 2)];
+        p0 += v.x, p1 += v.z;
+        c0 += __float_as_int(v.y), c1 += __float_as_int(v.w);
       }
     }
-    p_red[tid] = p;
-    c_red[tid] = cnt;
+    sm.p[tid] = make_float4(p0, __int_as_float(c0), p1, __int_as_float(c1));
     __syncthreads();
-    if (g == 0 && e < E) {
-      for (int i = 1; i < split; ++i) {
-        p += p_red[i * cols + c];
-        cnt += c_red[i * cols + c];
+    for (int m = split, h; m > 1; m = h) {  // the upper half's sums into the lower half's
+      h = (m + 1) / 2;
+      if (r < m - h) {
+        float4 v = sm.p[tid];
+        const float4 o = sm.p[tid + h * lanes];
+        v.x += o.x, v.z += o.z;
+        v.y = __int_as_float(__float_as_int(v.y) + __float_as_int(o.y));
+        v.w = __int_as_float(__float_as_int(v.w) + __float_as_int(o.w));
+        sm.p[tid] = v;
       }
-      const float P = n > 0 ? p / (float)n : 0.f;
-      a.counts[(int64_t)s * E + e] = cnt;
-      if (a.probs) a.probs[(int64_t)s * E + e] = P;
-      if (n > 0) l += (double)E * cnt / ((double)a.k * n) * P;
+      __syncthreads();
+    }
+    const int n = sm.n;
+    if (r == 0 && in) {
+      const float4 v = sm.p[tid];
+      const float p[2] = {v.x, v.z};
+      const int cnt[2] = {__float_as_int(v.y), __float_as_int(v.w)};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int e = e0 + w0 + 2 * c + i;
+        if (e >= a.E) continue;
+        const float P = n > 0 ? p[i] / (float)n : 0.f;
+        a.counts[(int64_t)s * a.E + e] = cnt[i];
+        if (a.probs) a.probs[(int64_t)s * a.E + e] = P;
+        if (n > 0) l += (double)a.E * cnt[i] / ((double)a.k * n) * P;
+      }
     }
     __syncthreads();
   }
   for (int d = 1; d < kWave; d <<= 1) l += __shfl_xor(l, d);
-  if ((tid & 63) == 0) lz[tid >> 6] = l;
+  if ((tid & 63) == 0) sm.l[tid >> 6] = l;
   __syncthreads();
-  if (tid == 0) {
-    l = 0.0;
-    for (int i = 0; i < kSeqThreads / kWave; ++i) l += lz[i];
-    if (a.S == 1) write_loss(a, l, z_tot, n > 0, n);
-    else a.seq_lz[s] = make_float2((float)l, z_tot);
+  if (tid == 0)
+    for (int i = 1; i < THREADS / kWave; ++i) l += sm.l[i];
+  return l;
+}
+
+// A block for a group of experts of a sequence.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) k_router_loss_seq(LossArgs a) {
+  __shared__ SeqSmem<THREADS> sm;
+  const int G = a.Ep / a.width, s = blockIdx.x / G, g = blockIdx.x % G;
+  const double l = add_slots(a, sm, s, g * a.width, a.width);
+  if (threadIdx.x == 0) {
+    a.seq_l[(int64_t)s * G + g] = l;
+    if (g == 0) {
+      a.seq_z[s] = sm.z;
+      a.tokens[s] = sm.n;
+    }
   }
 }
 
-// The sum over sequences, in a fixed order.
-__global__ void __launch_bounds__(256) k_router_loss_total(LossArgs a) {
-  __shared__ double red[3][4];
-  __shared__ int64_t n_red[4];
+// One block for all of a single sequence.
+__global__ void __launch_bounds__(kAloneThreads) k_router_loss_alone(LossArgs a) {
+  __shared__ SeqSmem<kAloneThreads> sm;
+  const double l = add_slots(a, sm, 0, 0, a.Ep);
+  if (threadIdx.x == 0) {
+    a.tokens[0] = sm.n;
+    write_loss(a, l, sm.z, sm.n > 0, sm.n);
+  }
+}
+
+// The sum over sequences, by one block in a fixed order (what a sequence without tokens left is 0).
+__global__ void __launch_bounds__(kAloneThreads) k_router_loss_total(LossArgs a) {
+  __shared__ double red[(kAloneThreads / kWave)][4];
   const int tid = threadIdx.x;
+  const int64_t m = (int64_t)a.S * (a.Ep / a.width);
   double l = 0, z = 0;
-  int64_t seqs = 0, n = 0;
-  for (int s = tid; s < a.S; s += 256) {
+  int seqs = 0, n = 0;
+#pragma unroll 4
+  for (int64_t i = tid; i < m; i += kAloneThreads) l += a.seq_l[i];
+#pragma unroll 4
+  for (int s = tid; s < a.S; s += kAloneThreads) {
     const int ns = a.tokens[s];
-    if (ns <= 0) continue;
-    const float2 q = a.seq_lz[s];
-    l += q.x;
-    z += q.y;
-    ++seqs;
+    z += a.seq_z[s];
+    seqs += ns > 0;
     n += ns;
   }
   for (int d = 1; d < kWave; d <<= 1) {
@@ -439,50 +369,333 @@ __global__ void __launch_bounds__(256) k_router_loss_total(LossArgs a) {
     n += __shfl_xor(n, d);
   }
   if ((tid & 63) == 0) {
-    red[0][tid >> 6] = l;
-    red[1][tid >> 6] = z;
-    red[2][tid >> 6] = (double)seqs;
-    n_red[tid >> 6] = n;
+    double* const q = red[tid >> 6];
+    q[0] = l, q[1] = z, q[2] = seqs, q[3] = n;
   }
   __syncthreads();
   if (tid == 0) {
-    for (int i = 1; i < 4; ++i) {
-      l += red[0][i];
-      z += red[1][i];
-      seqs += (int64_t)red[2][i];
-      n += n_red[i];
+    for (int i = 1; i < (kAloneThreads / kWave); ++i) {
+      l += red[i][0];
+      z += red[i][1];
+      seqs += (int)red[i][2];
+      n += (int)red[i][3];
     }
-    write_loss(a, l, z, (int)seqs, (int)n);
+    write_loss(a, l, z, seqs, n);
   }
+}
+
+// ONE: the batch is one block's, which has every sequence's sums and finishes them.
+template <int V, int NC, bool BF, bool SIG, bool ONE>
+__global__ void __launch_bounds__(ONE ? kOneThreads : kLossThreads) k_router_loss(LossArgs a) {
+  constexpr int kThreads = ONE ? kOneThreads : kLossThreads, kWaves = kThreads / kWave;
+  // Rows of logits a wave holds at a time.
+  constexpr int kRows = V * NC <= 4 ? 4 : V * NC <= 8 ? 2 : 1;
+  extern __shared__ __attribute__((aligned(16))) float loss_smem[];
+  float* const red = loss_smem;                                          // [kWaves / 2][E]
+  int32_t* const hist = reinterpret_cast<int32_t*>(red + kWaves / 2 * a.E);  // [E]
+  __shared__ float z_red[kWaves];
+  __shared__ int32_t n_red[kWaves];
+  __shared__ double l_red[kWaves];
+  __shared__ int32_t first;
+  double l_sum = 0.0, z_sum = 0.0;  // ONE, thread 0: over the sequences so far
+  int seqs = 0, n_sum = 0;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int E = a.E, k = a.k;
+  const int t0 = blockIdx.x * a.chunk, t1 = min(t0 + a.chunk, a.T);
+  const float kNegInf = -__builtin_huge_valf();
+
+  // The first sequence that may reach past t0: the number of ends at or before it.
+  if (tid == 0) first = 0;
+  for (int e = tid; e < E; e += kThreads) hist[e] = 0;
+  __syncthreads();
+  if (!ONE && a.off) {
+    int n = 0;
+    for (int s = tid; s < a.S; s += kThreads) n += offset_at(a.off, s + 1, a.T) <= t0;
+    if (n) atomicAdd(&first, n);
+    __syncthreads();
+  }
+  for (int s = first; s < a.S; ++s) {
+    const int b0 = offset_at(a.off, s, a.T), b1 = offset_at(a.off, s + 1, a.T);
+    if (!ONE && b0 >= t1) break;
+    const int lo = max(t0, b0), hi = min(t1, b1);
+    if (!ONE && lo >= hi) continue;
+    float acc[V * NC];
+#pragma unroll
+    for (int i = 0; i < V * NC; ++i) acc[i] = 0.f;
+    float zsum = 0.f;
+    int n = 0;
+    // A wave's next rows are loaded before it works on the present ones.
+    Row<V, NC, BF> next[kRows];
+    uint32_t next_ok = 0;
+    int next_id = -1;
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+      next_ok = 0;
+      next_id = -1;
+      if (t >= hi) return;
+      // The slots of the rows' tokens, one a lane (16 a row), and from them which tokens are valid.
+      const int u = lane >> 4, j = lane & 15;
+      const bool in = u < kRows && t + u < hi && (!a.mask || a.mask[t + u] != 0);
+      if (in && j < k) next_id = a.ids[(int64_t)(t + u) * k + j];
+      const uint64_t ok = __ballot(in);
+#pragma unroll
+      for (int q = 0; q < kRows; ++q) {
+        if ((ok >> (16 * q)) & 1) {
+          next_ok |= 1u << q;
+          next[q].load(a.logits, t + q, a.ld, E, lane, kNegInf);
+        } else {
+          next[q].fill(0.f);
+        }
+      }
+    };
+    fetch(lo + w * kRows);
+    for (int t = lo + w * kRows; t < hi; t += kWaves * kRows) {
+      Row<V, NC, BF> r[kRows];
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) r[u] = next[u];
+      const uint32_t ok = next_ok;
+      const int id = next_id;
+      fetch(t + kWaves * kRows);
+      if (id >= E) atomicOr(a.err, DAMOE_DEVERR_EXPERT_ID);
+      else if (id >= 0) atomicAdd(&hist[id], 1);
+      float m[kRows], sum[kRows], inv[kRows];
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) m[u] = wave_max(r[u].max());
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        const float mm = m[u] == kNegInf ? 0.f : m[u];  // a row of -inf alone: every term 0
+        sum[u] = 0.f;
+        float sg = 0.f;
+#pragma unroll
+        for (int i = 0; i < V * NC; ++i) {
+          const float l = r[u].v[i], x = shifted_exp(l, mm);
+          sum[u] += x;
+          if constexpr (SIG) {
+            r[u].v[i] = sigmoids(l, x, mm).x;
+            sg += r[u].v[i];
+          } else {
+            r[u].v[i] = x;
+          }
+        }
+        inv[u] = sg;
+      }
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        sum[u] = wave_sum(sum[u]);
+        inv[u] = SIG ? wave_sum(inv[u]) : sum[u];
+      }
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        const bool live = ((ok >> u) & 1) && m[u] != kNegInf;
+        n += (ok >> u) & 1;
+        const float lse = lse_of(m[u], sum[u]), f = 1.f / inv[u];
+        if (!live) continue;
+        zsum += lse * lse;
+#pragma unroll
+        for (int i = 0; i < V * NC; ++i) acc[i] += r[u].v[i] * f;
+      }
+    }
+    // The waves' sums by expert: the upper half's go to LDS and into the lower half's, whose go there next.
+    auto put = [&](int row, bool add) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const int e = Row<V, NC, BF>::col(c, lane) + i;
+          if (e < E) red[row * E + e] = add ? red[row * E + e] + acc[V * c + i] : acc[V * c + i];
+        }
+    };
+    if (w >= kWaves / 2) put(w - kWaves / 2, false);
+    if (lane == 0) {
+      z_red[w] = zsum;
+      n_red[w] = n;
+    }
+    __syncthreads();
+    if (w < kWaves / 2) put(w, true);
+    __syncthreads();
+    float z = 0.f;
+    int nn = 0;
+    for (int i = 0; i < kWaves; ++i) {
+      z += z_red[i];
+      nn += n_red[i];
+    }
+    const int64_t slot = (int64_t)blockIdx.x + s;
+    double l = 0.0;
+    for (int e = tid; e < (ONE ? E : a.Ep); e += kThreads) {
+      float p = 0.f;
+      int cnt = 0;
+      if (e < E) {
+#pragma unroll
+        for (int i = 0; i < kWaves / 2; ++i) p += red[i * E + e];
+        cnt = hist[e];
+        hist[e] = 0;
+      }
+      if constexpr (ONE) {
+        const float P = nn > 0 ? p / (float)nn : 0.f;
+        a.counts[(int64_t)s * E + e] = cnt;
+        if (a.probs) a.probs[(int64_t)s * E + e] = P;
+        if (nn > 0) l += (double)E * cnt / ((double)k * nn) * P;
+      } else {
+        a.part[slot * a.Ep + e] = make_float2(p, __int_as_float(cnt));
+      }
+    }
+    if constexpr (ONE) {
+      for (int d = 1; d < kWave; d <<= 1) l += __shfl_xor(l, d);
+      if (lane == 0) l_red[w] = l;
+    } else if (tid == 0) {
+      a.part_zn[slot] = make_float2(z, __int_as_float(nn));
+    }
+    __syncthreads();
+    if (ONE && tid == 0) {
+      a.tokens[s] = nn;
+      if (nn > 0) {
+        for (int i = 0; i < kWaves; ++i) l_sum += l_red[i];
+        z_sum += z;
+        ++seqs;
+        n_sum += nn;
+      }
+    }
+  }
+  if (ONE && tid == 0) write_loss(a, l_sum, z_sum, seqs, n_sum);
 }
 
 // ---------------------------------------------------------------- gradient
 
+// Sum over the 16 lanes of a DPP row, in each of them.
+__device__ __forceinline__ float row16_sum(float x) {
+  x += dppf<0xB1>(x);
+  x += dppf<0x4E>(x);
+  x += dppf<0x141>(x);
+  return x + dppf<0x140>(x);
+}
+
 template <int V, int NC, bool BF, bool SIG>
-__global__ void __launch_bounds__(kLossThreads) k_router_loss_grad(GradArgs a) {
-  extern __shared__ float grad_smem[];  // [waves][E]: the gates' gradient of a row
+struct Grad {
+  static constexpr int kVals = V * NC;
+  // Rows a wave works on together where they lie in one sequence: fewer for sigmoids, whose registers would leave three
+  // waves a SIMD (65536 tokens, 384 experts: 47 us with two rows, 58 with four).
+  static constexpr int kRows = kVals <= 8 ? (SIG ? 2 : 4) : kVals <= 12 ? 2 : 1;
+  const GradArgs& a;
+  float* gate;  // LDS of the wave, [kRows][E], zero between rows
+  int lane;
+  float zc, bal;
+  float f[kVals];
+
+  // Rows t .. t + U - 1, all in the sequence of f and bal; those that are not valid get 0.
+  template <int U>
+  __device__ __forceinline__ void rows(int t) const {
+    const int E = a.E, k = a.k;
+    const float kNegInf = -__builtin_huge_valf();
+    const int u16 = lane >> 4, j = lane & 15;
+    const bool in = u16 < U && (!a.mask || a.mask[t + (u16 < U ? u16 : 0)] != 0);
+    const uint64_t ok = __ballot(in);
+    Row<V, NC, BF> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if ((ok >> (16 * u)) & 1) r[u].load(a.logits, t + u, a.ld, E, lane, kNegInf);
+      else r[u].fill(0.f);
+    }
+    if (a.w) {
+      // dw_j -> w_j (dw_j - sum_i w_i dw_i), added to the expert's column (twice for an id held twice).
+      int id = -1;
+      float wj = 0.f, dj = 0.f;
+      if (in && j < k) {
+        const int64_t i = (int64_t)(t + u16) * k + j;
+        id = a.ids[i];
+        if (id >= 0 && id < E) {
+          wj = a.w[i];
+          dj = a.dw[i];
+        }
+      }
+      const float dot = row16_sum(wj * dj);
+      wave_fence();
+      if (id >= 0 && id < E) atomicAdd(&gate[u16 * E + id], wj * (dj - dot));
+      wave_fence();
+    }
+    float m[U], sum[U], ps[U], fp[U], ex[U][kVals], p[SIG ? U : 1][kVals];
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = wave_max(r[u].max());
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float mm = m[u] == kNegInf ? 0.f : m[u];
+      sum[u] = ps[u] = fp[u] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) {
+        ex[u][i] = shifted_exp(r[u].v[i], mm);
+        sum[u] += ex[u][i];
+        if constexpr (SIG) {
+          const float2 sg = sigmoids(r[u].v[i], ex[u][i], mm);
+          p[u][i] = sg.x;
+          r[u].v[i] = sg.y;  // 1 - sigmoid
+          ps[u] += p[u][i];
+          fp[u] += p[u][i] * f[i];
+        } else {
+          fp[u] += ex[u][i] * f[i];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      sum[u] = wave_sum(sum[u]);
+      ps[u] = SIG ? wave_sum(ps[u]) : sum[u];
+      fp[u] = wave_sum(fp[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool live = m[u] != kNegInf;
+      const float ip = live ? 1.f / ps[u] : 0.f, dot = fp[u] * ip, b = bal * ip;
+      const float zt = live && a.z_coef != 0.f ? zc * lse_of(m[u], sum[u]) / sum[u] : 0.f;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) {
+        float d;
+        if constexpr (SIG) d = b * p[u][i] * (f[i] - dot) * r[u].v[i] + zt * ex[u][i];
+        else d = (b * (f[i] - dot) + zt) * ex[u][i];
+        r[u].v[i] = d;
+      }
+      if (a.w) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int e = Row<V, NC, BF>::col(c, lane);
+          if (e >= E) continue;
+          typedef typename Row<V, NC, BF>::Vec Vec;
+          Vec* const q = reinterpret_cast<Vec*>(gate + u * E + e);
+          const Vec x = *q;
+          *q = Vec(0.f);
+#pragma unroll
+          for (int i = 0; i < V; ++i) r[u].v[V * c + i] += x[i];
+        }
+      }
+      if (!((ok >> (16 * u)) & 1)) r[u].fill(0.f);
+      r[u].store(a.dlogits, t + u, a.ldd, E, lane);
+    }
+  }
+};
+
+template <int V, int NC, bool BF, bool SIG>
+__global__ void __launch_bounds__(kGradThreads) k_router_loss_grad(GradArgs a) {
+  using G = Grad<V, NC, BF, SIG>;
+  extern __shared__ __attribute__((aligned(16))) float grad_smem[];  // [waves][kRows][E]: the gates' gradient of rows
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int E = a.E, k = a.k;
-  float* const gate = grad_smem + w * E;
-  const int t0 = (blockIdx.x * kLossWaves + w) * a.run, t1 = min(t0 + a.run, a.T);
+  const int E = a.E;
+  const int t0 = (blockIdx.x * kGradWaves + w) * a.run, t1 = min(t0 + a.run, a.T);
   if (t0 >= t1) return;
-  const float kNegInf = -__builtin_huge_valf();
-  for (int e = lane; e < E; e += kWave) gate[e] = 0.f;
+  G d{a, grad_smem + w * G::kRows * E, lane};
+  if (a.w)
+    for (int e = lane; e < G::kRows * E; e += kWave) d.gate[e] = 0.f;
   const float g = a.dloss ? *a.dloss : 1.f;
   const float n_seq = (float)a.tokens[a.S], n_tok = (float)a.tokens[a.S + 1];
-  const float zc = a.z_coef != 0.f ? g * a.z_coef * 2.f / n_tok : 0.f;
+  d.zc = a.z_coef != 0.f ? g * a.z_coef * 2.f / n_tok : 0.f;
+  d.bal = 0.f;
 
-  int s = 0;
+  int s = 0;  // the number of ends at or before t0
   if (a.off) {
     for (int i = lane; i < a.S; i += kWave) s += offset_at(a.off, i + 1, a.T) <= t0;
-    for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d);
+    for (int q = 1; q < kWave; q <<= 1) s += __shfl_xor(s, q);
     s = __builtin_amdgcn_readfirstlane(s);
   }
   int begin = 0, end = -1, cur = -1;  // of sequence s once `cur` names it
-  float f[V * NC], bal = 0.f;
-  for (int t = t0; t < t1; ++t) {
-    // The sequence of t; its f in registers.
+  for (int t = t0; t < t1;) {
     while (s < a.S && (cur != s || t >= end)) {
       if (cur == s) ++s;
       if (s >= a.S) break;
@@ -491,93 +704,43 @@ __global__ void __launch_bounds__(kLossThreads) k_router_loss_grad(GradArgs a) {
       end = offset_at(a.off, s + 1, a.T);
       if (t < end) {
         const float n = (float)a.tokens[s];
-        bal = a.alpha != 0.f ? g * a.alpha / (n_seq * n) : 0.f;
-        const float fs = (float)E / ((float)k * n);
+        d.bal = a.alpha != 0.f ? g * a.alpha / (n_seq * n) : 0.f;
+        const float fs = (float)E / ((float)a.k * n);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             const int e = Row<V, NC, BF>::col(c, lane) + i;
-            f[V * c + i] = e < E ? fs * (float)a.counts[(int64_t)s * E + e] : 0.f;
+            d.f[V * c + i] = e < E ? fs * (float)a.counts[(int64_t)s * E + e] : 0.f;
           }
       }
     }
-    const bool ok = s < a.S && t >= begin && t < end && (!a.mask || a.mask[t] != 0);
-    Row<V, NC, BF> r;
-    if (!ok) {
-#pragma unroll
-      for (int i = 0; i < V * NC; ++i) r.v[i] = 0.f;
+    if (s >= a.S || t < begin) {  // in no sequence
+      Row<V, NC, BF> r;
+      r.fill(0.f);
       r.store(a.dlogits, t, a.ldd, E, lane);
-      continue;
+      ++t;
+    } else if (t + G::kRows <= min(t1, end)) {
+      d.template rows<G::kRows>(t);
+      t += G::kRows;
+    } else {
+      d.template rows<1>(t);
+      ++t;
     }
-    r.load(a.logits, t, a.ld, E, lane, kNegInf);
-    if (a.w) {
-      // dw_j -> w_j (dw_j - sum_i w_i dw_i), added to the expert's column (twice for an id held twice).
-      int id = -1;
-      float wj = 0.f, dj = 0.f;
-      if (lane < k) {
-        id = a.ids[(int64_t)t * k + lane];
-        if (id >= 0 && id < E) {
-          wj = a.w[(int64_t)t * k + lane];
-          dj = a.dw[(int64_t)t * k + lane];
-        }
-      }
-      const float dot = wave_sum(wj * dj);
-      wave_fence();
-      if (id >= 0 && id < E) atomicAdd(&gate[id], wj * (dj - dot));
-      wave_fence();
-    }
-    const float m = wave_max(r.max());
-    const float mm = m == kNegInf ? 0.f : m;
-    float sum = 0.f, ps = 0.f, fp = 0.f;
-    float ex[V * NC], p[V * NC];
-#pragma unroll
-    for (int i = 0; i < V * NC; ++i) {
-      ex[i] = shifted_exp(r.v[i], mm);
-      p[i] = SIG ? shifted_sigmoid(r.v[i], mm) : ex[i];
-      sum += ex[i];
-      ps += p[i];
-      fp += p[i] * f[i];
-    }
-    sum = wave_sum(sum);
-    ps = SIG ? wave_sum(ps) : sum;
-    fp = wave_sum(fp);
-    const bool live = m != kNegInf;
-    const float ip = live ? 1.f / ps : 0.f;
-    const float dot = fp * ip;
-    const float zt = live && a.z_coef != 0.f ? zc * (m + __logf(sum)) / sum : 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int j = V * c + i, e = Row<V, NC, BF>::col(c, lane) + i;
-        float d = bal * p[j] * ip * (f[j] - dot);
-        if constexpr (SIG) d *= one_minus_sigmoid(r.v[j]);
-        d += zt * ex[j];
-        if (a.w && e < E) {
-          d += gate[e];
-          gate[e] = 0.f;
-        }
-        r.v[j] = d;
-      }
-    r.store(a.dlogits, t, a.ldd, E, lane);
   }
 }
 
 // ---------------------------------------------------------------- launches
 
-// Columns a lane holds: fours where rows are whole aligned fours, else single ones; NC chunks of 64 V columns.
-template <template <int, int, bool, bool> class L, class A>
-hipError_t pick(const A& a, bool four, bool bf, bool sig, dim3 grid, size_t lds, hipStream_t stream) {
-  auto go = [&](auto v, auto nc) {
-    constexpr int V = decltype(v)::value, NC = decltype(nc)::value;
-    if (bf) return sig ? L<V, NC, true, true>::run(a, grid, lds, stream) : L<V, NC, true, false>::run(a, grid, lds, stream);
-    return sig ? L<V, NC, false, true>::run(a, grid, lds, stream) : L<V, NC, false, false>::run(a, grid, lds, stream);
-  };
+// Columns a lane holds: fours where rows are whole aligned fours (twos where those leave no lane idle), else single
+// ones; NC chunks of 64 V columns.
+template <class F>
+hipError_t by_columns(int32_t E, bool four, F f) {
+  const auto go = [&](auto v, auto nc) { return f(v, nc); };
   using std::integral_constant;
-  const int E = a.E;
   if (four) {
     const integral_constant<int, 4> v;
+    if (E > 256 && E <= 384) return go(integral_constant<int, 2>{}, integral_constant<int, 3>{});
     return E <= 256   ? go(v, integral_constant<int, 1>{})
            : E <= 512 ? go(v, integral_constant<int, 2>{})
                       : go(v, integral_constant<int, 4>{});
@@ -590,38 +753,39 @@ hipError_t pick(const A& a, bool four, bool bf, bool sig, dim3 grid, size_t lds,
                     : go(v, integral_constant<int, 16>{});
 }
 
-template <int V, int NC, bool BF, bool SIG>
-struct RunLoss {
-  static hipError_t run(const LossArgs& a, dim3 grid, size_t lds, hipStream_t stream) {
-    hipLaunchKernelGGL((k_router_loss<V, NC, BF, SIG>), grid, dim3(kLossThreads), lds, stream, a);
-    return hipGetLastError();
-  }
-};
+// f of the logits' type and the score as integral constants.
+template <class F>
+hipError_t by_kind(int32_t dtype, int32_t score, F f) {
+  using std::false_type;
+  using std::true_type;
+  const bool sig = score == DAMOE_SCORE_SIGMOID;
+  if (dtype == DAMOE_BF16) return sig ? f(true_type{}, true_type{}) : f(true_type{}, false_type{});
+  return sig ? f(false_type{}, true_type{}) : f(false_type{}, false_type{});
+}
 
-template <int V, int NC, bool BF, bool SIG>
-struct RunGrad {
-  static hipError_t run(const GradArgs& a, dim3 grid, size_t lds, hipStream_t stream) {
-    hipLaunchKernelGGL((k_router_loss_grad<V, NC, BF, SIG>), grid, dim3(kLossThreads), lds, stream, a);
-    return hipGetLastError();
-  }
-};
+// Tokens and sequences that one block takes alone.
+constexpr int32_t kOneTokens = 96, kOneSeqs = 2;
+// Partial sums of a single sequence that one block adds.
+constexpr size_t kAlonePartials = 65536;
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Workspace: control word, then the partial sums of nb + S slots, then the sequences'.
+// Workspace: the control word, then the partial sums of nb + S slots, then the sequences'.
 struct LossWs {
-  size_t p, c, zn, seq, total;
+  size_t part, zn, seq_l, seq_z, total;
 };
 
+int32_t padded(int32_t E) { return (E + kGroup - 1) / kGroup * kGroup; }
+
 LossWs loss_ws(int32_t T, int32_t E, int32_t S) {
-  const int32_t chunk = std::max(chunk_tokens(T), kMinChunk);
+  const int32_t chunk = std::max(chunk_tokens(T), kMinChunk), Ep = padded(E);
   const size_t slots = (size_t)((T + chunk - 1) / chunk) + S;
   LossWs o;
-  o.p = 256;
-  o.c = o.p + up256(slots * E * 4);
-  o.zn = o.c + up256(slots * E * 4);
-  o.seq = o.zn + up256(slots * 8);
-  o.total = o.seq + up256((size_t)S * 8);
+  o.part = 256;
+  o.zn = o.part + up256(slots * Ep * 8);
+  o.seq_l = o.zn + up256(slots * 8);
+  o.seq_z = o.seq_l + up256((size_t)S * (Ep / kGroup) * 8);
+  o.total = o.seq_z + up256((size_t)S * 4);
   return o;
 }
 
@@ -677,24 +841,41 @@ damoe_status damoe_router_loss(const void* logits, int32_t dtype, int64_t ld, co
   a.chunk = std::max(chunk_tokens(T), kMinChunk);
   a.nb = (T + a.chunk - 1) / a.chunk;
   a.err = reinterpret_cast<int32_t*>(base);
-  a.part_p = reinterpret_cast<float*>(base + o.p);
-  a.part_c = reinterpret_cast<int32_t*>(base + o.c);
+  a.part = reinterpret_cast<float2*>(base + o.part);
+  a.Ep = padded(E);
+  a.width = S < kManySeqs ? kGroup : a.Ep;
   a.part_zn = reinterpret_cast<float2*>(base + o.zn);
-  a.seq_lz = reinterpret_cast<float2*>(base + o.seq);
+  a.seq_l = reinterpret_cast<double*>(base + o.seq_l);
+  a.seq_z = reinterpret_cast<float*>(base + o.seq_z);
   a.alpha = alpha;
   a.z_coef = z_coef;
   a.loss = loss;
   a.counts = counts;
   a.probs = probs;
   a.tokens = tokens;
-  if (a.nb > 0) {
-    const size_t lds = (size_t)(kLossWaves + 1) * E * 4;
-    if (pick<RunLoss>(a, fours(logits, ld, E, dtype), dtype == DAMOE_BF16, score == DAMOE_SCORE_SIGMOID, dim3(a.nb),
-                      lds, stream) != hipSuccess)
-      return DAMOE_ERR_HIP;
+  // One block does it all for up to kOneTokens tokens of a few sequences.
+  const bool one = T <= kOneTokens && S <= kOneSeqs;
+  if (one) a.chunk = std::max(T, 1), a.nb = 1;
+  const size_t lds = (size_t)((one ? kOneThreads : kLossThreads) / kWave / 2 + 1) * E * 4;
+  const dim3 grid(std::max(a.nb, 1));
+  const hipError_t e = by_columns(E, fours(logits, ld, E, dtype), [&](auto v, auto nc) {
+    return by_kind(dtype, score, [&](auto bf, auto sig) {
+      constexpr int V = decltype(v)::value, NC = decltype(nc)::value;
+      constexpr bool BF = decltype(bf)::value, SIG = decltype(sig)::value;
+      if (one) hipLaunchKernelGGL((k_router_loss<V, NC, BF, SIG, true>), grid, dim3(kOneThreads), lds, stream, a);
+      else hipLaunchKernelGGL((k_router_loss<V, NC, BF, SIG, false>), grid, dim3(kLossThreads), lds, stream, a);
+      return hipGetLastError();
+    });
+  });
+  if (e != hipSuccess) return DAMOE_ERR_HIP;
+  if (!one && S == 1 && (size_t)a.nb * a.Ep <= kAlonePartials) {
+    hipLaunchKernelGGL(k_router_loss_alone, dim3(1), dim3(kAloneThreads), 0, stream, a);
+  } else if (!one) {
+    const dim3 blocks((unsigned)S * (a.Ep / a.width));
+    if (S < kFewSeqs) hipLaunchKernelGGL(k_router_loss_seq<1024>, blocks, dim3(1024), 0, stream, a);
+    else hipLaunchKernelGGL(k_router_loss_seq<256>, blocks, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(k_router_loss_total, dim3(1), dim3(kAloneThreads), 0, stream, a);
   }
-  hipLaunchKernelGGL(k_router_loss_seq, dim3(S), dim3(kSeqThreads), 0, stream, a);
-  if (S > 1) hipLaunchKernelGGL(k_router_loss_total, dim3(1), dim3(256), 0, stream, a);
   return hipGetLastError() == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
 }
 
@@ -717,10 +898,17 @@ damoe_status damoe_router_loss_grad(const void* logits, int32_t dtype, int64_t l
   a.run = std::max(1, std::min(16, (T + 4095) / 4096));
   const int waves = (T + a.run - 1) / a.run;
   const bool four = fours(logits, ld, E, dtype) && fours(dlogits, ldd, E, dtype);
-  return pick<RunGrad>(a, four, dtype == DAMOE_BF16, score == DAMOE_SCORE_SIGMOID,
-                       dim3((waves + kLossWaves - 1) / kLossWaves), (size_t)kLossWaves * E * 4, stream) == hipSuccess
-             ? DAMOE_OK
-             : DAMOE_ERR_HIP;
+  const hipError_t e = by_columns(E, four, [&](auto v, auto nc) {
+    return by_kind(dtype, score, [&](auto bf, auto sig) {
+      constexpr int V = decltype(v)::value, NC = decltype(nc)::value;
+      constexpr bool BF = decltype(bf)::value, SIG = decltype(sig)::value;
+      const size_t lds = topk_w ? (size_t)kGradWaves * Grad<V, NC, BF, SIG>::kRows * E * 4 : 0;
+      hipLaunchKernelGGL((k_router_loss_grad<V, NC, BF, SIG>), dim3((waves + kGradWaves - 1) / kGradWaves),
+                         dim3(kGradThreads), lds, stream, a);
+      return hipGetLastError();
+    });
+  });
+  return e == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
 }
 
 }  // extern "C"

@@ -44,7 +44,7 @@ class Case:
         self.tokens = torch.full((self.S + 2,), -7, dtype=torch.int32, device="cuda")
         self.loss = torch.full((3,), 7.0, device="cuda")
         self.ws = torch.full((damoe.router_loss_workspace_size(T, E, self.S),), 0xFF, dtype=torch.uint8, device="cuda")
-        self.ws[:4] = 0
+        self.ws[:4] = 0  # the error word
 
     def forward(self, score, alpha, zc, stream=None):
         damoe.router_loss(self.logits, self.d_ids, self.T, self.E, self.k, self.loss, self.counts, self.tokens, self.ws,
