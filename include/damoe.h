@@ -42,6 +42,8 @@
  *     are masked slots (expert parallelism), dropped without an error.
  *   - All calls are thread-safe as long as concurrent calls use distinct
  *     workspaces.
+ *   - A call runs on the current device, whose memory its pointers name and to
+ *     which its stream belongs.
  */
 #ifndef DAMOE_H
 #define DAMOE_H
@@ -534,7 +536,8 @@ damoe_status damoe_mxfp4_pack(const uint8_t* codes, const uint8_t* scales, int64
  *   x    bf16 or fp32 (xdtype) [T][ldx], quantised in the call as damoe_mxfp4_quantise does
  *   w    DAMOE_LAYOUT_TILE32 of the N x K weights, K a multiple of 32
  *   add  NULL, or [T][ld_add] of y's type; it may be y itself (ld_add = ldy)
- *   y    bf16 or fp32 (ydtype) [T][ldy], ldy >= N; columns past N are left as they were
+ *   y    bf16 or fp32 (ydtype) [T][ldy], ldy >= N; columns past N are left as they were.  Overlaps neither x, w
+ *        nor ws
  *   ws   16-byte aligned, at least damoe_mxfp4_linear_workspace_size(T, N, K) bytes; nothing is kept in it.
  * Products and scales are exact, sums fp32 in a fixed order; a NaN block makes its row (x) or column (w) of y
  * NaN.  T = 0 is a no-op; T <= DAMOE_MAX_T, N and K <= 2^20, and T ceil(K / 256) 136, N ceil(K / 256) 136

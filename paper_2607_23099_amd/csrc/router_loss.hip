@@ -164,6 +164,8 @@ struct Row {
     for (int i = 0; i < V * NC; ++i) v[i] = x;
   }
 
+  // With the nontemporal hint, which is as fast or faster at every size (fp32, 256 experts: 16384 tokens 9.1 against
+  // 11.7 us, 131072 52 against 59; three batches of 65536 x 384 in turn 46 against 53).
   __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int E, int lane) const {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -177,14 +179,17 @@ struct Row {
           uint32_t q[V / 2];
 #pragma unroll
           for (int i = 0; i < V / 2; ++i) q[i] = (uint32_t)bf16_of(v[V * c + 2 * i]) | (uint32_t)bf16_of(v[V * c + 2 * i + 1]) << 16;
-          if constexpr (V == 4) *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
-          else *reinterpret_cast<uint32_t*>(p) = q[0];
+          typedef uint32_t Words __attribute__((ext_vector_type(V / 2)));
+          Words d;
+#pragma unroll
+          for (int i = 0; i < V / 2; ++i) d[i] = q[i];
+          __builtin_nontemporal_store(d, reinterpret_cast<Words*>(p));
         }
       } else {
         Vec q;
 #pragma unroll
         for (int i = 0; i < V; ++i) q[i] = v[V * c + i];
-        *reinterpret_cast<Vec*>(static_cast<float*>(base) + row * ld + e) = q;
+        __builtin_nontemporal_store(q, reinterpret_cast<Vec*>(static_cast<float*>(base) + row * ld + e));
       }
     }
   }
@@ -218,6 +223,27 @@ __device__ __forceinline__ float2 sigmoids(float l, float ex, float m) {
 __device__ __forceinline__ int offset_at(const int32_t* off, int32_t s, int32_t T) {
   const int o = off ? off[s] : (s == 0 ? 0 : T);
   return min(max(o, 0), T);
+}
+
+// The first sequence from s on that ends behind token t, S if there is none; the same in every lane.  64 ends at a time,
+// then, past a long run of empty sequences or from a start far ahead, 64 equal steps of what is left.  The result lies in
+// [s, S] whatever the offsets hold.
+__device__ __forceinline__ int seq_behind(const int32_t* off, int s, int S, int T, int t, int lane) {
+  if (!off) return s == 0 && t < T ? 0 : S;
+  int lo = s, hi = S;  // the result lies in [lo, hi]
+  for (bool first = true;; first = false) {
+    const uint64_t behind = __ballot(lo + lane >= hi || offset_at(off, lo + lane + 1, T) > t);
+    if (behind || hi - lo <= kWave) return __builtin_amdgcn_readfirstlane(behind ? min(lo + (int)__builtin_ctzll(behind), hi) : hi);
+    if (first) {
+      lo += kWave;
+    }
+    while (hi - lo > kWave) {
+      const int step = (hi - lo + kWave - 1) / kWave, i = lo + (lane + 1) * step - 1;
+      const int n = __popcll(__ballot(i < hi && offset_at(off, i + 1, T) <= t));  // steps that end at or before t
+      lo = min(lo + n * step, hi);
+      hi = min(lo + step, hi);
+    }
+  }
 }
 
 // ---------------------------------------------------------------- forward
@@ -396,7 +422,6 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kLossThreads) k_router_los
   __shared__ float z_red[kWaves];
   __shared__ int32_t n_red[kWaves];
   __shared__ double l_red[kWaves];
-  __shared__ int32_t first;
   double l_sum = 0.0, z_sum = 0.0;  // ONE, thread 0: over the sequences so far
   int seqs = 0, n_sum = 0;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -405,21 +430,17 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kLossThreads) k_router_los
   const int t0 = blockIdx.x * a.chunk, t1 = min(t0 + a.chunk, a.T);
   const float kNegInf = -__builtin_huge_valf();
 
-  // The first sequence that may reach past t0: the number of ends at or before it.
-  if (tid == 0) first = 0;
   for (int e = tid; e < E; e += kThreads) hist[e] = 0;
   __syncthreads();
-  if (!ONE && a.off) {
-    int n = 0;
-    for (int s = tid; s < a.S; s += kThreads) n += offset_at(a.off, s + 1, a.T) <= t0;
-    if (n) atomicAdd(&first, n);
-    __syncthreads();
-  }
-  for (int s = first; s < a.S; ++s) {
+  // The sequences with tokens in the block (ONE: all, as those without have their zeros to write).
+  int t_next = t0;
+  for (int s = ONE ? 0 : seq_behind(a.off, 0, a.S, a.T, t0, lane); s < a.S;
+       s = ONE ? s + 1 : seq_behind(a.off, s + 1, a.S, a.T, t_next, lane)) {
     const int b0 = offset_at(a.off, s, a.T), b1 = offset_at(a.off, s + 1, a.T);
     if (!ONE && b0 >= t1) break;
     const int lo = max(t0, b0), hi = min(t1, b1);
-    if (!ONE && lo >= hi) continue;
+    if (!ONE && lo >= hi) continue;  // decreasing offsets
+    t_next = hi;
     float acc[V * NC];
 #pragma unroll
     for (int i = 0; i < V * NC; ++i) acc[i] = 0.f;
@@ -486,7 +507,7 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kLossThreads) k_router_los
       }
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
-        const bool live = ((ok >> u) & 1) && m[u] != kNegInf;
+        const bool live = ((ok >> u) & 1) && sum[u] != 0.f;  // 0: nothing but -inf (a NaN makes it NaN)
         n += (ok >> u) & 1;
         const float lse = lse_of(m[u], sum[u]), f = 1.f / inv[u];
         if (!live) continue;
@@ -642,7 +663,7 @@ struct Grad {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool live = m[u] != kNegInf;
+      const bool live = sum[u] != 0.f;
       const float ip = live ? 1.f / ps[u] : 0.f, dot = fp[u] * ip, b = bal * ip;
       const float zt = live && a.z_coef != 0.f ? zc * lse_of(m[u], sum[u]) / sum[u] : 0.f;
 #pragma unroll
@@ -686,23 +707,14 @@ __global__ void __launch_bounds__(kGradThreads) k_router_loss_grad(GradArgs a) {
   const float g = a.dloss ? *a.dloss : 1.f;
   const float n_seq = (float)a.tokens[a.S], n_tok = (float)a.tokens[a.S + 1];
   d.zc = a.z_coef != 0.f ? g * a.z_coef * 2.f / n_tok : 0.f;
-  d.bal = 0.f;
-
-  int s = 0;  // the number of ends at or before t0
-  if (a.off) {
-    for (int i = lane; i < a.S; i += kWave) s += offset_at(a.off, i + 1, a.T) <= t0;
-    for (int q = 1; q < kWave; q <<= 1) s += __shfl_xor(s, q);
-    s = __builtin_amdgcn_readfirstlane(s);
-  }
-  int begin = 0, end = -1, cur = -1;  // of sequence s once `cur` names it
+  int s = -1, begin = 0, end = 0;  // the sequence that t is in or ahead of
   for (int t = t0; t < t1;) {
-    while (s < a.S && (cur != s || t >= end)) {
-      if (cur == s) ++s;
-      if (s >= a.S) break;
-      cur = s;
-      begin = offset_at(a.off, s, a.T);
-      end = offset_at(a.off, s + 1, a.T);
-      if (t < end) {
+    if (s < a.S && (s < 0 || t >= end)) {
+      s = seq_behind(a.off, s + 1, a.S, a.T, t, lane);
+      begin = end = a.T;
+      if (s < a.S) {
+        begin = offset_at(a.off, s, a.T);
+        end = offset_at(a.off, s + 1, a.T);
         const float n = (float)a.tokens[s];
         d.bal = a.alpha != 0.f ? g * a.alpha / (n_seq * n) : 0.f;
         const float fs = (float)E / ((float)a.k * n);

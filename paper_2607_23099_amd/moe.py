@@ -115,6 +115,9 @@ class MxLinear:
         T = x.shape[0]
         if T > self.T_max:
             raise ValueError("more rows than T_max")
+        for t, cols in ((x, self.K), (y, self.N), (add, self.N)):
+            if t is not None and tuple(t.shape) != (T, cols):
+                raise ValueError(f"a matrix of {tuple(t.shape)} where {(T, cols)} is wanted")
         if y is None:
             y = torch.empty((T, self.N), dtype=x.dtype if add is None else add.dtype, device=x.device)
         damoe.mxfp4_linear(x, T, self.K, self.tiles, self.N, y, self.ws, add=add, stream=stream)

@@ -107,6 +107,18 @@ def test_sequences(offsets, T, score):
         Case(torch, T, 48, 4, offsets=offsets, mask=m).check(torch, score)
 
 
+def test_many_sequences():
+    """Thousands of sequences of 0 to 5 tokens, and a long run of empty ones."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(2)
+    n = rng.integers(0, 6, 5000)
+    n[1000:4500] = 0
+    off = np.concatenate([[0], np.cumsum(n)]).tolist()
+    for score in (0, 1):
+        Case(torch, off[-1] + 9, 40, 3, offsets=off, mask=(rng.random(off[-1] + 9) < 0.9).astype(np.uint8)).check(torch, score)
+    Case(torch, 50, 16, 2, offsets=[0] + [30] * 5000 + [45]).check(torch, 0)
+
+
 def test_many_tokens_ragged():
     torch = torch_cuda()
     rng = np.random.default_rng(1)
@@ -162,6 +174,21 @@ def test_nan_in_a_valid_row():
     c.backward(out, 0, 1.0, 0.1)
     rows = torch.isnan(out).any(dim=1).cpu().numpy()
     assert rows[2] and rows.sum() == 1
+
+
+def test_nan_among_switched_off_experts():
+    torch = torch_cuda()
+
+    def edit(l, ids):
+        l[7] = -np.inf
+        l[7, 3] = np.nan
+
+    c = Case(torch, 200, 32, 2, edit=edit)
+    c.forward(0, 1.0, 0.1)
+    assert torch.isnan(c.loss).all() and torch.isnan(c.probs).all()
+    out = torch.zeros((200, 32), device="cuda")
+    c.backward(out, 0, 1.0, 0.1, gates=False)
+    assert torch.isnan(out[7]).all() and torch.isfinite(out[:7]).all() and torch.isfinite(out[8:]).all()
 
 
 def test_nothing_valid():
