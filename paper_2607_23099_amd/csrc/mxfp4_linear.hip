@@ -598,7 +598,7 @@ Path path_of(int32_t T, int32_t N, int32_t K, int cus) {
 template <int NB>
 hipError_t launch_gemm(const LinearArgs& a, int cus, hipStream_t stream) {
   const int64_t tiles = a.tiles_r * tiles_of(a.T, 32 * NB);
-  const dim3 grid((unsigned)std::min<int64_t>(tiles_of(tiles, 8), std::max(1, cus * (NB <= 2 ? 2 : 1) / 8)) * 8);  // 1 or 2 a CU
+  const dim3 grid((unsigned)std::min<int64_t>(tiles_of(tiles, 8), std::max(1, cus * (NB == 1 ? 2 : 1) / 8)) * 8);  // as many as fit the CUs
   const auto go = [&](void (*f)(LinearArgs)) { hipLaunchKernelGGL(f, grid, dim3(256), gemm_lds<NB>(), stream, a); };
   if (a.y_bf) go(a.add ? k_mxfp4_gemm<NB, true, true> : k_mxfp4_gemm<NB, true, false>);
   else go(a.add ? k_mxfp4_gemm<NB, false, true> : k_mxfp4_gemm<NB, false, false>);

@@ -102,37 +102,33 @@ __global__ void __launch_bounds__(kThreads) k_quantise_tile(QuantArgs a, int64_t
 
 // ---------------------------------------------------------------- dequantise
 
-// Eight values of the codes c and the scale byte s: an e2m1 value times 2^(s - 127) from integer and exact
-// fp32 steps (twice the value, an integer up to 12, then a power of two that may be below the normal range).
+// Eight values of the codes c and the scale byte s.  The conversions multiply by the scale exactly, results below the
+// normal range included, and give infinity past the type's range and NaN for a NaN scale (checked on the device for
+// every code under every scale).
 template <bool BF, bool V, bool NT>
 __device__ __forceinline__ void store8(void* base, int64_t i, uint32_t c, uint32_t s) {
-  float v[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t m = (c >> (4 * j)) & 7u;
-    const float twice = (float)(m < 4u ? m : m < 6u ? 2u * m - 4u : 4u * m - 16u);
-    float f = s == 255u ? __uint_as_float(0x7FC00000u) : ldexpf(twice, (int)s - 128);
-    v[j] = (c >> (4 * j + 3)) & 1u ? -f : f;
-  }
+  const float f = e8m0_to_f32(s);
   if constexpr (BF) {
     uint16_t* p = static_cast<uint16_t*>(base) + i;
-    uint32_t q[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
+    const uint4 q = fp4x8_to_bf16x8(c, f);
     if constexpr (V) {
-      store16<NT>(p, make_uint4(q[0], q[1], q[2], q[3]));
+      store16<NT>(p, q);
     } else {
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+      for (int j = 0; j < 8; ++j) p[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
     }
   } else {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, f, 3)};
     float* p = static_cast<float*>(base) + i;
     if constexpr (V) {
-      store16<NT>(p, __builtin_bit_cast(uint4, make_float4(v[0], v[1], v[2], v[3])));
-      store16<NT>(p + 4, __builtin_bit_cast(uint4, make_float4(v[4], v[5], v[6], v[7])));
+      store16<NT>(p, __builtin_bit_cast(uint4, make_float4(v[0][0], v[0][1], v[1][0], v[1][1])));
+      store16<NT>(p + 4, __builtin_bit_cast(uint4, make_float4(v[2][0], v[2][1], v[3][0], v[3][1])));
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] = v[j];
+      for (int j = 0; j < 8; ++j) p[j] = v[j / 2][j & 1];
     }
   }
 }
