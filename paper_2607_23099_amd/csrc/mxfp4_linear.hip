@@ -677,8 +677,10 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
   const bool fused = T <= 4 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * (int64_t)xs % 16 == 0;
   if (!fused && launch_quantise_tiles(x, x_bf, T, K, ldx, xt, stream) != hipSuccess) return DAMOE_ERR_HIP;
   int cus = 0;
-  const damoe_status st = device_cus(&cus);
-  if (st != DAMOE_OK) return st;
+  if (T > 32) {
+    const damoe_status st = device_cus(&cus);
+    if (st != DAMOE_OK) return st;
+  }
   const RowsArgs r{a, x, ldx, K};
   const auto rows = [&](void (*f)(RowsArgs), int mr, int nt) {
     hipLaunchKernelGGL(f, dim3((unsigned)tiles_of(N, 16 * mr), (unsigned)tiles_of(T, 16 * nt)), dim3(kRowsThreads), 0, stream, r);

@@ -25,26 +25,44 @@ struct QuantArgs {
 
 // ---------------------------------------------------------------- quantise
 
-// Row-major.  Rows without a gap (ld = cols) are one long row.
-template <bool BF, bool V, bool NT>
-__global__ void __launch_bounds__(kThreads) k_quantise_rows(QuantArgs a, int64_t n8) {
-  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const int64_t first = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
-    Eight<BF> e[kUnroll];
+// Row-major, eights in order.  Where an eight of the matrix lies in x: rows without a gap (GAP false) are one long row;
+// else a block row of the grid has `chunk` rows' eights, few enough that 32 bits number them.
+template <bool GAP>
+struct Eights {
+  int64_t first, n;  // the block row's eights: codes from number `first` on, n of them
+  int64_t row0, ld;
+  uint32_t n8;
+
+  __device__ __forceinline__ Eights(const QuantArgs& a, int64_t n_all, int64_t chunk) : ld(a.ld), n8((uint32_t)(a.cols / 8)) {
+    row0 = GAP ? (int64_t)blockIdx.y * chunk : 0;
+    first = GAP ? row0 * n8 : 0;
+    n = GAP ? min(chunk, a.rows - row0) * n8 : n_all;
+  }
+  __device__ __forceinline__ int64_t at(int64_t i) const {
+    if constexpr (!GAP) return i * 8;
+    const uint32_t r = (uint32_t)i / n8;
+    return (row0 + r) * ld + (int64_t)((uint32_t)i - r * n8) * 8;
+  }
+};
+
+template <bool BF, bool V, bool NT, bool GAP>
+__global__ void __launch_bounds__(kThreads) k_quantise_rows(QuantArgs a, int64_t n_all, int64_t chunk) {
+  const Eights<GAP> w(a, n_all, chunk);
+  const int64_t i0 = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
+  Eight<BF> e[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int64_t i = first + u * kThreads;
-      if (i < n8) e[u].template load<V, NT>(a.x, row * a.ld + i * 8);
-      else e[u].zero();
-    }
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t i = i0 + u * kThreads;
+    if (i < w.n) e[u].template load<V, NT>(a.x, w.at(i));
+    else e[u].zero();
+  }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int64_t i = first + u * kThreads;
-      const uint32_t s = e[u].scale_byte();
-      if (i >= n8) continue;
-      reinterpret_cast<uint32_t*>(a.codes)[row * n8 + i] = e[u].codes(s);
-      if ((i & 3) == 0) a.scales[(row * n8 + i) >> 2] = (uint8_t)s;
-    }
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t i = i0 + u * kThreads;
+    const uint32_t s = e[u].scale_byte();
+    if (i >= w.n) continue;
+    reinterpret_cast<uint32_t*>(a.codes)[w.first + i] = e[u].codes(s);
+    if ((i & 3) == 0) a.scales[(w.first + i) >> 2] = (uint8_t)s;
   }
 }
 
@@ -133,17 +151,15 @@ __device__ __forceinline__ void store8(void* base, int64_t i, uint32_t c, uint32
   }
 }
 
-template <bool BF, bool V, bool NT>
-__global__ void __launch_bounds__(kThreads) k_dequantise_rows(QuantArgs a, int64_t n8) {
-  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const int64_t first = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
+template <bool BF, bool V, bool NT, bool GAP>
+__global__ void __launch_bounds__(kThreads) k_dequantise_rows(QuantArgs a, int64_t n_all, int64_t chunk) {
+  const Eights<GAP> w(a, n_all, chunk);
+  const int64_t i0 = (int64_t)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int64_t i = first + u * kThreads;
-      if (i >= n8) continue;
-      store8<BF, V, NT>(a.x, row * a.ld + i * 8, reinterpret_cast<const uint32_t*>(a.codes)[row * n8 + i],
-                    a.scales[(row * n8 + i) >> 2]);
-    }
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t i = i0 + u * kThreads;
+    if (i >= w.n) continue;
+    store8<BF, V, NT>(a.x, w.at(i), reinterpret_cast<const uint32_t*>(a.codes)[w.first + i], a.scales[(w.first + i) >> 2]);
   }
 }
 
@@ -212,6 +228,8 @@ __global__ void __launch_bounds__(kThreads) k_pack_tile(const uint8_t* __restric
 // ---------------------------------------------------------------- launches
 
 constexpr int64_t kMaxGrid = 1 << 20;
+// Eights of a block row of the row-major kernels with gaps.
+constexpr int64_t kChunkEights = (int64_t)1 << 30;
 
 // Bytes of x from which its accesses carry the nontemporal hint: what no longer fits the 256 MB cache in front of HBM is
 // not worth keeping there.  bf16, quantise / dequantise over and over: 470 MiB 95 / 91 us with the hint, 111 / 126
@@ -242,14 +260,16 @@ hipError_t launch(QuantArgs a, bool bf, int32_t layout, hipStream_t stream) {
   return by_type(bf, vec, nt, [&](auto b, auto v, auto n) {
     constexpr bool B = decltype(b)::value, V = decltype(v)::value, NT = decltype(n)::value;
     if (layout == DAMOE_LAYOUT_ROWMAJOR) {
-      int64_t n8 = a.cols / 8;
-      if (a.ld == a.cols) {  // one long row
-        n8 *= a.rows;
-        a.rows = 1;
-      }
-      const dim3 grid((unsigned)tiles_of(n8, kThreads * kUnroll), (unsigned)std::min<int64_t>(a.rows, 65535));
-      if constexpr (QUANT) hipLaunchKernelGGL((k_quantise_rows<B, V, NT>), grid, dim3(kThreads), 0, stream, a, n8);
-      else hipLaunchKernelGGL((k_dequantise_rows<B, V, NT>), grid, dim3(kThreads), 0, stream, a, n8);
+      const int64_t n8 = a.cols / 8, n_all = a.rows * n8;
+      const auto go = [&](auto gap) {
+        constexpr bool GAP = decltype(gap)::value;
+        const int64_t chunk = GAP ? std::min(a.rows, kChunkEights / n8) : a.rows;
+        const dim3 grid((unsigned)tiles_of(chunk * n8, kThreads * kUnroll), (unsigned)((a.rows + chunk - 1) / chunk));
+        if constexpr (QUANT) hipLaunchKernelGGL((k_quantise_rows<B, V, NT, GAP>), grid, dim3(kThreads), 0, stream, a, n_all, chunk);
+        else hipLaunchKernelGGL((k_dequantise_rows<B, V, NT, GAP>), grid, dim3(kThreads), 0, stream, a, n_all, chunk);
+      };
+      if (a.ld == a.cols) go(std::false_type{});
+      else go(std::true_type{});
     } else if (layout == DAMOE_LAYOUT_FRAG16) {
       const int32_t per_row = a.cols / 128;
       const int64_t quads = a.rows / 16 * per_row;

@@ -183,6 +183,7 @@ class Path:
         self.ws = torch.zeros(damoe.workspace_size(dl.layer, T_max), dtype=torch.uint8, device=device)
         self.candidates = 0  # variants the last dispatch could choose (0 = all)
         self.logits = torch.zeros((max(T_max, 1), sh.E), dtype=torch.float32, device=device)
+        self.loss_S = 0  # set by prepare_loss
         self.router_ws = torch.zeros(damoe.router_workspace_size(sh.E, sh.H, T_max), dtype=torch.uint8,
                                      device=device)
 
@@ -217,10 +218,15 @@ class Path:
         self.loss_ws = torch.zeros(damoe.router_loss_workspace_size(self.T_max, sh.E, S), dtype=torch.uint8, device=dev)
         self.dlogits = torch.zeros_like(self.logits)
 
+    def _need_loss(self):
+        if not self.loss_S:
+            raise RuntimeError("prepare_loss() makes the buffers of router_loss")
+
     def router_loss(self, T: int, alpha: float, z_coef: float = 0.0, *, mask=None, seq_offsets=None,
                     score: int = damoe.SCORE_SOFTMAX, stream=None):
         """Balance and z-loss of the router's last call on T tokens (its logits and ids) into loss; counts, mean
         probabilities and token counts into loss_counts, loss_probs and loss_tokens."""
+        self._need_loss()
         sh = self.dl.shape
         damoe.router_loss(self.logits, self.ids, T, sh.E, sh.k, self.loss, self.loss_counts, self.loss_tokens,
                           self.loss_ws, mask=mask, seq_offsets=seq_offsets, S=self.loss_S, score=score, alpha=alpha,
@@ -230,6 +236,7 @@ class Path:
                          seq_offsets=None, score: int = damoe.SCORE_SOFTMAX, stream=None):
         """Gradient of router_loss (same arguments) and of the gates (dw [T][k]), with respect to the logits, into
         the first T rows of dlogits."""
+        self._need_loss()
         sh = self.dl.shape
         damoe.router_loss_grad(self.logits, self.ids, T, sh.E, sh.k, self.loss_counts, self.loss_tokens, self.dlogits,
                                mask=mask, seq_offsets=seq_offsets, S=self.loss_S, score=score, alpha=alpha,

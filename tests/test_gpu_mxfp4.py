@@ -80,6 +80,22 @@ def test_strided_and_unaligned_rows(layout, dtype):
         np.testing.assert_array_equal(got, want)
 
 
+def test_many_short_strided_rows():
+    torch = torch_cuda()
+    rows, cols, ld = 70001, 32, 40
+    v = np.random.default_rng(8).standard_normal((rows, cols))
+    x = torch.full((rows, ld), float("nan"), dtype=torch.bfloat16, device="cuda")
+    x[:, :cols] = _bf16(torch, v).cuda()
+    code, scale = fp4_ref.quantise(x[:, :cols].double().cpu().numpy())
+    codes, scales = _quantise(torch, x, rows, cols, "rowmajor")
+    assert np.array_equal(codes.cpu().numpy(), fp4_ref.rowmajor(code, scale)[0].reshape(-1))
+    assert np.array_equal(scales.cpu().numpy(), scale.reshape(-1))
+    out = torch.full((rows, ld), 7.0, dtype=torch.float32, device="cuda")
+    damoe.mxfp4_dequantise(codes, scales, rows, cols, out, damoe.LAYOUT_ROWMAJOR)
+    np.testing.assert_array_equal(out[:, :cols].double().cpu().numpy(), fp4_ref.values(code, scale))
+    assert (out[:, cols:] == 7.0).all()
+
+
 @pytest.mark.parametrize("layout", sorted(LAYOUTS))
 def test_every_code_under_every_scale(layout):
     torch = torch_cuda()
