@@ -672,9 +672,12 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
   const bool vec = N % 8 == 0 && rows_ok(y, ldy) && (!add || rows_ok(add, ld_add));
   const LinearArgs a{w, xt, add, y, ld_add, ldy, T, N, (int32_t)tiles_of(K, kTileCols), ydtype == DAMOE_BF16, vec,
                      (int32_t)tiles_of(N, 256)};
-  // Up to four tokens are quantised where they are used, which saves a launch (4096 x 7168, T = 1: 5.8 us against 3.6 and
-  // 2.9; from T = 8 on the workgroups' reads of x cost more, 7.5 us).
-  const bool fused = T <= 4 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * (int64_t)xs % 16 == 0;
+  // Up to four tokens are quantised where they are used, which saves a launch of 2.9 us, unless the workgroups of a CU
+  // (16 rows each, 256 CUs) go over so many tiles that doing it in each of them costs more.  T = 1, quantised in the kernel
+  // / before it: 4096 x 7168 5.8 / 3.6 + 2.9 us, 7168 x 2048 4.6 / 3.2 + 2.9, 8192 x 8192 11.5 / 6.9 + 2.9; from T = 8 on the
+  // reads of x cost more (4096 x 7168 7.5).
+  const bool fused = T <= 4 && tiles_of(K, kTileCols) * tiles_of(N, 16 * 256) <= 36 &&
+                     reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * (int64_t)xs % 16 == 0;
   if (!fused && launch_quantise_tiles(x, x_bf, T, K, ldx, xt, stream) != hipSuccess) return DAMOE_ERR_HIP;
   int cus = 0;
   if (T > 32) {
