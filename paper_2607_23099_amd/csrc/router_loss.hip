@@ -258,7 +258,7 @@ __device__ __forceinline__ void write_loss(const LossArgs& a, double balance, do
   a.tokens[a.S + 1] = n_tok;
 }
 
-constexpr int kAloneThreads = 1024;
+constexpr int kAloneThreads = 1024, kTotalThreads = 256;
 
 template <int THREADS>
 struct SeqSmem {
@@ -373,16 +373,16 @@ __global__ void __launch_bounds__(kAloneThreads) k_router_loss_alone(LossArgs a)
 }
 
 // The sum over sequences, by one block in a fixed order (what a sequence without tokens left is 0).
-__global__ void __launch_bounds__(kAloneThreads) k_router_loss_total(LossArgs a) {
-  __shared__ double red[(kAloneThreads / kWave)][4];
+__global__ void __launch_bounds__(kTotalThreads) k_router_loss_total(LossArgs a) {
+  __shared__ double red[kTotalThreads / kWave][4];
   const int tid = threadIdx.x;
   const int64_t m = (int64_t)a.S * (a.Ep / a.width);
   double l = 0, z = 0;
   int seqs = 0, n = 0;
 #pragma unroll 4
-  for (int64_t i = tid; i < m; i += kAloneThreads) l += a.seq_l[i];
+  for (int64_t i = tid; i < m; i += kTotalThreads) l += a.seq_l[i];
 #pragma unroll 4
-  for (int s = tid; s < a.S; s += kAloneThreads) {
+  for (int s = tid; s < a.S; s += kTotalThreads) {
     const int ns = a.tokens[s];
     z += a.seq_z[s];
     seqs += ns > 0;
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(kAloneThreads) k_router_loss_total(LossArgs a)
   }
   __syncthreads();
   if (tid == 0) {
-    for (int i = 1; i < (kAloneThreads / kWave); ++i) {
+    for (int i = 1; i < kTotalThreads / kWave; ++i) {
       l += red[i][0];
       z += red[i][1];
       seqs += (int)red[i][2];
@@ -886,7 +886,7 @@ damoe_status damoe_router_loss(const void* logits, int32_t dtype, int64_t ld, co
     const dim3 blocks((unsigned)S * (a.Ep / a.width));
     if (S < kFewSeqs) hipLaunchKernelGGL(k_router_loss_seq<1024>, blocks, dim3(1024), 0, stream, a);
     else hipLaunchKernelGGL(k_router_loss_seq<256>, blocks, dim3(256), 0, stream, a);
-    hipLaunchKernelGGL(k_router_loss_total, dim3(1), dim3(kAloneThreads), 0, stream, a);
+    hipLaunchKernelGGL(k_router_loss_total, dim3(1), dim3(kTotalThreads), 0, stream, a);
   }
   return hipGetLastError() == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
 }

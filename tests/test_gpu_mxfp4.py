@@ -142,6 +142,27 @@ def test_pack_equals_quantise(rows, cols):
     assert torch.equal(tiles[:-64], want) and (tiles[-64:] == 0xA5).all()
 
 
+@pytest.mark.parametrize("layout", sorted(LAYOUTS))
+def test_more_values_than_32_bits(layout):
+    """The last rows of a matrix of 4.3e9 values, past every 32-bit offset."""
+    torch = torch_cuda()
+    cols, rows = 32768, (1 << 17) + 48
+    log(f"quantise {rows}x{cols} {layout}")
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    x[:-48] = torch.randn((1, cols), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    x[-48:] = torch.randn((48, cols), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    codes, scales = _quantise(torch, x, rows, cols, layout)
+    want, want_s = _quantise(torch, x[-48:].contiguous(), 48, cols, layout)
+    per = {"rowmajor": 48 * cols // 2, "frag16": 48 * cols // 32 * 17, "tile32": 2 * cols // 256 * 4352}[layout]
+    # rows - 48 is a multiple of 32: the last rows' tiles are whole ones and as in the small matrix.
+    assert torch.equal(codes[-per:], want[-per:])
+    assert scales is None or torch.equal(scales[-48 * cols // 32:], want_s)
+    out = torch.empty((48, cols), dtype=torch.bfloat16, device="cuda")
+    damoe.mxfp4_dequantise(want, want_s, 48, cols, out, LAYOUTS[layout])
+    damoe.mxfp4_dequantise(codes, scales, rows, cols, x, LAYOUTS[layout])
+    assert torch.equal(x[-48:], out)
+
+
 # ---------------------------------------------------------------- the product
 
 class Linear:
@@ -284,6 +305,45 @@ def test_linear_streams_and_graphs(T):
         torch.cuda.synchronize()
         for i in (0, 1):
             assert torch.equal(outs[i], eager[i] if rep != 1 else other[i]), (rep, i)
+
+
+def test_linear_results_past_32_bits():
+    torch = torch_cuda()
+    T, N, K = 1 << 20, 1100, 32
+    log(f"linear T={T} N={N} K={K}")
+    p = Linear(torch, 64, N, K, seed=6)
+    x = p.x.repeat(T // 64, 1)
+    ws = torch.empty(damoe.mxfp4_linear_workspace_size(T, N, K), dtype=torch.uint8, device="cuda")
+    small = torch.empty((64, N), dtype=torch.float32, device="cuda")
+    damoe.mxfp4_linear(p.x, 64, K, p.tiles, N, small, p.ws)
+    _check(small, p.y, p.tol("f32", p.y))
+    for n in (N, 1097):  # rows of y at 16 bytes, and any
+        y = torch.full((T, n), float("nan"), dtype=torch.float32, device="cuda")
+        damoe.mxfp4_linear(x, T, K, p.tiles, n, y, ws)
+        assert torch.isfinite(y[::4097]).all()
+        # K = 32 is one product of one block: no sums whose order the kernels could differ in.
+        for t0 in (0, T // 2, T - 64):
+            _check(y[t0: t0 + 64], p.y[:, :n], p.tol("f32", p.y)[:, :n])
+        del y
+
+
+def test_two_products_at_once():
+    """Two streams, a workspace each, many calls in flight."""
+    torch = torch_cuda()
+    ps = [Linear(torch, T, 512, 1024, seed=7) for T in (8, 200)]
+    want, ys = [], []
+    for p in ps:
+        y = torch.zeros((p.T, 512), dtype=torch.float32, device="cuda")
+        damoe.mxfp4_linear(p.x, p.T, 1024, p.tiles, 512, y, p.ws)
+        want.append(y)
+        ys.append([torch.zeros_like(y) for _ in range(20)])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i in range(20):
+        for p, s, y in zip(ps, streams, ys):
+            damoe.mxfp4_linear(p.x, p.T, 1024, p.tiles, 512, y[i], p.ws, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, w) for w, all_y in zip(want, ys) for y in all_y)
 
 
 def test_quantised_layer_with_a_shared_expert():

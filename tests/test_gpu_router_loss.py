@@ -241,6 +241,52 @@ def test_strides_and_alignment(E, ld, shift, dtype):
     assert (np.abs(want.double().cpu().numpy() - d) <= tol).all()
 
 
+def test_largest_batch():
+    """2^20 tokens of 1024 experts: rows past every 32-bit offset, and every output of the forward call but probs."""
+    torch = torch_cuda()
+    T, E, k = 1 << 20, 1024, 16
+    base = Case(torch, 64, E, k, seed=3)
+    rep = T // 64
+    logits = base.logits[: 64 * E].view(64, E).repeat(rep, 1)
+    ids, w, dw = base.d_ids.repeat(rep, 1), base.d_w.repeat(rep, 1), base.d_dw.repeat(rep, 1)
+    ws = torch.zeros(damoe.router_loss_workspace_size(T, E), dtype=torch.uint8, device="cuda")
+    counts, tokens = torch.zeros((1, E), dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    loss = torch.zeros(3, device="cuda")
+    damoe.router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, alpha=1.0, z_coef=1.0)
+    want, c, _, _ = ref.loss(base.l, base.ids, k, None, None, 0, 1.0, 1.0)
+    assert np.array_equal(counts.cpu().numpy(), c * rep) and tokens.tolist() == [T, 1, T]
+    # 2048 tokens a block, 256 a wave, and 512 blocks: up to 300 roundings more than REL counts.
+    np.testing.assert_allclose(loss.double().cpu().numpy(), want, rtol=REL + 300 * 2.0 ** -24)
+    damoe.router_loss_grad(logits, ids, T, E, k, counts, tokens, logits, alpha=1.0, z_coef=1.0, w=w, dw=dw)  # in place
+    d, mag = ref.grad(base.l, base.ids, k, None, None, 0, 0.0, 0.0, c, 1.0, base.w.astype(np.float64), base.dw.astype(np.float64))
+    # The loss's share of a row's gradient is 1 / T of what it is for 64 tokens.
+    d2, mag2 = ref.grad(base.l, base.ids, k, None, None, 0, 1.0, 1.0, c, 1.0 / rep)
+    for t0 in (0, T // 2, T - 64):
+        got = logits[t0: t0 + 64].double().cpu().numpy()
+        assert (np.abs(got - d - d2) <= 2 * REL * (mag + mag2) + 1e-30).all(), t0
+
+
+def test_two_batches_at_once():
+    torch = torch_cuda()
+    cs = [Case(torch, T, 64, 4, offsets=off, seed=9) for T, off in ((50, None), (3000, [0, 700, 701, 2990]))]
+    want, outs = [], []
+    for c in cs:
+        c.forward(1, 0.5, 0.1)
+        o = torch.zeros((c.T, 64), device="cuda")
+        c.backward(o, 1, 0.5, 0.1)
+        want.append((c.loss.clone(), c.counts.clone(), c.probs.clone(), o))
+        outs.append(torch.zeros_like(o))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        for c, s, o in zip(cs, streams, outs):
+            c.forward(1, 0.5, 0.1, s)
+            c.backward(o, 1, 0.5, 0.1, stream=s)
+    torch.cuda.synchronize()
+    for c, w, o in zip(cs, want, outs):
+        assert all(torch.equal(a, b) for a, b in zip(w, (c.loss, c.counts, c.probs, o)))
+
+
 def test_gates_alone_and_loss_alone():
     torch = torch_cuda()
     c = Case(torch, 60, 48, 5)
