@@ -569,27 +569,35 @@ __global__ void __launch_bounds__(kRowsThreads, NT > 2 ? 2 : 4) k_mxfp4_rows(Row
   }
 }
 
-// Which kernel a call of more than 32 tokens takes: the one with the least estimated time, in us, fitted to measured
-// calls (N x K of 4096 x 7168, 7168 x 2048, 8192 x 8192 and 512 x 1024, T = 33 to 8192; at most 15% over the fastest).
+// Which kernel a call of more than 32 tokens takes: the one with the least estimated time, in us, fitted to
+// 180 measured calls (random T = 33 to 8192, N = 100 to 8192, K = 256 to 8192; in 110 others the pick took at most 1.12
+// of the fastest kernel's time, 1.005 in the geometric mean).
 // k_mxfp4_rows<2, 4> runs rounds of a workgroup a CU, each a start and its waves' tiles.  k_mxfp4_gemm<NB> runs rounds
-// of tiles, each a fixed part and stages, which take the longer the more CUs share L2 (and, at NB = 8, the card's power).
+// of tiles, each a fixed part, stages, which take the longer the more CUs share L2 (and, at NB = 8, the card's power),
+// and, for rows of y that take no 16-byte stores, an element a lane at a time.
 // Fastest at T = 64 / 300 / 1000 / 4096: 4096 x 7168 rows 6.1, gemm<1> 15.0 (rows 16.3), <2> 20.8 (<4> 27.3),
 // <8> 57.3 (<4> 62.2); 7168 x 2048 rows 4.3, <2> 7.6 (<1> 8.6), <4> 12.6 (<8> 18.1), <4> 38.8 (<8> 40.0).
 enum Path { kRows, kGemm1, kGemm2, kGemm4, kGemm8 };
 
-Path path_of(int32_t T, int32_t N, int32_t K, int cus) {
+Path path_of(int32_t T, int32_t N, int32_t K, bool vec, int cus) {
   const double nk = (double)tiles_of(K, kTileCols);
+  const double stages = std::max(4.0, nk + (double)(tiles_of(K, kTileCols) & 1));
   const auto rounds = [&](int64_t n) { return (double)((n + cus - 1) / cus); };
-  double best = 2.8 + rounds(tiles_of(N, 32) * tiles_of(T, 64)) * (1.0 + 0.13 * nk);
+  const int64_t groups = tiles_of(N, 32) * tiles_of(T, 64);
+  double best = 1.6 + 0.5 * (rounds(groups) + std::max(1.0, (double)groups / cus)) * (1.6 + 0.18 * nk);
   Path path = kRows;
   constexpr struct {
     Path path;
     int nb;
-    double stage, shared, fixed;
-  } gemms[] = {{kGemm1, 1, 0.33, 0.14, 0.3}, {kGemm2, 2, 0.40, 0.24, 0.6}, {kGemm4, 4, 0.60, 0.45, 1.2}, {kGemm8, 8, 1.10, 0.85, 4.0}};
+    double stage, shared, fixed, any;
+  } gemms[] = {{kGemm1, 1, 0.27, 0.11, -0.1, 1.1},
+               {kGemm2, 2, 0.37, 0.27, 0.4, 2.4},
+               {kGemm4, 4, 0.56, 0.48, 0.9, 5.4},
+               {kGemm8, 8, 0.92, 1.20, 2.2, 11.8}};
   for (const auto& g : gemms) {
     const int64_t tiles = tiles_of(N, 256) * tiles_of(T, 32 * g.nb);
-    const double t = 2.7 + rounds(tiles) * (nk * (g.stage + g.shared * std::min(1.0, (double)tiles / cus)) + g.fixed);
+    const double load = std::min(1.0, (double)tiles / cus);
+    const double t = 3.3 + rounds(tiles) * (stages * (g.stage + g.shared * load) + g.fixed + (vec ? 0.0 : g.any));
     if (t < best) best = t, path = g.path;
   }
   return path;
@@ -693,7 +701,7 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
   if (fused) e = rows(x_bf ? k_mxfp4_rows<1, 1, 1> : k_mxfp4_rows<1, 1, 2>, 1, 1);
   else if (T <= 16) e = rows(k_mxfp4_rows<1, 1, 0>, 1, 1);
   else if (T <= 32) e = rows(k_mxfp4_rows<1, 2, 0>, 1, 2);
-  else switch (path_of(T, N, K, cus)) {
+  else switch (path_of(T, N, K, vec, cus)) {
     case kRows: e = rows(k_mxfp4_rows<2, 4, 0>, 2, 4); break;
     case kGemm1: e = launch_gemm<1>(a, cus, stream); break;
     case kGemm2: e = launch_gemm<2>(a, cus, stream); break;
