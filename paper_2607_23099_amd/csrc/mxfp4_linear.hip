@@ -22,7 +22,7 @@ struct LinearArgs {
   int32_t T, N, nk;   // nk: tiles along K
   int32_t y_bf;
   int32_t vec;        // rows of y and add start at 16 bytes, N is whole eights, 32 rows lie within 2^31 bytes
-  int32_t tiles_r;    // 256-row tiles of W (the kernel of many tokens)
+  int32_t tiles_r;    // row tiles of W (the kernel of many tokens)
 };
 
 // Both operands' fp4 codes fill the lower half of the instruction's 8-register operands.
@@ -39,8 +39,11 @@ __device__ __forceinline__ float load_elem(const void* p, int64_t i, bool bf) {
 
 // ---------------------------------------------------------------- many tokens
 //
-// A workgroup of four waves takes tiles of 256 rows of W x 32 NB tokens, one after the other: wave w has 64 rows (two
-// blocks) and all the tokens, 2 NB accumulator blocks.  A stage, 256 columns, is 8 NB MFMAs a wave.
+// A workgroup of four waves takes tiles of 128 MA rows of W x 32 NB tokens, one after the other: a wave has 32 MA rows
+// (MA blocks) and all the tokens, MA NB accumulator blocks.  A stage, 256 columns, is 4 MA NB MFMAs a wave.  A CU loads
+// about 100 GB/s, which bounds the small tiles, so they are as near to square as whole waves of rows allow, and
+// two workgroups of 128 rows share a CU, one's start and end beside the other's stages (256 x 32 / 128 x 64, 256 x 64 /
+// 128 x 128: 15.0 / 12.5 and 17.7 / 16.7 us at T = 300, 4096 x 7168; 49.9 / 43.4 and 45.0 / 37.1 at 4096, 7168 x 2048).
 //   W      straight into registers, every fragment read by one wave: the registers of a step are loaded for a
 //          stage D ahead as soon as its MFMAs have read them.
 //   tokens through LDS, which the four waves share: global -> registers (D stages ahead) -> LDS (the wave's quarter
@@ -50,8 +53,6 @@ __device__ __forceinline__ float load_elem(const void* p, int64_t i, bool bf) {
 // that of the stage before last.  Reads, writes and loads stand one at a time behind pairs of MFMAs.  The stages of a
 // workgroup's tiles run on without a gap: the last stages of a tile load the first of the next one, whose results
 // leave while those loads are in flight.
-constexpr int kRowBlocks = 8;  // 32-row blocks of W a workgroup
-
 constexpr int wait_lgkm(int n) { return 15 | (7 << 4) | (n << 8) | (3 << 14); }
 
 typedef __attribute__((address_space(3))) uint8_t lds_t;
@@ -97,21 +98,21 @@ struct TileWalk {
   }
 };
 
-// A wave's 32 tokens x 64 columns of results on their way through LDS, so that stores fill whole 128-byte lines (a lane
+// A wave's 32 tokens x 32 MA columns of results on their way through LDS, so that stores fill whole 128-byte lines (a lane
 // of the accumulators holds four columns of one token): rows of bf16 where nothing is added, of fp32 otherwise, 16
 // bytes apart.  LDS carries out a wave's accesses in order, so only the compiler is held back between them.
-constexpr uint32_t kOutBytes = 32 * (64 * 4 + 16);
+constexpr uint32_t out_bytes(int MA) { return 32 * (32 * MA * 4 + 16); }
 
 __device__ __forceinline__ void wave_lds_fence() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_wave_barrier();
 }
 
-template <bool YBF, bool ADD>
+template <int MA, bool YBF, bool ADD>
 struct Out {
   static constexpr bool kHalf = YBF && !ADD;             // bf16 rows in LDS
-  static constexpr uint32_t kElem = kHalf ? 2 : 4, kPitch = 64 * kElem + 16;
-  static constexpr int kLanes = 64 * kElem / 16;         // lanes of a row, 16 bytes each
+  static constexpr uint32_t kElem = kHalf ? 2 : 4, kCols = 32 * MA, kPitch = kCols * kElem + 16;
+  static constexpr int kLanes = kCols * kElem / 16;         // lanes of a row, 16 bytes each
   static constexpr int kRowsAt = 64 / kLanes, kTrips = 32 / kRowsAt;
   uint4 v[kTrips];
 
@@ -137,7 +138,7 @@ struct Out {
     for (int i = 0; i < kTrips; ++i) v[i] = lds_read16(p + i * kRowsAt * kPitch);
   }
 
-  // The rows of tokens t0 .. t0 + 31, columns n0 .. + 63, where a.vec: whole lanes in or out of range, rows within 32-bit
+  // The rows of tokens t0 .. t0 + 31, columns n0 .. + kCols - 1, where a.vec: whole lanes in or out of range, rows within 32-bit
   // offsets of the block's first.
   __device__ __forceinline__ void store(const LinearArgs& a, int64_t t0, int n0, int lane) const {
     constexpr uint32_t es = YBF ? 2 : 4;
@@ -180,11 +181,11 @@ struct Out {
 
   // The same for any strides and alignment, from LDS: a column a lane, a row at a time.
   static __device__ __forceinline__ void store_any(const LinearArgs& a, const lds_t* out, int64_t t0, int n0, int lane) {
-    const int n = n0 + lane;
+    const int c = lane % (int)kCols, n = n0 + c;
     const int rows = n < a.N ? (int)min((int64_t)32, a.T - t0) : 0;
 #pragma unroll 1
-    for (int r = 0; r < rows; ++r) {
-      const lds_t* p = out + (uint32_t)r * kPitch + (uint32_t)lane * kElem;
+    for (int r = lane / (int)kCols; r < rows; r += 64 / (int)kCols) {
+      const lds_t* p = out + (uint32_t)r * kPitch + (uint32_t)c * kElem;
       if constexpr (kHalf) {
         static_cast<uint16_t*>(a.y)[(t0 + r) * a.ldy + n] = *reinterpret_cast<const __attribute__((address_space(3))) uint16_t*>(p);
       } else {
@@ -197,8 +198,8 @@ struct Out {
   }
 };
 
-template <int NB, bool YBF, bool ADD>
-__global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
+template <int MA, int NB, bool YBF, bool ADD>
+__global__ void __launch_bounds__(256, 3 - MA) k_mxfp4_gemm(LinearArgs a) {
   constexpr uint32_t kStage = NB * kTileBytes;
   // Token operands read ahead of their MFMAs; reads of the next stage's start behind the barrier, in step 2.
   constexpr int kAhead = NB >= 2 ? 4 : 2;
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t gemm_smem[];
   lds_t* const lds = (lds_t*)gemm_smem;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  lds_t* const mine = lds + 3 * kStage + w * kOutBytes;
+  lds_t* const mine = lds + 3 * kStage + w * out_bytes(MA);
   const int nrb = (a.N + 31) / 32, ntb = (a.T + 31) / 32, nk = a.nk;
   // Stages of a tile: whole turns of the D sets of registers, and two at least (a stage's loads reach into the next
   // tile at most); stages past nk multiply zero weights.
@@ -224,12 +225,12 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
   // Where a tile's weights and tokens start: row and token blocks past the last repeat it, and their results are not
   // stored.
   struct Base {
-    uint32_t w[2], x[NB], xs[kScaleMoves];
+    uint32_t w[MA], x[NB], xs[kScaleMoves];
   };
   auto base_of = [&](int rt_, int tt_) __attribute__((always_inline)) {
     Base b;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) b.w[m] = (uint32_t)min(rt_ * kRowBlocks + 2 * w + m, nrb - 1) * row_bytes;
+    for (int m = 0; m < MA; ++m) b.w[m] = (uint32_t)min((rt_ * 4 + w) * MA + m, nrb - 1) * row_bytes;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       const int piece = w * NB + i;
@@ -243,9 +244,9 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
   Base cur = base_of(rt, tt), nxt = cur;
 
   // Sets by the stage modulo D, of scales from LDS modulo 2.
-  uint4 wq[D][2][4], st[D][NB], xr[kAhead];
-  uint32_t wsc[D][2], sts[D][kScaleMoves], xs[2][NB];
-  floatx16 acc[2][NB];
+  uint4 wq[D][MA][4], st[D][NB], xr[kAhead];
+  uint32_t wsc[D][MA], sts[D][kScaleMoves], xs[2][NB];
+  floatx16 acc[MA][NB];
 
   // Loads of stage t of the current tile, or t - ns of the next.
   auto at = [&](int t) __attribute__((always_inline)) { return (uint32_t)min(t < ns ? t : t - ns, nk - 1) * kTileBytes; };
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
     for (int n = 0; n < NB; ++n) {
       const int i = J * NB + n, f = i + kAhead;
 #pragma unroll
-      for (int m = 0; m < 2; ++m) acc[m][n] = mfma_fp4<J>(wq[P][m][J], wsc[P][m], xr[i % kAhead], xs[P % 2][n], acc[m][n]);
+      for (int m = 0; m < MA; ++m) acc[m][n] = mfma_fp4<J>(wq[P][m][J], wsc[P][m], xr[i % kAhead], xs[P % 2][n], acc[m][n]);
       xr[i % kAhead] = f < 4 * NB ? read_x(buf, f) : read_x(next, f - 4 * NB);
       if constexpr (J == 0) {
         write_x(next, Q, n);
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
         read_xs(next, 1 - P % 2, n);
       }
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
+      for (int m = 0; m < MA; ++m) {
         if (n != (m + 1) * NB / 3) continue;
         if constexpr (J == 0) {
           load_w(t - 1 + D, R, 3, m);
@@ -334,7 +335,7 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
 #pragma unroll
     for (int i = 0; i < kScaleMoves; ++i) load_xs(p, p, i);
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
+    for (int m = 0; m < MA; ++m) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) load_w(p, p, j, m);
       load_ws(p, p, m);
@@ -360,7 +361,7 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
     const bool more = walk.tile(++turn, rt1, tt1);
     nxt = base_of(rt1, tt1);  // with no next tile, the loads repeat this one's
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < MA; ++m)
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -376,14 +377,14 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
     }
     // Results, a token block at a time through LDS of the wave's own; a block's stores go out while the next one's
     // values come back from LDS.
-    using O = Out<YBF, ADD>;
+    using O = Out<MA, YBF, ADD>;
     O o[2];
-    const int nb = min(NB, ntb - tt * NB), n0 = (rt * kRowBlocks + 2 * w) * 32;
+    const int nb = min(NB, ntb - tt * NB), n0 = (rt * 4 + w) * 32 * MA;
 #pragma unroll
     for (int n = 0; n <= NB; ++n) {
       if (n < NB && n < nb) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m) O::put(mine, acc[m][n], m, lane);
+        for (int m = 0; m < MA; ++m) O::put(mine, acc[m][n], m, lane);
         wave_lds_fence();
         if (a.vec) o[n & 1].get(mine, lane);
         else O::store_any(a, mine, (int64_t)(tt * NB + n) * 32, n0, lane);
@@ -397,9 +398,9 @@ __global__ void __launch_bounds__(256, 1) k_mxfp4_gemm(LinearArgs a) {
   }
 }
 
-template <int NB>
+template <int MA, int NB>
 constexpr size_t gemm_lds() {
-  return 3 * NB * kTileBytes + 4 * kOutBytes;
+  return 3 * NB * kTileBytes + 4 * out_bytes(MA);
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -570,55 +571,61 @@ __global__ void __launch_bounds__(kRowsThreads, NT > 2 ? 2 : 4) k_mxfp4_rows(Row
 }
 
 // Which kernel a call of more than 32 tokens takes: the one with the least estimated time, in us, fitted to
-// 180 measured calls (random T = 33 to 8192, N = 100 to 8192, K = 256 to 8192; in 110 others the pick took at most 1.12
-// of the fastest kernel's time, 1.005 in the geometric mean).
-// k_mxfp4_rows<2, 4> runs rounds of a workgroup a CU, each a start and its waves' tiles.  k_mxfp4_gemm<NB> runs rounds
-// of tiles, each a fixed part, stages, which take the longer the more CUs share L2 (and, at NB = 8, the card's power),
-// and, for rows of y that take no 16-byte stores, an element a lane at a time.
-// Fastest at T = 64 / 300 / 1000 / 4096: 4096 x 7168 rows 6.1, gemm<1> 15.0 (rows 16.3), <2> 20.8 (<4> 27.3),
-// <8> 57.3 (<4> 62.2); 7168 x 2048 rows 4.3, <2> 7.6 (<1> 8.6), <4> 12.6 (<8> 18.1), <4> 38.8 (<8> 40.0).
-enum Path { kRows, kGemm1, kGemm2, kGemm4, kGemm8 };
+// 220 measured calls (random T = 33 to 8192, N = 100 to 8192, K = 256 to 8192; in 220 others the pick took at most
+// 1.17 of the fastest kernel's time, 1.005 in the geometric mean).
+// k_mxfp4_rows<2, 4> runs rounds of a workgroup a CU, each a start and its waves' tiles, and its XCDs take each tile from
+// behind their L2s (`moved`, bytes).  k_mxfp4_gemm<MA, NB> runs rounds of tiles, each a fixed part, stages, which take the
+// longer the more CUs share the caches and the card's power, and, for rows of y that take no 16-byte stores, an element
+// a lane at a time.  A last round that is not full costs half of a full one more where the CUs hold two workgroups.
+// Fastest at T = 64 / 300 / 1000 / 4096: 4096 x 7168 rows 6.2, gemm<1, 2> 12.5 (rows 16.6), <1, 4> 20.6 (<1, 2> 21.4),
+// <2, 8> 57.1 (<2, 4> 61.3); 7168 x 2048 rows 4.5, <1, 4> 7.9 (<1, 2> 8.0), <1, 4> 12.2 (<2, 4> 12.5), <1, 4> 37.1
+// (<2, 8> 40.2).
+enum Path { kRows, kGemm12, kGemm14, kGemm24, kGemm28 };
 
 Path path_of(int32_t T, int32_t N, int32_t K, bool vec, int cus) {
   const double nk = (double)tiles_of(K, kTileCols);
   const double stages = std::max(4.0, nk + (double)(tiles_of(K, kTileCols) & 1));
   const auto rounds = [&](int64_t n) { return (double)((n + cus - 1) / cus); };
-  const int64_t groups = tiles_of(N, 32) * tiles_of(T, 64);
-  double best = 1.6 + 0.5 * (rounds(groups) + std::max(1.0, (double)groups / cus)) * (1.6 + 0.18 * nk);
+  const auto part_rounds = [&](int64_t n) { return 0.5 * (rounds(n) + std::max(1.0, (double)n / cus)); };
+  const int64_t nb = tiles_of(N, 32), tb = tiles_of(T, 32);
+  const double moved = (double)(tb * std::min<int64_t>(8, nb) + nb * std::min<int64_t>(8, (tb + 1) / 2)) * nk * kTileBytes;
+  double best = 0.9 + part_rounds(nb * ((tb + 1) / 2)) * (2.1 + 0.082 * nk) + 0.068e-6 * moved;
   Path path = kRows;
   constexpr struct {
     Path path;
-    int nb;
+    int ma, nb;
     double stage, shared, fixed, any;
-  } gemms[] = {{kGemm1, 1, 0.27, 0.11, -0.1, 1.1},
-               {kGemm2, 2, 0.37, 0.27, 0.4, 2.4},
-               {kGemm4, 4, 0.56, 0.48, 0.9, 5.4},
-               {kGemm8, 8, 0.92, 1.20, 2.2, 11.8}};
+  } gemms[] = {{kGemm12, 1, 2, 0.27, 0.13, -0.15, 1.1},
+               {kGemm14, 1, 4, 0.40, 0.22, 0.3, 2.25},
+               {kGemm24, 2, 4, 0.52, 0.57, 1.25, 4.4},
+               {kGemm28, 2, 8, 0.94, 0.85, 3.8, 10.0}};
   for (const auto& g : gemms) {
-    const int64_t tiles = tiles_of(N, 256) * tiles_of(T, 32 * g.nb);
-    const double load = std::min(1.0, (double)tiles / cus);
-    const double t = 3.3 + rounds(tiles) * (stages * (g.stage + g.shared * load) + g.fixed + (vec ? 0.0 : g.any));
+    const int64_t tiles = tiles_of(N, 128 * g.ma) * tiles_of(T, 32 * g.nb);
+    const double stage = g.stage + g.shared * std::min(1.0, (double)tiles / cus);
+    const double t = 3.6 + (g.ma == 1 ? part_rounds(tiles) : rounds(tiles)) * (stages * stage + g.fixed + (vec ? 0.0 : g.any));
     if (t < best) best = t, path = g.path;
   }
   return path;
 }
 
-template <int NB>
-hipError_t launch_gemm(const LinearArgs& a, int cus, hipStream_t stream) {
+// As many workgroups as the CUs hold: two a CU of the 128-row tiles (at most 256 registers), one of the others.
+template <int MA, int NB>
+hipError_t launch_gemm(LinearArgs a, int cus, hipStream_t stream) {
+  a.tiles_r = (int32_t)tiles_of(a.N, 128 * MA);
   const int64_t tiles = a.tiles_r * tiles_of(a.T, 32 * NB);
-  const dim3 grid((unsigned)std::min<int64_t>(tiles_of(tiles, 8), std::max(1, cus * (NB == 1 ? 2 : 1) / 8)) * 8);  // as many as fit the CUs
-  const auto go = [&](void (*f)(LinearArgs)) { hipLaunchKernelGGL(f, grid, dim3(256), gemm_lds<NB>(), stream, a); };
-  if (a.y_bf) go(a.add ? k_mxfp4_gemm<NB, true, true> : k_mxfp4_gemm<NB, true, false>);
-  else go(a.add ? k_mxfp4_gemm<NB, false, true> : k_mxfp4_gemm<NB, false, false>);
+  const dim3 grid((unsigned)std::min<int64_t>(tiles_of(tiles, 8), std::max(1, cus * (3 - MA) / 8)) * 8);
+  const auto go = [&](void (*f)(LinearArgs)) { hipLaunchKernelGGL(f, grid, dim3(256), (gemm_lds<MA, NB>()), stream, a); };
+  if (a.y_bf) go(a.add ? k_mxfp4_gemm<MA, NB, true, true> : k_mxfp4_gemm<MA, NB, true, false>);
+  else go(a.add ? k_mxfp4_gemm<MA, NB, false, true> : k_mxfp4_gemm<MA, NB, false, false>);
   return hipGetLastError();
 }
 
-template <int NB>
+template <int MA, int NB>
 hipError_t gemm_limits() {
-  for (auto f : {k_mxfp4_gemm<NB, false, false>, k_mxfp4_gemm<NB, false, true>, k_mxfp4_gemm<NB, true, false>,
-                 k_mxfp4_gemm<NB, true, true>}) {
+  for (auto f : {k_mxfp4_gemm<MA, NB, false, false>, k_mxfp4_gemm<MA, NB, false, true>, k_mxfp4_gemm<MA, NB, true, false>,
+                 k_mxfp4_gemm<MA, NB, true, true>}) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                             gemm_lds<NB>());
+                                             gemm_lds<MA, NB>());
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -641,7 +648,7 @@ size_t x_tiles_bytes(int32_t T, int32_t K) {
 }  // namespace
 
 hipError_t mxfp4_set_lds_limits() {
-  for (const hipError_t e : {gemm_limits<1>(), gemm_limits<2>(), gemm_limits<4>(), gemm_limits<8>()})
+  for (const hipError_t e : {gemm_limits<1, 2>(), gemm_limits<1, 4>(), gemm_limits<2, 4>(), gemm_limits<2, 8>()})
     if (e != hipSuccess) return e;
   return hipSuccess;
 }
@@ -678,8 +685,7 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)ys % 16 == 0 && ld * (int64_t)ys * 32 < (int64_t)1 << 31;
   };
   const bool vec = N % 8 == 0 && rows_ok(y, ldy) && (!add || rows_ok(add, ld_add));
-  const LinearArgs a{w, xt, add, y, ld_add, ldy, T, N, (int32_t)tiles_of(K, kTileCols), ydtype == DAMOE_BF16, vec,
-                     (int32_t)tiles_of(N, 256)};
+  const LinearArgs a{w, xt, add, y, ld_add, ldy, T, N, (int32_t)tiles_of(K, kTileCols), ydtype == DAMOE_BF16, vec, 0};
   // Up to four tokens are quantised where they are used, which saves a launch of 2.9 us, unless the workgroups of a CU
   // (16 rows each, 256 CUs) go over so many tiles that doing it in each of them costs more.  T = 1, quantised in the kernel
   // / before it: 4096 x 7168 5.8 / 3.6 + 2.9 us, 7168 x 2048 4.6 / 3.2 + 2.9, 8192 x 8192 11.5 / 6.9 + 2.9; from T = 8 on the
@@ -703,10 +709,10 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
   else if (T <= 32) e = rows(k_mxfp4_rows<1, 2, 0>, 1, 2);
   else switch (path_of(T, N, K, vec, cus)) {
     case kRows: e = rows(k_mxfp4_rows<2, 4, 0>, 2, 4); break;
-    case kGemm1: e = launch_gemm<1>(a, cus, stream); break;
-    case kGemm2: e = launch_gemm<2>(a, cus, stream); break;
-    case kGemm4: e = launch_gemm<4>(a, cus, stream); break;
-    default: e = launch_gemm<8>(a, cus, stream);
+    case kGemm12: e = launch_gemm<1, 2>(a, cus, stream); break;
+    case kGemm14: e = launch_gemm<1, 4>(a, cus, stream); break;
+    case kGemm24: e = launch_gemm<2, 4>(a, cus, stream); break;
+    default: e = launch_gemm<2, 8>(a, cus, stream);
   }
   return e == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
 }
