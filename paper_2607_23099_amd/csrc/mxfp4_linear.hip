@@ -4,6 +4,8 @@
 // the call.  v_mfma_scale_f32_32x32x64_f8f6f4 multiplies a step of 64 columns: lane 32 h + r holds row r,
 // columns 32 h .. + 31, one scale block, and takes its scale from a byte of a register.  Products and scales
 // are exact (a product is a multiple of 2^-2 times the scales, at most 36), the sums are fp32.
+#include <type_traits>
+
 #include "common.h"
 #include "device.h"
 #include "mxfp4.h"
@@ -179,20 +181,49 @@ struct Out {
     }
   }
 
-  // The same for any strides and alignment, from LDS: a column a lane, a row at a time.
-  static __device__ __forceinline__ void store_any(const LinearArgs& a, const lds_t* out, int64_t t0, int n0, int lane) {
-    const int c = lane % (int)kCols, n = n0 + c;
-    const int rows = n < a.N ? (int)min((int64_t)32, a.T - t0) : 0;
-#pragma unroll 1
-    for (int r = lane / (int)kCols; r < rows; r += 64 / (int)kCols) {
-      const lds_t* p = out + (uint32_t)r * kPitch + (uint32_t)c * kElem;
+  // The same for any strides, alignment and N: global accesses of whole lanes at an element's alignment, and the
+  // elements of a row's last lane one by one (60 calls with odd N take 0.76 to 0.88 of the time that a column a lane, an
+  // element at a time, took; where `store` applies it is 3% faster).
+  __device__ __forceinline__ void store_any(const LinearArgs& a, int64_t t0, int n0, int lane) const {
+    constexpr int kN = 16 / (int)kElem;
+    typedef std::conditional_t<YBF, uint16_t, float> T;
+    typedef uint32_t Words __attribute__((ext_vector_type(kN * sizeof(T) / 4), aligned(sizeof(T))));
+    const int n = n0 + kN * (lane % kLanes), r0 = lane / kLanes;
+    const int rows = (int)min((int64_t)32, a.T - t0) - r0, cols = min(kN, a.N - n);
+    T* y = static_cast<T*>(a.y) + (t0 + r0) * a.ldy + n;
+    const T* add = static_cast<const T*>(a.add) + (t0 + r0) * a.ld_add + n;
+#pragma unroll
+    for (int i = 0; i < kTrips; ++i, y += kRowsAt * a.ldy, add += kRowsAt * a.ld_add) {
+      if (i * kRowsAt >= rows || cols <= 0) continue;
+      union {
+        Words w;
+        T e[kN];
+      } o, d;
+      const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+      if constexpr (ADD) {
+        if (cols == kN) d.w = *reinterpret_cast<const Words*>(add);
+        else
+          for (int e = 0; e < kN; ++e) d.e[e] = e < cols ? add[e] : T(0);
+      }
       if constexpr (kHalf) {
-        static_cast<uint16_t*>(a.y)[(t0 + r) * a.ldy + n] = *reinterpret_cast<const __attribute__((address_space(3))) uint16_t*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o.w[e] = u[e];
       } else {
-        float f = __uint_as_float(lds_read4(p));
-        if constexpr (ADD) f += load_elem(a.add, (t0 + r) * a.ld_add + n, YBF);
-        if constexpr (YBF) static_cast<uint16_t*>(a.y)[(t0 + r) * a.ldy + n] = __builtin_bit_cast(uint16_t, (__bf16)f);
-        else static_cast<float*>(a.y)[(t0 + r) * a.ldy + n] = f;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+          float f = __uint_as_float(u[e]);
+          if constexpr (ADD && YBF) f += bf16_to_f32(d.e[e]);
+          if constexpr (ADD && !YBF) f += d.e[e];
+          if constexpr (YBF) o.e[e] = __builtin_bit_cast(uint16_t, (__bf16)f);
+          else o.e[e] = f;
+        }
+      }
+      if (cols == kN) {
+        *reinterpret_cast<Words*>(y) = o.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < kN; ++e)
+          if (e < cols) y[e] = o.e[e];
       }
     }
   }
@@ -386,11 +417,14 @@ __global__ void __launch_bounds__(256, 3 - MA) k_mxfp4_gemm(LinearArgs a) {
 #pragma unroll
         for (int m = 0; m < MA; ++m) O::put(mine, acc[m][n], m, lane);
         wave_lds_fence();
-        if (a.vec) o[n & 1].get(mine, lane);
-        else O::store_any(a, mine, (int64_t)(tt * NB + n) * 32, n0, lane);
+        o[n & 1].get(mine, lane);
         wave_lds_fence();
       }
-      if (a.vec && n > 0 && n <= nb) o[(n - 1) & 1].store(a, (int64_t)(tt * NB + n - 1) * 32, n0, lane);
+      if (n > 0 && n <= nb) {
+        const int64_t t0 = (int64_t)(tt * NB + n - 1) * 32;
+        if (a.vec) o[(n - 1) & 1].store(a, t0, n0, lane);
+        else o[(n - 1) & 1].store_any(a, t0, n0, lane);
+      }
     }
     if (!more) break;
     rt = rt1, tt = tt1;
@@ -572,11 +606,10 @@ __global__ void __launch_bounds__(kRowsThreads, NT > 2 ? 2 : 4) k_mxfp4_rows(Row
 
 // Which kernel a call of more than 32 tokens takes: the one with the least estimated time, in us, fitted to
 // 220 measured calls (random T = 33 to 8192, N = 100 to 8192, K = 256 to 8192; in 220 others the pick took at most
-// 1.17 of the fastest kernel's time, 1.005 in the geometric mean).
+// 1.10 of the fastest kernel's time, 1.002 in the geometric mean).
 // k_mxfp4_rows<2, 4> runs rounds of a workgroup a CU, each a start and its waves' tiles, and its XCDs take each tile from
 // behind their L2s (`moved`, bytes).  k_mxfp4_gemm<MA, NB> runs rounds of tiles, each a fixed part, stages, which take the
-// longer the more CUs share the caches and the card's power, and, for rows of y that take no 16-byte stores, an element
-// a lane at a time.  A last round that is not full costs half of a full one more where the CUs hold two workgroups.
+// longer the more CUs share the caches and the card's power, and, where rows of y or add are unaligned, slower stores.  A last round that is not full costs half of a full one more where the CUs hold two workgroups.
 // Fastest at T = 64 / 300 / 1000 / 4096: 4096 x 7168 rows 6.2, gemm<1, 2> 12.5 (rows 16.6), <1, 4> 20.6 (<1, 2> 21.4),
 // <2, 8> 57.1 (<2, 4> 61.3); 7168 x 2048 rows 4.5, <1, 4> 7.9 (<1, 2> 8.0), <1, 4> 12.2 (<2, 4> 12.5), <1, 4> 37.1
 // (<2, 8> 40.2).
@@ -589,20 +622,20 @@ Path path_of(int32_t T, int32_t N, int32_t K, bool vec, int cus) {
   const auto part_rounds = [&](int64_t n) { return 0.5 * (rounds(n) + std::max(1.0, (double)n / cus)); };
   const int64_t nb = tiles_of(N, 32), tb = tiles_of(T, 32);
   const double moved = (double)(tb * std::min<int64_t>(8, nb) + nb * std::min<int64_t>(8, (tb + 1) / 2)) * nk * kTileBytes;
-  double best = 0.9 + part_rounds(nb * ((tb + 1) / 2)) * (2.1 + 0.082 * nk) + 0.068e-6 * moved;
+  double best = 0.8 + part_rounds(nb * ((tb + 1) / 2)) * (2.2 + 0.085 * nk) + 0.05e-6 * moved;
   Path path = kRows;
   constexpr struct {
     Path path;
     int ma, nb;
     double stage, shared, fixed, any;
-  } gemms[] = {{kGemm12, 1, 2, 0.27, 0.13, -0.15, 1.1},
-               {kGemm14, 1, 4, 0.40, 0.22, 0.3, 2.25},
-               {kGemm24, 2, 4, 0.52, 0.57, 1.25, 4.4},
-               {kGemm28, 2, 8, 0.94, 0.85, 3.8, 10.0}};
+  } gemms[] = {{kGemm12, 1, 2, 0.28, 0.11, 0.3, 0.0},
+               {kGemm14, 1, 4, 0.39, 0.22, 0.6, 0.5},
+               {kGemm24, 2, 4, 0.52, 0.51, 1.8, 1.1},
+               {kGemm28, 2, 8, 0.98, 1.03, 4.0, 2.5}};
   for (const auto& g : gemms) {
     const int64_t tiles = tiles_of(N, 128 * g.ma) * tiles_of(T, 32 * g.nb);
     const double stage = g.stage + g.shared * std::min(1.0, (double)tiles / cus);
-    const double t = 3.6 + (g.ma == 1 ? part_rounds(tiles) : rounds(tiles)) * (stages * stage + g.fixed + (vec ? 0.0 : g.any));
+    const double t = 2.95 + (g.ma == 1 ? part_rounds(tiles) : rounds(tiles)) * (stages * stage + g.fixed + (vec ? 0.0 : g.any));
     if (t < best) best = t, path = g.path;
   }
   return path;
