@@ -287,10 +287,28 @@ def _ld(t, cols: int, ld) -> int:
         return int(ld)
     stride = t.stride()
     if len(stride) != 2:
+        if not t.is_contiguous():
+            raise ValueError("a tensor that is no matrix must be contiguous")
         return cols
     if stride[1] != 1 and t.shape[1] > 1:
         raise ValueError("the elements of a row must lie side by side")
     return max(cols, stride[0]) if t.shape[0] == 1 else stride[0]
+
+
+_INT32, _FLOAT32, _BYTES = set(), set(), set()  # torch types, filled by the first call
+
+
+def _list(name: str, t, types: set, n: int):
+    """Refuses a tensor that is not n elements side by side of one of the types: an int64 list of offsets, or the
+    gradient of a sum, whose elements are all the same one, would be read as something else."""
+    if not _INT32:
+        import torch
+        _BYTES.update((torch.uint8, torch.bool, torch.int8))
+        _FLOAT32.add(torch.float32)
+        _INT32.add(torch.int32)  # last: another thread takes it for all three
+    if t.dtype not in types or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous elements of {'/'.join(str(d) for d in types)} are wanted, "
+                         f"not {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
 
 
 def router_loss_workspace_size(T_max: int, E: int, S: int = 1) -> int:
@@ -300,6 +318,12 @@ def router_loss_workspace_size(T_max: int, E: int, S: int = 1) -> int:
 def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, seq_offsets=None, S=1,
                 score=SCORE_SOFTMAX, alpha=0.0, z_coef=0.0, probs=None, ld=None, stream=None):
     """Balance loss, z-loss, counts and mean probabilities of a routed batch (damoe_router_loss)."""
+    if ids is not None:
+        _list("ids", ids, _INT32, T * k)
+    if mask is not None:
+        _list("mask", mask, _BYTES, T)
+    if seq_offsets is not None:
+        _list("seq_offsets", seq_offsets, _INT32, S + 1)
     _check("damoe_router_loss", lib().damoe_router_loss(
         _p(logits), _dtype(logits), _ld(logits, E, ld), _p(ids), _p(mask), _p(seq_offsets), T, E, k, S, score, alpha,
         z_coef, _p(loss), _p(counts), _p(probs), _p(tokens), _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
@@ -311,6 +335,18 @@ def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None
     """Gradient of the loss and of the gates w with respect to the logits (damoe_router_loss_grad)."""
     if dlogits.dtype != logits.dtype:
         raise ValueError("dlogits has the logits' type")
+    if ids is not None:
+        _list("ids", ids, _INT32, T * k)
+    if w is not None:
+        _list("w", w, _FLOAT32, T * k)
+    if dw is not None:
+        _list("dw", dw, _FLOAT32, T * k)
+    if mask is not None:
+        _list("mask", mask, _BYTES, T)
+    if seq_offsets is not None:
+        _list("seq_offsets", seq_offsets, _INT32, S + 1)
+    if dloss is not None:
+        _list("dloss", dloss, _FLOAT32, 1)
     _check("damoe_router_loss_grad", lib().damoe_router_loss_grad(
         _p(logits), _dtype(logits), _ld(logits, E, ld), _p(ids), _p(w), _p(dw), _p(mask), _p(seq_offsets), _p(counts),
         _p(tokens), T, E, k, S, score, alpha, z_coef, _p(dloss), _p(dlogits), _ld(dlogits, E, ldd), _stream(stream)))

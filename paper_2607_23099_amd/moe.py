@@ -116,8 +116,12 @@ class MxLinear:
         if T > self.T_max:
             raise ValueError("more rows than T_max")
         for t, cols in ((x, self.K), (y, self.N), (add, self.N)):
-            if t is not None and tuple(t.shape) != (T, cols):
+            if t is None:
+                continue
+            if tuple(t.shape) != (T, cols):
                 raise ValueError(f"a matrix of {tuple(t.shape)} where {(T, cols)} is wanted")
+            if t.device != self.tiles.device:
+                raise ValueError(f"a matrix on {t.device}, the weights are on {self.tiles.device}")
         if y is None:
             y = torch.empty((T, self.N), dtype=x.dtype if add is None else add.dtype, device=x.device)
         damoe.mxfp4_linear(x, T, self.K, self.tiles, self.N, y, self.ws, add=add, stream=stream)
@@ -218,15 +222,17 @@ class Path:
         self.loss_ws = torch.zeros(damoe.router_loss_workspace_size(self.T_max, sh.E, S), dtype=torch.uint8, device=dev)
         self.dlogits = torch.zeros_like(self.logits)
 
-    def _need_loss(self):
+    def _need_loss(self, T: int):
         if not self.loss_S:
             raise RuntimeError("prepare_loss() makes the buffers of router_loss")
+        if T > self.T_max:
+            raise ValueError("more tokens than T_max")
 
     def router_loss(self, T: int, alpha: float, z_coef: float = 0.0, *, mask=None, seq_offsets=None,
                     score: int = damoe.SCORE_SOFTMAX, stream=None):
         """Balance and z-loss of the router's last call on T tokens (its logits and ids) into loss; counts, mean
         probabilities and token counts into loss_counts, loss_probs and loss_tokens."""
-        self._need_loss()
+        self._need_loss(T)
         sh = self.dl.shape
         damoe.router_loss(self.logits, self.ids, T, sh.E, sh.k, self.loss, self.loss_counts, self.loss_tokens,
                           self.loss_ws, mask=mask, seq_offsets=seq_offsets, S=self.loss_S, score=score, alpha=alpha,
@@ -236,7 +242,7 @@ class Path:
                          seq_offsets=None, score: int = damoe.SCORE_SOFTMAX, stream=None):
         """Gradient of router_loss (same arguments) and of the gates (dw [T][k]), with respect to the logits, into
         the first T rows of dlogits."""
-        self._need_loss()
+        self._need_loss(T)
         sh = self.dl.shape
         damoe.router_loss_grad(self.logits, self.ids, T, sh.E, sh.k, self.loss_counts, self.loss_tokens, self.dlogits,
                                mask=mask, seq_offsets=seq_offsets, S=self.loss_S, score=score, alpha=alpha,

@@ -133,3 +133,62 @@ def test_tensor_forms_that_the_binding_refuses():
         damoe.mxfp4_linear(a, 8, 64, a, 64, a, a, add=a.to(torch.bfloat16), stream=0)
     with pytest.raises(damoe.DamoeError):  # fp16 is no type of these calls
         damoe.mxfp4_quantise(a.half(), 8, 64, a, a, damoe.LAYOUT_ROWMAJOR, stream=0)
+
+
+def test_lists_that_the_binding_refuses():
+    torch = pytest.importorskip("torch")
+    T, E, k, S = 8, 64, 4, 2
+    a = torch.zeros(T, E)
+    ids = torch.zeros(T, k, dtype=torch.int32)
+    off = torch.zeros(S + 1, dtype=torch.int32)
+    w = torch.zeros(T, k)
+    mask = torch.ones(T, dtype=torch.uint8)
+    good = dict(mask=mask, seq_offsets=off)
+
+    def loss(ids=ids, **kw):
+        damoe.router_loss(a, ids, T, E, k, a, a, a, a[0], S=S, stream=0, **{**good, **kw})
+
+    def grad(ids=ids, **kw):
+        damoe.router_loss_grad(a, ids, T, E, k, a, a, a, S=S, stream=0, **{**good, "w": w, "dw": w, **kw})
+
+    bad = [dict(ids=ids.long()), dict(ids=ids[:-1]), dict(ids=torch.zeros(k, T, dtype=torch.int32).t()), dict(mask=mask.long()),
+           dict(mask=mask[:-1]), dict(mask=torch.ones(2 * T, dtype=torch.uint8)[::2]), dict(seq_offsets=off.long()),
+           dict(seq_offsets=off[:-1])]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            loss(**kw)
+        with pytest.raises(ValueError):
+            grad(**kw)
+    for kw in [dict(dw=torch.zeros(1, 1).expand(T, k)), dict(w=w.double()), dict(dw=w[:-1]), dict(dloss=torch.zeros((), dtype=torch.float64))]:
+        with pytest.raises(ValueError):
+            grad(**kw)
+    with pytest.raises(damoe.DamoeError, match="workspace"):  # the lists are good: the library's own check is next
+        loss()
+    with pytest.raises(damoe.DamoeError, match="invalid argument"):
+        loss(ids=None)
+    damoe.router_loss_grad(a, None, 0, E, k, a, a, a, stream=0)  # no gates, no tokens
+    with pytest.raises(ValueError):
+        damoe.mxfp4_quantise(torch.zeros(4, 8, 64).transpose(0, 1), 32, 64, a, a, damoe.LAYOUT_ROWMAJOR, stream=0)
+
+
+def test_objects_refuse_what_their_buffers_do_not_hold():
+    torch = pytest.importorskip("torch")
+    from paper_2607_23099_amd.moe import MxLinear, Path
+
+    lin = MxLinear.__new__(MxLinear)
+    lin.N, lin.K, lin.T_max = 64, 32, 4
+    lin.tiles = lin.ws = torch.zeros(1, dtype=torch.uint8)
+    x = torch.zeros(4, 32)
+    for args, kw in [((torch.zeros(5, 32),), {}), ((torch.zeros(4, 64),), {}), ((x.to("meta"),), {}), ((x, torch.zeros(4, 63)), {}),
+                     ((x,), dict(add=torch.zeros(1, 64))), ((x,), dict(add=torch.zeros(1, 64).expand(4, 64).to("meta")))]:
+        with pytest.raises(ValueError):
+            lin(*args, stream=0, **kw)
+    path = Path.__new__(Path)
+    path.loss_S, path.T_max = 0, 4
+    for call in (path.router_loss, path.router_loss_grad):
+        with pytest.raises(RuntimeError):
+            call(4, 0.1)
+    path.loss_S = 1
+    for call in (path.router_loss, path.router_loss_grad):
+        with pytest.raises(ValueError):
+            call(5, 0.1)
