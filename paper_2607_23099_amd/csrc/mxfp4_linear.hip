@@ -141,7 +141,9 @@ struct Out {
   }
 
   // The rows of tokens t0 .. t0 + 31, columns n0 .. + kCols - 1, where a.vec: whole lanes in or out of range, rows within 32-bit
-  // offsets of the block's first.
+  // offsets of the block's first.  A store's offset is all in its vector register: behind a 16-byte store with one in a
+  // scalar register the compiler lets the next instruction write the store's data, which reached memory now and then
+  // (an address in place of a sum, fp32 with `add`); behind one without it puts the wait that is needed.
   __device__ __forceinline__ void store(const LinearArgs& a, int64_t t0, int n0, int lane) const {
     constexpr uint32_t es = YBF ? 2 : 4;
     const int n = 16 / (int)kElem * (lane % kLanes), r0 = lane / kLanes;
@@ -151,9 +153,9 @@ struct Out {
 #pragma unroll
     for (int i = 0; i < kTrips; ++i) {
       const bool in = i * kRowsAt < rows;
-      const uint32_t o = in ? yo : kOobOffset, so = (uint32_t)(i * kRowsAt) * ldy;
+      const uint32_t o = in ? yo + (uint32_t)(i * kRowsAt) * ldy : kOobOffset;
       if constexpr (kHalf) {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v[i]), ry, o, so, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v[i]), ry, o, 0, 0);
         continue;
       }
       float f[4] = {__uint_as_float(v[i].x), __uint_as_float(v[i].y), __uint_as_float(v[i].z), __uint_as_float(v[i].w)};
@@ -173,10 +175,10 @@ struct Out {
       }
       if constexpr (YBF) {
         const u32x2 h = {pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
-        __builtin_amdgcn_raw_buffer_store_b64(h, ry, o, so, 0);
+        __builtin_amdgcn_raw_buffer_store_b64(h, ry, o, 0, 0);
       } else {
         const u32x4 h = {__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
-        __builtin_amdgcn_raw_buffer_store_b128(h, ry, o, so, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(h, ry, o, 0, 0);
       }
     }
   }

@@ -331,6 +331,23 @@ def test_linear_results_past_32_bits():
         del y
 
 
+def test_linear_add_gives_the_same_bits_each_time():
+    """Results in fp32 with rows added, many calls: stores whose data is overwritten too early differ now and then."""
+    torch = torch_cuda()
+    for T, N, K in [(600, 7168, 320), (1100, 7168, 544), (2300, 7168, 1056)]:
+        log(f"linear with add, again and again, T={T} N={N} K={K}")
+        p = Linear(torch, T, N, K, seed=8)
+        add = torch.randn(T, N, device="cuda")
+        want = p.y + add.double().cpu().numpy()
+        y = torch.zeros((T, N), device="cuda")
+        damoe.mxfp4_linear(p.x, T, K, p.tiles, N, y, p.ws, add=add)
+        _check(y, want, p.tol("f32", want) + 2.0 ** -23 * np.abs(want))
+        for _ in range(30):
+            again = torch.zeros_like(y)
+            damoe.mxfp4_linear(p.x, T, K, p.tiles, N, again, p.ws, add=add)
+            assert torch.equal(again, y)
+
+
 def test_two_products_at_once():
     """Two streams, a workspace each, many calls in flight."""
     torch = torch_cuda()
