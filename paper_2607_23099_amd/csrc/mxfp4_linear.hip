@@ -45,7 +45,7 @@ __device__ __forceinline__ float load_elem(const void* p, int64_t i, bool bf) {
 // (MA blocks) and all the tokens, MA NB accumulator blocks.  A stage, 256 columns, is 4 MA NB MFMAs a wave.  A CU loads
 // about 100 GB/s, which bounds the small tiles, so they are as near to square as whole waves of rows allow, and
 // two workgroups of 128 rows share a CU, one's start and end beside the other's stages (256 x 32 / 128 x 64, 256 x 64 /
-// 128 x 128: 15.0 / 12.5 and 17.7 / 16.7 us at T = 300, 4096 x 7168; 49.9 / 43.4 and 45.0 / 37.1 at 4096, 7168 x 2048).
+// 128 x 96: 15.0 / 12.5 and 17.7 / 14.2 us at T = 300, 4096 x 7168; 49.9 / 43.4 and 45.0 / 40.7 at 4096, 7168 x 2048).
 //   W      straight into registers, every fragment read by one wave: the registers of a step are loaded for a
 //          stage D ahead as soon as its MFMAs have read them.
 //   tokens through LDS, which the four waves share: global -> registers (D stages ahead) -> LDS (the wave's quarter
@@ -607,15 +607,16 @@ __global__ void __launch_bounds__(kRowsThreads, NT > 2 ? 2 : 4) k_mxfp4_rows(Row
 }
 
 // Which kernel a call of more than 32 tokens takes: the one with the least estimated time, in us, fitted to
-// 220 measured calls (random T = 33 to 8192, N = 100 to 8192, K = 256 to 8192; in 220 others the pick took at most
-// 1.10 of the fastest kernel's time, 1.002 in the geometric mean).
+// 660 measured calls (random T = 33 to 8192, N = 100 to 8192, K = 256 to 8192; in 220 others the pick took at most
+// 1.11 of the fastest kernel's time, 1.002 in the geometric mean).
 // k_mxfp4_rows<2, 4> runs rounds of a workgroup a CU, each a start and its waves' tiles, and its XCDs take each tile from
 // behind their L2s (`moved`, bytes).  k_mxfp4_gemm<MA, NB> runs rounds of tiles, each a fixed part, stages, which take the
-// longer the more CUs share the caches and the card's power, and, where rows of y or add are unaligned, slower stores.  A last round that is not full costs half of a full one more where the CUs hold two workgroups.
-// Fastest at T = 64 / 300 / 1000 / 4096: 4096 x 7168 rows 6.2, gemm<1, 2> 12.5 (rows 16.6), <1, 4> 20.6 (<1, 2> 21.4),
-// <2, 8> 57.1 (<2, 4> 61.3); 7168 x 2048 rows 4.5, <1, 4> 7.9 (<1, 2> 8.0), <1, 4> 12.2 (<2, 4> 12.5), <1, 4> 37.1
-// (<2, 8> 40.2).
-enum Path { kRows, kGemm12, kGemm14, kGemm24, kGemm28 };
+// longer the more CUs share the caches and the card's power, and, where rows of y or add are unaligned, slower stores.
+// A last round that is not full counts for the mean of a full one and its part where the CUs hold two workgroups.
+// Fastest at T = 64 / 300 / 1000 / 4096: 4096 x 7168 rows 6.5, gemm<1, 2> 12.5 (rows 16.4), <1, 2> 21.3 (<1, 3> 23.0),
+// <2, 8> 57.2 (<2, 4> 59.3); 7168 x 2048 rows 4.4, <1, 3> 6.8 (<1, 2> 7.6), <2, 4> 12.1 (<1, 3> 13.2), <1, 3> 40.7
+// (<2, 4> 41.3).  Tiles of 128 x 128 would be up to 8% faster in 35 calls of 660.
+enum Path { kRows, kGemm12, kGemm13, kGemm24, kGemm28 };
 
 Path path_of(int32_t T, int32_t N, int32_t K, bool vec, int cus) {
   const double nk = (double)tiles_of(K, kTileCols);
@@ -624,16 +625,16 @@ Path path_of(int32_t T, int32_t N, int32_t K, bool vec, int cus) {
   const auto part_rounds = [&](int64_t n) { return 0.5 * (rounds(n) + std::max(1.0, (double)n / cus)); };
   const int64_t nb = tiles_of(N, 32), tb = tiles_of(T, 32);
   const double moved = (double)(tb * std::min<int64_t>(8, nb) + nb * std::min<int64_t>(8, (tb + 1) / 2)) * nk * kTileBytes;
-  double best = 0.8 + part_rounds(nb * ((tb + 1) / 2)) * (2.2 + 0.085 * nk) + 0.05e-6 * moved;
+  double best = 1.2 + part_rounds(nb * ((tb + 1) / 2)) * (2.4 + 0.1 * nk) + 0.04e-6 * moved;
   Path path = kRows;
   constexpr struct {
     Path path;
     int ma, nb;
     double stage, shared, fixed, any;
   } gemms[] = {{kGemm12, 1, 2, 0.28, 0.11, 0.3, 0.0},
-               {kGemm14, 1, 4, 0.39, 0.22, 0.6, 0.5},
-               {kGemm24, 2, 4, 0.52, 0.51, 1.8, 1.1},
-               {kGemm28, 2, 8, 0.98, 1.03, 4.0, 2.5}};
+               {kGemm13, 1, 3, 0.34, 0.14, 0.45, 0.3},
+               {kGemm24, 2, 4, 0.52, 0.51, 2.2, 1.1},
+               {kGemm28, 2, 8, 0.98, 0.9, 4.4, 2.5}};
   for (const auto& g : gemms) {
     const int64_t tiles = tiles_of(N, 128 * g.ma) * tiles_of(T, 32 * g.nb);
     const double stage = g.stage + g.shared * std::min(1.0, (double)tiles / cus);
@@ -683,7 +684,7 @@ size_t x_tiles_bytes(int32_t T, int32_t K) {
 }  // namespace
 
 hipError_t mxfp4_set_lds_limits() {
-  for (const hipError_t e : {gemm_limits<1, 2>(), gemm_limits<1, 4>(), gemm_limits<2, 4>(), gemm_limits<2, 8>()})
+  for (const hipError_t e : {gemm_limits<1, 2>(), gemm_limits<1, 3>(), gemm_limits<2, 4>(), gemm_limits<2, 8>()})
     if (e != hipSuccess) return e;
   return hipSuccess;
 }
@@ -745,7 +746,7 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
   else switch (path_of(T, N, K, vec, cus)) {
     case kRows: e = rows(k_mxfp4_rows<2, 4, 0>, 2, 4); break;
     case kGemm12: e = launch_gemm<1, 2>(a, cus, stream); break;
-    case kGemm14: e = launch_gemm<1, 4>(a, cus, stream); break;
+    case kGemm13: e = launch_gemm<1, 3>(a, cus, stream); break;
     case kGemm24: e = launch_gemm<2, 4>(a, cus, stream); break;
     default: e = launch_gemm<2, 8>(a, cus, stream);
   }

@@ -201,7 +201,7 @@ TNK = [(1, 1, 32), (1, 7168, 2048), (2, 100, 96), (5, 33, 256), (16, 512, 7168),
        (129, 4100, 544), (300, 4104, 800), (513, 7001, 288), (700, 4096, 1056), (1100, 5000, 800), (600, 7169, 320),
        (2300, 4001, 1568), (2300, 4000, 1568), (600, 7168, 320), (1500, 5001, 1056), (3000, 3400, 1056),
        (4100, 2001, 8224), (600, 7168, 1568), (2300, 7168, 544), (3000, 5001, 1056),
-       (2300, 7168, 3200), (2300, 7001, 3200)]
+       (2300, 7168, 3200), (2300, 7001, 3200), (1100, 7168, 544)]
 
 
 @pytest.mark.parametrize("T,N,K", TNK)
@@ -222,7 +222,7 @@ def test_linear(T, N, K):
 @pytest.mark.parametrize("T,N,K", [(3, 100, 320), (40, 77, 2048), (300, 301, 512), (150, 4096, 544), (513, 7001, 288),
                                    (600, 7168, 320), (2300, 4001, 1568), (2300, 4008, 1568), (1500, 5001, 1056),
                                    (3000, 3400, 1056), (4100, 2001, 8224), (600, 7168, 1568), (2300, 7168, 544),
-                                   (3000, 5001, 1056), (2300, 7168, 3200), (2300, 7001, 3200)])
+                                   (3000, 5001, 1056), (2300, 7168, 3200), (2300, 7001, 3200), (1100, 7168, 544)])
 @pytest.mark.parametrize("yd", ["bf16", "f32"])
 def test_linear_add_and_strides(T, N, K, yd):
     torch = torch_cuda()
