@@ -148,9 +148,10 @@ def _p(t) -> int:
     """Device (or host numpy) pointer of a tensor, or 0 for None."""
     if t is None:
         return 0
-    if isinstance(t, np.ndarray):
+    try:
+        return t.data_ptr()
+    except AttributeError:
         return t.ctypes.data
-    return t.data_ptr()
 
 
 def _stream(stream) -> int:
@@ -326,7 +327,7 @@ def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, se
         _list("seq_offsets", seq_offsets, _INT32, S + 1)
     _check("damoe_router_loss", lib().damoe_router_loss(
         _p(logits), _dtype(logits), _ld(logits, E, ld), _p(ids), _p(mask), _p(seq_offsets), T, E, k, S, score, alpha,
-        z_coef, _p(loss), _p(counts), _p(probs), _p(tokens), _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
+        z_coef, _p(loss), _p(counts), _p(probs), _p(tokens), _p(ws), ws.nbytes, _stream(stream)))
 
 
 def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None, seq_offsets=None, S=1,
@@ -382,7 +383,7 @@ def mxfp4_linear(x, T, K, w_tiles, N, y, ws, add=None, ldx=None, ldy=None, ld_ad
         raise ValueError("add has y's type")
     _check("damoe_mxfp4_linear", lib().damoe_mxfp4_linear(
         _p(x), _dtype(x), _ld(x, K, ldx), T, K, _p(w_tiles), N, _p(add), 0 if add is None else _ld(add, N, ld_add),
-        _p(y), _dtype(y), _ld(y, N, ldy), _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
+        _p(y), _dtype(y), _ld(y, N, ldy), _p(ws), ws.nbytes, _stream(stream)))
 
 
 def read_device_error(ws, stream=None) -> int:
