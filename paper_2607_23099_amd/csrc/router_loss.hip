@@ -12,12 +12,12 @@
 // are wave reductions.  Memory bound at many tokens (the logits, and the gradient on the way back), latency
 // bound at few.
 //
-// Forward: a block takes a chunk of tokens and, for each sequence that it meets, writes one slot of partial
-// sums (probabilities and counts by expert, z, tokens).  Block b's slot of sequence s is b + s: the slots of a walk
-// over the tokens, distinct while offsets do not decrease.  The next launch adds the slots of each sequence, 32 experts
-// a block, in a fixed order, and a third one adds the sequences (the last block of the second could, found by an atomic
-// count, which takes as long as the launch).  One block adds the slots of a single sequence where they are few, and a
-// batch that fits one block takes one launch.
+// Forward: a block (of one wave, where sequences are short) takes a chunk of tokens and, for each sequence that it
+// meets, writes one slot of partial sums (probabilities and counts by expert, z, tokens).  Block b's slot of sequence s is
+// b + s: the slots of a walk over the tokens, distinct while offsets do not decrease.  The next launch adds the slots of
+// each sequence, 32 experts a block, in a fixed order, and a third one adds the sequences (the last block of the second
+// could, found by an atomic count, which takes as long as the launch).  One block adds the slots of a single sequence where
+// they are few, and a batch that fits one block takes one launch.
 #include "common.h"
 
 namespace damoe {
@@ -27,16 +27,26 @@ constexpr int kLossThreads = 512;
 constexpr int kOneThreads = 1024;  // of the block that takes a small batch alone
 constexpr int kMaxChunks = 512;    // blocks of the forward pass: two per compute unit
 constexpr int kMinChunk = 4 * kLossThreads / kWave;
+constexpr int kWaveChunk = 4;      // tokens of a block of one wave
 constexpr int kGroup = 32;         // experts of a block that adds slots, where there are few sequences
 constexpr int kFewSeqs = 16;       // below this many sequences their blocks have 1024 threads, else 256
 constexpr int kManySeqs = 128;     // from here on a block adds all experts of a sequence
 constexpr int kGradThreads = 256;
 constexpr int kGradWaves = kGradThreads / kWave;
 
+// Up to kWaveTokens tokens, in sequences of up to kWaveMean in the mean, blocks are single waves of four tokens: a block
+// goes over its sequences in turn, 1.7 us each.  One wave / eight, all launches: 40 tokens in 28 sequences 14.5 / 56 us,
+// 512 in 512 (256 experts) 18.6 / 77, 512 in 8 12.1 / 12.9, 4096 in 64 12.8 / 12.8, one of 3969 tokens and 127 of one
+// 50 / 80; beyond, the slots of long sequences cost more (4096 in 2 15.6 / 13.1, 16384 in 512 19.4 / 15.4).
+constexpr int32_t kWaveTokens = 4096, kWaveMean = 64;
+
+bool by_waves(int32_t T, int32_t S) { return T <= kWaveTokens && T <= (int64_t)S * kWaveMean; }
+
 // Tokens of a block of the forward pass.
-__host__ __device__ inline int32_t chunk_tokens(int32_t T) {
+int32_t chunk_tokens(int32_t T, int32_t S) {
+  if (by_waves(T, S)) return kWaveChunk;
   const int32_t c = (T + kMaxChunks - 1) / kMaxChunks;
-  return (c + kMinChunk - 1) / kMinChunk * kMinChunk;
+  return std::max((c + kMinChunk - 1) / kMinChunk * kMinChunk, kMinChunk);
 }
 
 struct LossArgs {
@@ -260,6 +270,9 @@ __device__ __forceinline__ void write_loss(const LossArgs& a, double balance, do
 
 constexpr int kAloneThreads = 1024, kTotalThreads = 256;
 
+// Rows of sums that a block's waves leave in LDS.
+constexpr int loss_rows(int threads) { return threads > kWave ? threads / kWave / 2 : 1; }
+
 template <int THREADS>
 struct SeqSmem {
   float4 p[THREADS];
@@ -410,15 +423,16 @@ __global__ void __launch_bounds__(kTotalThreads) k_router_loss_total(LossArgs a)
   }
 }
 
-// ONE: the batch is one block's, which has every sequence's sums and finishes them.
-template <int V, int NC, bool BF, bool SIG, bool ONE>
-__global__ void __launch_bounds__(ONE ? kOneThreads : kLossThreads) k_router_loss(LossArgs a) {
-  constexpr int kThreads = ONE ? kOneThreads : kLossThreads, kWaves = kThreads / kWave;
+// ONE (kOneThreads): the batch is one block's, which has every sequence's sums and finishes them.
+template <int V, int NC, bool BF, bool SIG, int kThreads>
+__global__ void __launch_bounds__(kThreads) k_router_loss(LossArgs a) {
+  constexpr bool ONE = kThreads == kOneThreads;
+  constexpr int kWaves = kThreads / kWave, kRed = loss_rows(kThreads);
   // Rows of logits a wave holds at a time.
   constexpr int kRows = V * NC <= 4 ? 4 : V * NC <= 8 ? 2 : 1;
   extern __shared__ __attribute__((aligned(16))) float loss_smem[];
-  float* const red = loss_smem;                                          // [kWaves / 2][E]
-  int32_t* const hist = reinterpret_cast<int32_t*>(red + kWaves / 2 * a.E);  // [E]
+  float* const red = loss_smem;                                      // [kRed][E]
+  int32_t* const hist = reinterpret_cast<int32_t*>(red + kRed * a.E);  // [E]
   __shared__ float z_red[kWaves];
   __shared__ int32_t n_red[kWaves];
   __shared__ double l_red[kWaves];
@@ -547,7 +561,7 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kLossThreads) k_router_los
       int cnt = 0;
       if (e < E) {
 #pragma unroll
-        for (int i = 0; i < kWaves / 2; ++i) p += red[i * E + e];
+        for (int i = 0; i < kRed; ++i) p += red[i * E + e];
         cnt = hist[e];
         hist[e] = 0;
       }
@@ -790,7 +804,7 @@ struct LossWs {
 int32_t padded(int32_t E) { return (E + kGroup - 1) / kGroup * kGroup; }
 
 LossWs loss_ws(int32_t T, int32_t E, int32_t S) {
-  const int32_t chunk = std::max(chunk_tokens(T), kMinChunk), Ep = padded(E);
+  const int32_t chunk = chunk_tokens(T, S), Ep = padded(E);
   const size_t slots = (size_t)((T + chunk - 1) / chunk) + S;
   LossWs o;
   o.part = 256;
@@ -821,10 +835,12 @@ extern "C" {
 
 size_t damoe_router_loss_workspace_size(int32_t T_max, int32_t E, int32_t S) {
   if (!loss_shape_ok(T_max, E, 1, S)) return 0;
-  // The chunk grows with T in steps, so a smaller T may take more blocks, but never over kMaxChunks.
+  // The chunk grows with T in steps, so a smaller T may take more blocks: never over kMaxChunks, or those of the last T
+  // that waves take.
   const size_t at = loss_ws(T_max, E, S).total;
   const int32_t full = std::min<int32_t>(T_max, kMaxChunks * kMinChunk);
-  return std::max({at, loss_ws(full, E, S).total, loss_ws(std::min(T_max, 1), E, S).total});
+  const int32_t waves = (int32_t)std::min<int64_t>({T_max, kWaveTokens, (int64_t)S * kWaveMean});
+  return std::max({at, loss_ws(full, E, S).total, loss_ws(waves, E, S).total});
 }
 
 damoe_status damoe_router_loss(const void* logits, int32_t dtype, int64_t ld, const int32_t* topk_ids,
@@ -850,7 +866,7 @@ damoe_status damoe_router_loss(const void* logits, int32_t dtype, int64_t ld, co
   a.E = E;
   a.k = k;
   a.S = S;
-  a.chunk = std::max(chunk_tokens(T), kMinChunk);
+  a.chunk = chunk_tokens(T, S);
   a.nb = (T + a.chunk - 1) / a.chunk;
   a.err = reinterpret_cast<int32_t*>(base);
   a.part = reinterpret_cast<float2*>(base + o.part);
@@ -868,14 +884,16 @@ damoe_status damoe_router_loss(const void* logits, int32_t dtype, int64_t ld, co
   // One block does it all for up to kOneTokens tokens of a few sequences.
   const bool one = T <= kOneTokens && S <= kOneSeqs;
   if (one) a.chunk = std::max(T, 1), a.nb = 1;
-  const size_t lds = (size_t)((one ? kOneThreads : kLossThreads) / kWave / 2 + 1) * E * 4;
+  const bool waves = !one && by_waves(T, S);
+  const size_t lds = (size_t)(loss_rows(one ? kOneThreads : waves ? kWave : kLossThreads) + 1) * E * 4;
   const dim3 grid(std::max(a.nb, 1));
   const hipError_t e = by_columns(E, fours(logits, ld, E, dtype), [&](auto v, auto nc) {
     return by_kind(dtype, score, [&](auto bf, auto sig) {
       constexpr int V = decltype(v)::value, NC = decltype(nc)::value;
       constexpr bool BF = decltype(bf)::value, SIG = decltype(sig)::value;
-      if (one) hipLaunchKernelGGL((k_router_loss<V, NC, BF, SIG, true>), grid, dim3(kOneThreads), lds, stream, a);
-      else hipLaunchKernelGGL((k_router_loss<V, NC, BF, SIG, false>), grid, dim3(kLossThreads), lds, stream, a);
+      if (one) hipLaunchKernelGGL((k_router_loss<V, NC, BF, SIG, kOneThreads>), grid, dim3(kOneThreads), lds, stream, a);
+      else if (waves) hipLaunchKernelGGL((k_router_loss<V, NC, BF, SIG, kWave>), grid, dim3(kWave), lds, stream, a);
+      else hipLaunchKernelGGL((k_router_loss<V, NC, BF, SIG, kLossThreads>), grid, dim3(kLossThreads), lds, stream, a);
       return hipGetLastError();
     });
   });

@@ -119,6 +119,21 @@ def test_many_sequences():
     Case(torch, 50, 16, 2, offsets=[0] + [30] * 5000 + [45]).check(torch, 0)
 
 
+@pytest.mark.parametrize("T,E,k,lengths,dtype", [
+    (40, 64, 8, [1] * 20 + [0, 3, 0, 9], "f32"), (99, 37, 4, [1] * 99, "bf16"), (513, 256, 8, [400] + [1] * 100, "f32"),
+    (120, 1000, 6, [4] * 29, "bf16"), (130, 1023, 3, [3, 5] * 16, "f32"), (1030, 384, 8, [0, 0, 7] * 140 + [21], "f32"),
+    (4096, 48, 2, [64] * 64, "f32"), (4097, 48, 2, [64] * 64 + [1], "f32"), (5003, 48, 2, [0, 1, 2, 3, 4] * 500, "bf16"),
+    (16500, 40, 2, [16] * 1031, "f32")])
+def test_short_sequences(T, E, k, lengths, dtype):
+    torch = torch_cuda()
+    off = np.concatenate([[0], np.cumsum(lengths)]).tolist()
+    assert off[-1] <= T
+    for score in (0, 1):
+        log(f"router loss of {len(lengths)} short sequences T={T} E={E} {dtype} score={score}")
+        mask = (np.random.default_rng(T).random(T) < 0.85).astype(np.uint8)
+        Case(torch, T, E, k, offsets=off, mask=mask, dtype=dtype).check(torch, score)
+
+
 def test_many_tokens_ragged():
     torch = torch_cuda()
     rng = np.random.default_rng(1)

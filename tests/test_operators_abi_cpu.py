@@ -192,3 +192,9 @@ def test_objects_refuse_what_their_buffers_do_not_hold():
     for call in (path.router_loss, path.router_loss_grad):
         with pytest.raises(ValueError):
             call(5, 0.1)
+
+
+def test_router_loss_workspace_holds_every_smaller_batch():
+    for E, S in [(64, 2), (64, 15), (256, 64), (384, 65), (40, 5000)]:
+        sizes = [damoe.router_loss_workspace_size(T, E, S) for T in list(range(0, 5000, 7)) + [8192, 16384, 16385, 70000, 1 << 20]]
+        assert all(0 < a <= b for a, b in zip(sizes, sizes[1:])), (E, S)
