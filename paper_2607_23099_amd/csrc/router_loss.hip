@@ -27,24 +27,23 @@ constexpr int kLossThreads = 512;
 constexpr int kOneThreads = 1024;  // of the block that takes a small batch alone
 constexpr int kMaxChunks = 512;    // blocks of the forward pass: two per compute unit
 constexpr int kMinChunk = 4 * kLossThreads / kWave;
-constexpr int kWaveChunk = 4;      // tokens of a block of one wave
 constexpr int kGroup = 32;         // experts of a block that adds slots, where there are few sequences
 constexpr int kFewSeqs = 16;       // below this many sequences their blocks have 1024 threads, else 256
 constexpr int kManySeqs = 128;     // from here on a block adds all experts of a sequence
 constexpr int kGradThreads = 256;
 constexpr int kGradWaves = kGradThreads / kWave;
 
-// Up to kWaveTokens tokens, in sequences of up to kWaveMean in the mean, blocks are single waves of four tokens: a block
-// goes over its sequences in turn, 1.7 us each.  One wave / eight, all launches: 40 tokens in 28 sequences 14.5 / 56 us,
-// 512 in 512 (256 experts) 18.6 / 77, 512 in 8 12.1 / 12.9, 4096 in 64 12.8 / 12.8, one of 3969 tokens and 127 of one
-// 50 / 80; beyond, the slots of long sequences cost more (4096 in 2 15.6 / 13.1, 16384 in 512 19.4 / 15.4).
+// Up to kWaveTokens tokens, in sequences of up to kWaveMean in the mean, blocks are single waves of up to four tokens: a
+// block goes over its sequences in turn, 1.7 us each.  Waves / blocks of eight, all launches: 40 tokens in 28 sequences
+// 10.9 / 56 us, 512 in 512 (256 experts) 12.5 / 77, 512 in 8 12.1 / 12.9, 4096 in 64 12.8 / 12.8, one of 3969 tokens and
+// 127 of one 50 / 80; beyond, the slots of long sequences cost more (4096 in 2 15.6 / 13.1, 16384 in 512 19.4 / 15.4).
 constexpr int32_t kWaveTokens = 4096, kWaveMean = 64;
 
 bool by_waves(int32_t T, int32_t S) { return T <= kWaveTokens && T <= (int64_t)S * kWaveMean; }
 
 // Tokens of a block of the forward pass.
 int32_t chunk_tokens(int32_t T, int32_t S) {
-  if (by_waves(T, S)) return kWaveChunk;
+  if (by_waves(T, S)) return T < 2 * (int64_t)S ? 1 : T < 4 * (int64_t)S ? 2 : 4;
   const int32_t c = (T + kMaxChunks - 1) / kMaxChunks;
   return std::max((c + kMinChunk - 1) / kMinChunk * kMinChunk, kMinChunk);
 }
@@ -836,11 +835,13 @@ extern "C" {
 size_t damoe_router_loss_workspace_size(int32_t T_max, int32_t E, int32_t S) {
   if (!loss_shape_ok(T_max, E, 1, S)) return 0;
   // The chunk grows with T in steps, so a smaller T may take more blocks: never over kMaxChunks, or those of the last T
-  // that waves take.
+  // that waves take one, two or four tokens at a time.
   const size_t at = loss_ws(T_max, E, S).total;
   const int32_t full = std::min<int32_t>(T_max, kMaxChunks * kMinChunk);
-  const int32_t waves = (int32_t)std::min<int64_t>({T_max, kWaveTokens, (int64_t)S * kWaveMean});
-  return std::max({at, loss_ws(full, E, S).total, loss_ws(waves, E, S).total});
+  size_t most = std::max(at, loss_ws(full, E, S).total);
+  for (const int64_t t : {2 * (int64_t)S - 1, 4 * (int64_t)S - 1, (int64_t)S * kWaveMean})
+    most = std::max(most, loss_ws((int32_t)std::min<int64_t>({T_max, kWaveTokens, t}), E, S).total);
+  return most;
 }
 
 damoe_status damoe_router_loss(const void* logits, int32_t dtype, int64_t ld, const int32_t* topk_ids,
