@@ -465,7 +465,8 @@ typedef enum damoe_score {
  * (a term whose coefficient is 0 is left out of loss[0]; without a valid token all three are 0).
  *   logits      bf16 or fp32 (dtype) [T][ld], ld >= E; -inf is an expert that is switched off.  A
  *               valid row of -inf alone has p = 0 and adds nothing to z; a valid row with a NaN or
- *               +inf gives NaN.  Rows of tokens that are not valid are not read
+ *               +inf makes its sequence's P, balance and z NaN.  Rows of tokens that are not valid are
+ *               not read
  *   topk_ids    int32 [T][k]; a negative id is a masked slot, an id >= E is dropped and
  *               flagged (DAMOE_DEVERR_EXPERT_ID); an id that a token holds twice counts twice
  *   mask        uint8 [T], or NULL: every token of a sequence is valid
@@ -492,8 +493,9 @@ damoe_status damoe_router_loss(const void* logits, int32_t dtype, int64_t ld, co
  *                 + g z_coef 2 / N log(sum_j exp l_tj) exp(l_te) / sum_j exp(l_tj)
  *                 + sum over the slots j with topk_ids[t][j] = e of w_tj (dw_tj - sum_i w_ti dw_ti)
  * (sums over slots skip ids outside [0, E)).  dlogits has the logits' type, [T][ldd], ldd >= E; the row of
- * a token that is not valid, or in no sequence, is 0.  dlogits may be logits itself (ldd = ld).  counts and
- * tokens are damoe_router_loss's of the same inputs.  Stream-ordered, no workspace, capturable. */
+ * a token that is not valid, or in no sequence, is 0, that of a valid token whose logits hold a NaN or +inf is
+ * NaN.  dlogits may be logits itself (ldd = ld).  counts and tokens are damoe_router_loss's of the same
+ * inputs.  Stream-ordered, no workspace, capturable. */
 damoe_status damoe_router_loss_grad(const void* logits, int32_t dtype, int64_t ld, const int32_t* topk_ids,
                                     const float* topk_w, const float* dtopk_w, const uint8_t* mask,
                                     const int32_t* seq_offsets, const int32_t* counts, const int32_t* tokens,

@@ -229,6 +229,10 @@ __device__ __forceinline__ float2 sigmoids(float l, float ex, float m) {
   return make_float2(m < 0.f ? ex * r : l >= 0.f ? big : small, l >= 0.f ? small : big);
 }
 
+// What a row's sigmoids are divided by: their sum, or NaN where the sum of the shifted exponentials is, since the sigmoid of
+// +inf is a finite 1 (and a term of the gradient that a coefficient of 0 multiplies would be NaN in that column alone).
+__device__ __forceinline__ float norm_of(float sigmoid_sum, float exp_sum) { return exp_sum == exp_sum ? sigmoid_sum : exp_sum; }
+
 __device__ __forceinline__ int offset_at(const int32_t* off, int32_t s, int32_t T) {
   const int o = off ? off[s] : (s == 0 ? 0 : T);
   return min(max(o, 0), T);
@@ -516,7 +520,7 @@ __global__ void __launch_bounds__(kThreads) k_router_loss(LossArgs a) {
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
         sum[u] = wave_sum(sum[u]);
-        inv[u] = SIG ? wave_sum(inv[u]) : sum[u];
+        inv[u] = SIG ? norm_of(wave_sum(inv[u]), sum[u]) : sum[u];
       }
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
@@ -671,7 +675,7 @@ struct Grad {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       sum[u] = wave_sum(sum[u]);
-      ps[u] = SIG ? wave_sum(ps[u]) : sum[u];
+      ps[u] = SIG ? norm_of(wave_sum(ps[u]), sum[u]) : sum[u];
       fp[u] = wave_sum(fp[u]);
     }
 #pragma unroll
