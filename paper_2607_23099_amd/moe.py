@@ -8,6 +8,8 @@ the library and nothing else.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import damoe, synth
@@ -70,6 +72,14 @@ class DeviceLayer:
         return 3 * sh.H * sh.I + 3 * (sh.H // 128) * (sh.I // 128) * 4
 
 
+def _owned_by(stream, device):
+    """Context in which new tensors belong to `stream` (None: the current one; a Stream or a handle), so that the
+    allocator neither hands it memory that another stream's queued work still uses nor takes back what it still uses."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
+
+
 class QuantisedLayer:
     """An MXFP4 layer's packed weights and its descriptor (what DeviceLayer holds for generated ones)."""
 
@@ -82,22 +92,25 @@ class QuantisedLayer:
 
 def quantise_layer(shape: synth.Shape, w1, w3, w2, stream=None) -> QuantisedLayer:
     """MXFP4 layer of bf16 or fp32 weights on the device (w1, w3 [E][I][H], w2 [E][H][I], contiguous): one pass
-    over each into the packed layout, no row-major copy."""
+    over each into the packed layout, no row-major copy.  With `stream`, the passes run on it and the packed weights
+    belong to it: it waits for the weights, and other streams for it, by the caller."""
     packed = {}
     for name, t in (("w1", w1), ("w3", w3), ("w2", w2)):
         _, r, c = synth.weight_dims(shape, name)
         if tuple(t.shape) != (shape.E, r, c) or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous [{shape.E}][{r}][{c}] tensor")
         n = damoe.mxfp4_bytes(shape.E * r, c, damoe.LAYOUT_FRAG16)
-        packed[name] = torch.empty((shape.E, n // shape.E), dtype=torch.uint8, device=t.device)
+        with _owned_by(stream, t.device):
+            packed[name] = torch.empty((shape.E, n // shape.E), dtype=torch.uint8, device=t.device)
         damoe.mxfp4_quantise(t, shape.E * r, c, packed[name], None, damoe.LAYOUT_FRAG16, ldx=c, stream=stream)
     return QuantisedLayer(shape, packed)
 
 
 class MxLinear:
     """A dense MXFP4 product next to the experts (a shared expert's projections, a dense layer): the weights
-    [N][K] quantised once into the product's layout, and a workspace for up to T_max tokens.  Calls of one object
-    share its workspace, so they belong on one stream (and in one graph) at a time."""
+    [N][K] quantised once into the product's layout, and a workspace for up to T_max tokens.  The constructor waits
+    for the quantisation, so calls may come on any stream.  Calls of one object share its workspace, so they belong on
+    one stream (and in one graph) at a time, and the object is dropped when their work is done."""
 
     def __init__(self, weight, T_max: int):
         self.N, self.K = weight.shape
@@ -109,9 +122,12 @@ class MxLinear:
         damoe.mxfp4_quantise(weight, self.N, self.K, self.tiles)
         self.ws = torch.empty(damoe.mxfp4_linear_workspace_size(T_max, self.N, self.K), dtype=torch.uint8,
                               device=weight.device)
+        torch.cuda.current_stream(weight.device).synchronize()
 
     def __call__(self, x, y=None, add=None, stream=None):
-        """add + Q(x) W^T of the rows of x [T][K], into y (by default new, of x's type)."""
+        """add + Q(x) W^T of the rows of x [T][K], into y (by default new, of add's or else x's type).  With `stream`, the
+        product runs on it and a new y belongs to it, as if it were the current one: it waits for the inputs, and other
+        streams for y, by the caller."""
         T = x.shape[0]
         if T > self.T_max:
             raise ValueError("more rows than T_max")
@@ -123,7 +139,8 @@ class MxLinear:
             if t.device != self.tiles.device:
                 raise ValueError(f"a matrix on {t.device}, the weights are on {self.tiles.device}")
         if y is None:
-            y = torch.empty((T, self.N), dtype=x.dtype if add is None else add.dtype, device=x.device)
+            with _owned_by(stream, x.device):
+                y = torch.empty((T, self.N), dtype=x.dtype if add is None else add.dtype, device=x.device)
         damoe.mxfp4_linear(x, T, self.K, self.tiles, self.N, y, self.ws, add=add, stream=stream)
         return y
 

@@ -1,0 +1,76 @@
+"""Which stream owns the memory that MxLinear and quantise_layer allocate (no GPU: the library's calls are recorded)."""
+import contextlib
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2607_23099_amd import damoe, moe, synth
+
+
+class Side:
+    """Stands for a stream other than the current one."""
+
+
+@pytest.fixture
+def record(monkeypatch):
+    """What was allocated under which stream, which calls were made on which, and what was waited for."""
+    r = {"current": None, "made": {}, "calls": [], "waited": 0}
+
+    @contextlib.contextmanager
+    def stream(s):
+        before, r["current"] = r["current"], s
+        yield
+        r["current"] = before
+
+    real = torch.empty
+
+    def empty(*args, **kw):
+        t = real(*args, **kw)
+        r["made"][t.data_ptr()] = r["current"]
+        return t
+
+    class Current:
+        def synchronize(self):
+            r["waited"] += 1
+
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Current())
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: handle)
+    monkeypatch.setattr(damoe, "mxfp4_linear",
+                        lambda x, T, K, w, N, y, ws, add=None, stream=None: r["calls"].append((y, stream)))
+    monkeypatch.setattr(damoe, "mxfp4_quantise", lambda x, rows, cols, codes, scales=None, layout=2, ldx=None, stream=None:
+                        r["calls"].append((codes, stream)))
+    monkeypatch.setattr(damoe, "mxfp4_bytes", lambda rows, cols, layout=2: rows * cols)
+    monkeypatch.setattr(damoe, "mxfp4_linear_workspace_size", lambda T, N, K: 256)
+    return r
+
+
+@pytest.mark.parametrize("stream", [None, Side(), 0x1234], ids=["current", "stream", "handle"])
+def test_results_belong_to_the_stream_of_the_call(record, stream):
+    lin = moe.MxLinear(torch.zeros(64, 32), 8)
+    del record["calls"][:]
+    for x, add in [(torch.zeros(8, 32), None), (torch.zeros(3, 32), torch.zeros(3, 64))]:
+        y = lin(x, add=add, stream=stream)
+        made, used = record["calls"][-1]
+        assert made is y and used is stream and record["made"][y.data_ptr()] is stream
+    y = torch.zeros(8, 64)
+    assert lin(torch.zeros(8, 32), y, stream=stream) is y
+
+
+@pytest.mark.parametrize("stream", [None, Side(), 0x1234], ids=["current", "stream", "handle"])
+def test_packed_weights_belong_to_the_stream_of_the_call(record, stream):
+    sh = synth.Shape("streams", E=2, k=1, H=128, I=128, shape_id=9, wdtype="mxfp4")
+    w = {n: torch.zeros((sh.E,) + tuple(synth.weight_dims(sh, n)[1:])) for n in ("w1", "w3", "w2")}
+    dl = moe.quantise_layer(sh, **w, stream=stream)
+    assert len(record["calls"]) == 3
+    for made, used in record["calls"]:
+        assert used is stream and record["made"][made.data_ptr()] is stream
+    assert {t.data_ptr() for t in dl.w.values()} == {t.data_ptr() for t, _ in record["calls"]}
+
+
+def test_weights_are_ready_for_every_stream(record):
+    """A first call may come on any stream: the constructor ends when the tiles are there."""
+    moe.MxLinear(torch.zeros(64, 32), 8)
+    assert len(record["calls"]) == 1 and record["waited"] == 1
