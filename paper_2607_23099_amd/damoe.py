@@ -312,6 +312,13 @@ def _list(name: str, t, types: set, n: int):
                          f"not {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
 
 
+def _offsets(t, S: int):
+    """Refuses a list of offsets of another number of sequences than S: a longer one would lose its last sequences."""
+    _list("seq_offsets", t, _INT32, S + 1)
+    if t.numel() != S + 1:
+        raise ValueError(f"seq_offsets: S = {S} sequences have {S + 1} offsets, not {t.numel()}")
+
+
 def router_loss_workspace_size(T_max: int, E: int, S: int = 1) -> int:
     return int(lib().damoe_router_loss_workspace_size(T_max, E, S))
 
@@ -324,7 +331,7 @@ def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, se
     if mask is not None:
         _list("mask", mask, _BYTES, T)
     if seq_offsets is not None:
-        _list("seq_offsets", seq_offsets, _INT32, S + 1)
+        _offsets(seq_offsets, S)
     _check("damoe_router_loss", lib().damoe_router_loss(
         _p(logits), _dtype(logits), _ld(logits, E, ld), _p(ids), _p(mask), _p(seq_offsets), T, E, k, S, score, alpha,
         z_coef, _p(loss), _p(counts), _p(probs), _p(tokens), _p(ws), ws.nbytes, _stream(stream)))
@@ -345,7 +352,7 @@ def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None
     if mask is not None:
         _list("mask", mask, _BYTES, T)
     if seq_offsets is not None:
-        _list("seq_offsets", seq_offsets, _INT32, S + 1)
+        _offsets(seq_offsets, S)
     if dloss is not None:
         _list("dloss", dloss, _FLOAT32, 1)
     _check("damoe_router_loss_grad", lib().damoe_router_loss_grad(

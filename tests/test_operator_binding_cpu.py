@@ -1,0 +1,63 @@
+"""What the binding of the MXFP4 calls and the router's loss refuses (no GPU: every call ends before the library's)."""
+import os
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2607_23099_amd import build, damoe
+from paper_2607_23099_amd.moe import Path
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(damoe.LIB_PATH):
+        build.build_damoe()
+
+
+def _i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def _bytes(n):
+    return torch.zeros(n, dtype=torch.uint8)
+
+
+class Batch:
+    """A routed batch's tensors, good ones, any of which a call may replace."""
+    T, E, k, S = 8, 64, 4, 2
+
+    def __init__(self):
+        T, E, k, S = self.T, self.E, self.k, self.S
+        self.t = dict(logits=torch.zeros(T, E), ids=_i32(T, k), loss=torch.zeros(3), counts=_i32(S, E), tokens=_i32(S + 2),
+                      ws=_bytes(damoe.router_loss_workspace_size(T, E, S)), mask=torch.ones(T, dtype=torch.uint8),
+                      seq_offsets=_i32(S + 1), probs=torch.zeros(S, E), dlogits=torch.zeros(T, E), w=torch.zeros(T, k),
+                      dw=torch.zeros(T, k), dloss=torch.zeros(1))
+
+    def forward(self, **kw):
+        t = {**self.t, **kw}
+        damoe.router_loss(t["logits"], t["ids"], self.T, self.E, self.k, t["loss"], t["counts"], t["tokens"], t["ws"],
+                          mask=t["mask"], seq_offsets=t["seq_offsets"], S=self.S, probs=t["probs"], alpha=1.0, stream=0)
+
+    def backward(self, **kw):
+        t = {**self.t, **kw}
+        damoe.router_loss_grad(t["logits"], t["ids"], self.T, self.E, self.k, t["counts"], t["tokens"], t["dlogits"],
+                               mask=t["mask"], seq_offsets=t["seq_offsets"], S=self.S, dloss=t["dloss"], w=t["w"],
+                               dw=t["dw"], alpha=1.0, stream=0)
+
+
+def test_offsets_of_another_number_of_sequences():
+    b = Batch()
+    for call in (b.forward, b.backward):
+        for n in (2, 4, 40):
+            with pytest.raises(ValueError, match="seq_offsets"):
+                call(seq_offsets=_i32(n))
+    # Through the buffers' object: three sequences in buffers made for two.
+    path = Path.__new__(Path)
+    path.dl = type("Layer", (), {"shape": type("Shape", (), {"E": b.E, "k": b.k})})
+    path.loss_S, path.T_max, path.logits, path.ids, path.w = 2, b.T, b.t["logits"], b.t["ids"], b.t["w"]
+    path.loss, path.loss_counts, path.loss_tokens, path.loss_ws = (b.t[n] for n in ("loss", "counts", "tokens", "ws"))
+    path.loss_probs, path.dlogits = b.t["probs"], b.t["dlogits"]
+    for call in (path.router_loss, path.router_loss_grad):
+        with pytest.raises(ValueError, match="seq_offsets"):
+            call(b.T, 0.1, seq_offsets=torch.tensor([0, 2, 5, 8], dtype=torch.int32), stream=0)
