@@ -270,14 +270,22 @@ def router(x, wg, bias, T, H, E, k, logits, ids, w, ws, stream=None):
                                               _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
-_DTYPES = {}
+# torch types, filled by the first call
+_DTYPES = {}  # element types of matrices; anything else gets a code that the library refuses
+_INT32, _FLOAT32, _BYTES = set(), set(), set()
+
+
+def _types():
+    import torch
+    _BYTES.update((torch.uint8, torch.bool, torch.int8))
+    _FLOAT32.add(torch.float32)
+    _INT32.add(torch.int32)
+    _DTYPES.update({torch.bfloat16: BF16, torch.float32: F32})  # last: another thread takes it for all
 
 
 def _dtype(t) -> int:
-    """BF16 or F32 of a tensor; anything else gets a code that the library refuses."""
     if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.bfloat16: BF16, torch.float32: F32})
+        _types()
     return _DTYPES.get(t.dtype, -1)
 
 
@@ -296,27 +304,24 @@ def _ld(t, cols: int, ld) -> int:
     return max(cols, stride[0]) if t.shape[0] == 1 else stride[0]
 
 
-_INT32, _FLOAT32, _BYTES = set(), set(), set()  # torch types, filled by the first call
+def _list(name: str, t, types: set, n: int) -> int:
+    """Pointer of a tensor, 0 for None.  Refuses one that is not n elements side by side of one of the types: an int64 list
+    of offsets or of counts, or the gradient of a sum, whose elements are all the same one, would be taken for something
+    else, and a shorter list or output be read or written past its end."""
+    if t is None:
+        return 0
+    if t.dtype in types and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: {n} contiguous elements of {'/'.join(str(d) for d in types)} are wanted, "
+                     f"not {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
 
 
-def _list(name: str, t, types: set, n: int):
-    """Refuses a tensor that is not n elements side by side of one of the types: an int64 list of offsets, or the
-    gradient of a sum, whose elements are all the same one, would be read as something else."""
-    if not _INT32:
-        import torch
-        _BYTES.update((torch.uint8, torch.bool, torch.int8))
-        _FLOAT32.add(torch.float32)
-        _INT32.add(torch.int32)  # last: another thread takes it for all three
-    if t.dtype not in types or t.numel() < n or not t.is_contiguous():
-        raise ValueError(f"{name}: {n} contiguous elements of {'/'.join(str(d) for d in types)} are wanted, "
-                         f"not {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
-
-
-def _offsets(t, S: int):
+def _offsets(t, S: int) -> int:
     """Refuses a list of offsets of another number of sequences than S: a longer one would lose its last sequences."""
-    _list("seq_offsets", t, _INT32, S + 1)
-    if t.numel() != S + 1:
+    p = _list("seq_offsets", t, _INT32, S + 1)
+    if t is not None and t.numel() != S + 1:
         raise ValueError(f"seq_offsets: S = {S} sequences have {S + 1} offsets, not {t.numel()}")
+    return p
 
 
 def router_loss_workspace_size(T_max: int, E: int, S: int = 1) -> int:
@@ -326,38 +331,44 @@ def router_loss_workspace_size(T_max: int, E: int, S: int = 1) -> int:
 def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, seq_offsets=None, S=1,
                 score=SCORE_SOFTMAX, alpha=0.0, z_coef=0.0, probs=None, ld=None, stream=None):
     """Balance loss, z-loss, counts and mean probabilities of a routed batch (damoe_router_loss)."""
-    if ids is not None:
-        _list("ids", ids, _INT32, T * k)
-    if mask is not None:
-        _list("mask", mask, _BYTES, T)
-    if seq_offsets is not None:
-        _offsets(seq_offsets, S)
-    _check("damoe_router_loss", lib().damoe_router_loss(
-        _p(logits), _dtype(logits), _ld(logits, E, ld), _p(ids), _p(mask), _p(seq_offsets), T, E, k, S, score, alpha,
-        z_coef, _p(loss), _p(counts), _p(probs), _p(tokens), _p(ws), ws.nbytes, _stream(stream)))
+    if not _DTYPES:
+        _types()
+    p_ids, p_mask, p_off = _list("ids", ids, _INT32, T * k), _list("mask", mask, _BYTES, T), _offsets(seq_offsets, S)
+    try:
+        p_loss, p_counts = _list("loss", loss, _FLOAT32, 3), _list("counts", counts, _INT32, S * E)
+        p_probs, p_tokens = _list("probs", probs, _FLOAT32, S * E), _list("tokens", tokens, _INT32, S + 2)
+    except ValueError:  # what the library refuses by itself is named as it does
+        if ids is None and T > 0:
+            raise DamoeError("damoe_router_loss", -1) from None
+        if ws.nbytes < router_loss_workspace_size(T, E, S):
+            raise DamoeError("damoe_router_loss", -3) from None
+        raise
+    rc = (_lib or lib()).damoe_router_loss(
+        _p(logits), _DTYPES.get(logits.dtype, -1), _ld(logits, E, ld), p_ids, p_mask, p_off, T, E, k, S, score, alpha, z_coef,
+        p_loss, p_counts, p_probs, p_tokens, ws.data_ptr(), ws.nbytes, _stream(stream))
+    if rc:
+        raise DamoeError("damoe_router_loss", rc)
 
 
 def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None, seq_offsets=None, S=1,
                      score=SCORE_SOFTMAX, alpha=0.0, z_coef=0.0, dloss=None, w=None, dw=None, ld=None, ldd=None,
                      stream=None):
     """Gradient of the loss and of the gates w with respect to the logits (damoe_router_loss_grad)."""
+    if not _DTYPES:
+        _types()
     if dlogits.dtype != logits.dtype:
         raise ValueError("dlogits has the logits' type")
-    if ids is not None:
-        _list("ids", ids, _INT32, T * k)
-    if w is not None:
-        _list("w", w, _FLOAT32, T * k)
-    if dw is not None:
-        _list("dw", dw, _FLOAT32, T * k)
-    if mask is not None:
-        _list("mask", mask, _BYTES, T)
-    if seq_offsets is not None:
-        _offsets(seq_offsets, S)
-    if dloss is not None:
-        _list("dloss", dloss, _FLOAT32, 1)
-    _check("damoe_router_loss_grad", lib().damoe_router_loss_grad(
-        _p(logits), _dtype(logits), _ld(logits, E, ld), _p(ids), _p(w), _p(dw), _p(mask), _p(seq_offsets), _p(counts),
-        _p(tokens), T, E, k, S, score, alpha, z_coef, _p(dloss), _p(dlogits), _ld(dlogits, E, ldd), _stream(stream)))
+    p_ids, p_mask, p_off = _list("ids", ids, _INT32, T * k), _list("mask", mask, _BYTES, T), _offsets(seq_offsets, S)
+    p_w, p_dw, p_dloss = _list("w", w, _FLOAT32, T * k), _list("dw", dw, _FLOAT32, T * k), _list("dloss", dloss, _FLOAT32, 1)
+    if T > 0:
+        p_counts, p_tokens = _list("counts", counts, _INT32, S * E), _list("tokens", tokens, _INT32, S + 2)
+    else:  # without tokens neither is read
+        p_counts, p_tokens = _p(counts), _p(tokens)
+    rc = (_lib or lib()).damoe_router_loss_grad(
+        _p(logits), _DTYPES.get(logits.dtype, -1), _ld(logits, E, ld), p_ids, p_w, p_dw, p_mask, p_off, p_counts, p_tokens, T,
+        E, k, S, score, alpha, z_coef, p_dloss, _p(dlogits), _ld(dlogits, E, ldd), _stream(stream))
+    if rc:
+        raise DamoeError("damoe_router_loss_grad", rc)
 
 
 def mxfp4_bytes(rows: int, cols: int, layout: int = LAYOUT_TILE32) -> int:

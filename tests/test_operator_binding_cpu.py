@@ -61,3 +61,17 @@ def test_offsets_of_another_number_of_sequences():
     for call in (path.router_loss, path.router_loss_grad):
         with pytest.raises(ValueError, match="seq_offsets"):
             call(b.T, 0.1, seq_offsets=torch.tensor([0, 2, 5, 8], dtype=torch.int32), stream=0)
+
+
+@pytest.mark.parametrize("name", ["counts", "tokens", "loss", "probs"])
+def test_outputs_and_counts_of_another_type_or_size(name):
+    b = Batch()
+    t = b.t[name]
+    bad = [t.to(torch.int64), t.double(), t.to(torch.float32 if t.dtype == torch.int32 else torch.int32), t.reshape(-1)[:-1],
+           torch.zeros(2 * t.numel(), dtype=t.dtype)[::2], torch.zeros(1, dtype=t.dtype).expand(t.numel())]
+    for v in bad:
+        with pytest.raises(ValueError, match=name):
+            b.forward(**{name: v})
+        if name in ("counts", "tokens"):  # what torch's own counting gives is int64
+            with pytest.raises(ValueError, match=name):
+                b.backward(**{name: v})
