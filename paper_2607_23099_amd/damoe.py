@@ -289,19 +289,31 @@ def _dtype(t) -> int:
     return _DTYPES.get(t.dtype, -1)
 
 
-def _ld(t, cols: int, ld) -> int:
+def _ld(name: str, t, rows: int, cols: int, ld) -> int:
     """Row stride of a matrix in elements: as given, the tensor's own (2-D), or `cols`.  The elements of a row
-    lie side by side; a tensor of any other form is refused."""
-    if ld is not None:
+    lie side by side and the tensor holds rows x cols of them; any other is refused."""
+    if ld is None:
+        shape = t.shape
+        if len(shape) == 2:
+            if shape[0] >= rows and shape[1] >= cols:
+                if t.is_contiguous():
+                    return shape[1]
+                stride = t.stride()
+                if stride[1] == 1 or shape[1] == 1:
+                    return max(cols, stride[0]) if shape[0] == 1 else stride[0]
+        elif t.numel() >= rows * cols and t.is_contiguous():
+            return cols
+    elif rows <= 0 or (rows - 1) * ld + cols <= _reach(t):
         return int(ld)
-    stride = t.stride()
-    if len(stride) != 2:
-        if not t.is_contiguous():
-            raise ValueError("a tensor that is no matrix must be contiguous")
-        return cols
-    if stride[1] != 1 and t.shape[1] > 1:
-        raise ValueError("the elements of a row must lie side by side")
-    return max(cols, stride[0]) if t.shape[0] == 1 else stride[0]
+    raise ValueError(f"{name}: {rows} rows of {cols} elements side by side are wanted, not {tuple(t.shape)} with strides "
+                     f"{t.stride()}" + ("" if ld is None else f" taken with a row stride of {ld}"))
+
+
+def _reach(t) -> int:
+    """Elements from a tensor's first to its last."""
+    if t.is_contiguous():
+        return t.numel()
+    return 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else 0
 
 
 def _list(name: str, t, types: set, n: int) -> int:
@@ -344,7 +356,7 @@ def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, se
             raise DamoeError("damoe_router_loss", -3) from None
         raise
     rc = (_lib or lib()).damoe_router_loss(
-        _p(logits), _DTYPES.get(logits.dtype, -1), _ld(logits, E, ld), p_ids, p_mask, p_off, T, E, k, S, score, alpha, z_coef,
+        _p(logits), _DTYPES.get(logits.dtype, -1), _ld("logits", logits, T, E, ld), p_ids, p_mask, p_off, T, E, k, S, score, alpha, z_coef,
         p_loss, p_counts, p_probs, p_tokens, ws.data_ptr(), ws.nbytes, _stream(stream))
     if rc:
         raise DamoeError("damoe_router_loss", rc)
@@ -365,8 +377,8 @@ def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None
     else:  # without tokens neither is read
         p_counts, p_tokens = _p(counts), _p(tokens)
     rc = (_lib or lib()).damoe_router_loss_grad(
-        _p(logits), _DTYPES.get(logits.dtype, -1), _ld(logits, E, ld), p_ids, p_w, p_dw, p_mask, p_off, p_counts, p_tokens, T,
-        E, k, S, score, alpha, z_coef, p_dloss, _p(dlogits), _ld(dlogits, E, ldd), _stream(stream))
+        _p(logits), _DTYPES.get(logits.dtype, -1), _ld("logits", logits, T, E, ld), p_ids, p_w, p_dw, p_mask, p_off, p_counts, p_tokens, T,
+        E, k, S, score, alpha, z_coef, p_dloss, _p(dlogits), _ld("dlogits", dlogits, T, E, ldd), _stream(stream))
     if rc:
         raise DamoeError("damoe_router_loss_grad", rc)
 
@@ -378,12 +390,12 @@ def mxfp4_bytes(rows: int, cols: int, layout: int = LAYOUT_TILE32) -> int:
 
 def mxfp4_quantise(x, rows, cols, codes, scales=None, layout=LAYOUT_TILE32, ldx=None, stream=None):
     _check("damoe_mxfp4_quantise", lib().damoe_mxfp4_quantise(
-        _p(x), _dtype(x), rows, cols, _ld(x, cols, ldx), layout, _p(codes), _p(scales), _stream(stream)))
+        _p(x), _dtype(x), rows, cols, _ld("x", x, rows, cols, ldx), layout, _p(codes), _p(scales), _stream(stream)))
 
 
 def mxfp4_dequantise(codes, scales, rows, cols, x, layout=LAYOUT_TILE32, ldx=None, stream=None):
     _check("damoe_mxfp4_dequantise", lib().damoe_mxfp4_dequantise(
-        _p(codes), _p(scales), rows, cols, layout, _p(x), _dtype(x), _ld(x, cols, ldx), _stream(stream)))
+        _p(codes), _p(scales), rows, cols, layout, _p(x), _dtype(x), _ld("x", x, rows, cols, ldx), _stream(stream)))
 
 
 def mxfp4_pack(codes, scales, rows, cols, tiles, stream=None):
@@ -400,8 +412,8 @@ def mxfp4_linear(x, T, K, w_tiles, N, y, ws, add=None, ldx=None, ldy=None, ld_ad
     if add is not None and add.dtype != y.dtype:
         raise ValueError("add has y's type")
     _check("damoe_mxfp4_linear", lib().damoe_mxfp4_linear(
-        _p(x), _dtype(x), _ld(x, K, ldx), T, K, _p(w_tiles), N, _p(add), 0 if add is None else _ld(add, N, ld_add),
-        _p(y), _dtype(y), _ld(y, N, ldy), _p(ws), ws.nbytes, _stream(stream)))
+        _p(x), _dtype(x), _ld("x", x, T, K, ldx), T, K, _p(w_tiles), N, _p(add), 0 if add is None else _ld("add", add, T, N, ld_add),
+        _p(y), _dtype(y), _ld("y", y, T, N, ldy), _p(ws), ws.nbytes, _stream(stream)))
 
 
 def read_device_error(ws, stream=None) -> int:

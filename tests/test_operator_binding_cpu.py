@@ -75,3 +75,54 @@ def test_outputs_and_counts_of_another_type_or_size(name):
         if name in ("counts", "tokens"):  # what torch's own counting gives is int64
             with pytest.raises(ValueError, match=name):
                 b.backward(**{name: v})
+
+
+def _wider(t):
+    """The tensor's rows a column too short, a row too few, side by side in no matrix, and expanded."""
+    r, c = t.shape
+    flat = torch.zeros(r * c - 1, dtype=t.dtype)
+    return [t[:, :-1], t[:-1], t.new_zeros(r, 2 * c)[:, ::2], flat, t.new_zeros(c, r).t(), t.new_zeros(r, c - 1)]
+
+
+def test_matrices_that_do_not_hold_the_rows():
+    b = Batch()
+    for name, calls in [("logits", (b.forward, b.backward)), ("dlogits", (b.backward,))]:
+        for v in _wider(b.t[name]):
+            for call in calls:
+                with pytest.raises(ValueError, match=name):
+                    call(**{name: v})
+    T, N, K = 5, 64, 96
+    good = dict(x=torch.zeros(T, K), y=torch.zeros(T, N), add=torch.zeros(T, N))
+    tiles, ws = _bytes(damoe.mxfp4_bytes(N, K)), _bytes(damoe.mxfp4_linear_workspace_size(T, N, K))
+    for name in good:
+        for v in _wider(good[name]):
+            t = {**good, name: v}
+            with pytest.raises(ValueError, match=f"^{name}:"):
+                damoe.mxfp4_linear(t["x"], T, K, tiles, N, t["y"], ws, add=t["add"], stream=0)
+        # A stride given with the call: the last row has to end inside.
+        ld, cols = 128, good[name].shape[1]
+        for flat in (torch.zeros((T - 1) * ld + cols - 1), torch.zeros(T - 1, ld), torch.zeros(T, ld)[:, : cols - 1]):
+            t = {**good, name: flat}
+            with pytest.raises(ValueError, match=f"^{name}:"):
+                damoe.mxfp4_linear(t["x"], T, K, tiles, N, t["y"], ws, add=t["add"], stream=0,
+                                   **{{"x": "ldx", "y": "ldy", "add": "ld_add"}[name]: ld})
+    codes, scales = _bytes(T * K // 2), _bytes(T * K // 32)
+    for v in _wider(good["x"]):
+        with pytest.raises(ValueError, match="^x:"):
+            damoe.mxfp4_quantise(v, T, K, codes, scales, damoe.LAYOUT_ROWMAJOR, stream=0)
+        with pytest.raises(ValueError, match="^x:"):
+            damoe.mxfp4_dequantise(codes, scales, T, K, v, damoe.LAYOUT_ROWMAJOR, stream=0)
+
+
+def test_row_strides_that_the_binding_takes():
+    """What holds the rows is taken, whatever its form: the stride that the library is given."""
+    x = torch.zeros(6, 40)
+    assert damoe._ld("x", x, 6, 40, None) == 40 and damoe._ld("x", x, 5, 32, None) == 40
+    assert damoe._ld("x", x[:, 3:35], 6, 32, None) == 40 and damoe._ld("x", x[::2], 3, 40, None) == 80
+    assert damoe._ld("x", x[2:3, :32], 1, 32, None) >= 32  # of one row, any
+    assert damoe._ld("x", x[:, :1], 6, 1, None) == 40
+    assert damoe._ld("x", x.view(-1), 6, 40, None) == 40 and damoe._ld("x", x.view(2, 3, 40), 6, 40, None) == 40
+    assert damoe._ld("x", x.view(-1)[3:], 5, 32, 40) == 40 and damoe._ld("x", x[:, 3:35], 6, 32, 40) == 40
+    assert damoe._ld("x", x[1:], 5, 40, 40) == 40 and damoe._ld("x", x[:0], 0, 40, None) == 40
+    assert damoe._ld("x", x[:0].view(-1), 0, 40, 40) == 40
+    assert damoe._ld("x", x[:1].expand(6, 40), 6, 40, None) == 0  # refused by the library: a stride below the columns
