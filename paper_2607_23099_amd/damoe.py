@@ -328,6 +328,15 @@ def _list(name: str, t, types: set, n: int) -> int:
                      f"not {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
 
 
+def _room(name: str, t, n: int) -> int:
+    """Pointer of a buffer of at least n bytes side by side, 0 for None."""
+    if t is None:
+        return 0
+    if t.nbytes >= n and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: {n} contiguous bytes are wanted, not {t.nbytes} in {tuple(t.shape)} with strides {t.stride()}")
+
+
 def _offsets(t, S: int) -> int:
     """Refuses a list of offsets of another number of sequences than S: a longer one would lose its last sequences."""
     p = _list("seq_offsets", t, _INT32, S + 1)
@@ -356,8 +365,8 @@ def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, se
             raise DamoeError("damoe_router_loss", -3) from None
         raise
     rc = (_lib or lib()).damoe_router_loss(
-        _p(logits), _DTYPES.get(logits.dtype, -1), _ld("logits", logits, T, E, ld), p_ids, p_mask, p_off, T, E, k, S, score, alpha, z_coef,
-        p_loss, p_counts, p_probs, p_tokens, ws.data_ptr(), ws.nbytes, _stream(stream))
+        logits.data_ptr(), _DTYPES.get(logits.dtype, -1), _ld("logits", logits, T, E, ld), p_ids, p_mask, p_off, T, E, k, S,
+        score, alpha, z_coef, p_loss, p_counts, p_probs, p_tokens, _room("ws", ws, 0), ws.nbytes, _stream(stream))
     if rc:
         raise DamoeError("damoe_router_loss", rc)
 
@@ -377,8 +386,8 @@ def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None
     else:  # without tokens neither is read
         p_counts, p_tokens = _p(counts), _p(tokens)
     rc = (_lib or lib()).damoe_router_loss_grad(
-        _p(logits), _DTYPES.get(logits.dtype, -1), _ld("logits", logits, T, E, ld), p_ids, p_w, p_dw, p_mask, p_off, p_counts, p_tokens, T,
-        E, k, S, score, alpha, z_coef, p_dloss, _p(dlogits), _ld("dlogits", dlogits, T, E, ldd), _stream(stream))
+        logits.data_ptr(), _DTYPES.get(logits.dtype, -1), _ld("logits", logits, T, E, ld), p_ids, p_w, p_dw, p_mask, p_off,
+        p_counts, p_tokens, T, E, k, S, score, alpha, z_coef, p_dloss, dlogits.data_ptr(), _ld("dlogits", dlogits, T, E, ldd), _stream(stream))
     if rc:
         raise DamoeError("damoe_router_loss_grad", rc)
 
@@ -388,19 +397,36 @@ def mxfp4_bytes(rows: int, cols: int, layout: int = LAYOUT_TILE32) -> int:
     return int(lib().damoe_mxfp4_bytes(rows, cols, layout))
 
 
+def _codes_bytes(rows: int, cols: int, layout: int) -> int:
+    """mxfp4_bytes of a valid shape, without the call."""
+    if layout == LAYOUT_TILE32:
+        return -(-rows // 32) * -(-cols // 256) * 4352
+    return rows * cols // 2 if layout == LAYOUT_ROWMAJOR else rows * cols // 32 * 17
+
+
 def mxfp4_quantise(x, rows, cols, codes, scales=None, layout=LAYOUT_TILE32, ldx=None, stream=None):
-    _check("damoe_mxfp4_quantise", lib().damoe_mxfp4_quantise(
-        _p(x), _dtype(x), rows, cols, _ld("x", x, rows, cols, ldx), layout, _p(codes), _p(scales), _stream(stream)))
+    p_codes = _room("codes", codes, _codes_bytes(rows, cols, layout))
+    p_scales = _room("scales", scales, rows * cols // 32) if layout == LAYOUT_ROWMAJOR else 0
+    rc = (_lib or lib()).damoe_mxfp4_quantise(x.data_ptr(), _dtype(x), rows, cols, _ld("x", x, rows, cols, ldx), layout, p_codes,
+                                              p_scales, _stream(stream))
+    if rc:
+        raise DamoeError("damoe_mxfp4_quantise", rc)
 
 
 def mxfp4_dequantise(codes, scales, rows, cols, x, layout=LAYOUT_TILE32, ldx=None, stream=None):
-    _check("damoe_mxfp4_dequantise", lib().damoe_mxfp4_dequantise(
-        _p(codes), _p(scales), rows, cols, layout, _p(x), _dtype(x), _ld("x", x, rows, cols, ldx), _stream(stream)))
+    p_codes = _room("codes", codes, _codes_bytes(rows, cols, layout))
+    p_scales = _room("scales", scales, rows * cols // 32) if layout == LAYOUT_ROWMAJOR else 0
+    rc = (_lib or lib()).damoe_mxfp4_dequantise(p_codes, p_scales, rows, cols, layout, x.data_ptr(), _dtype(x),
+                                                _ld("x", x, rows, cols, ldx), _stream(stream))
+    if rc:
+        raise DamoeError("damoe_mxfp4_dequantise", rc)
 
 
 def mxfp4_pack(codes, scales, rows, cols, tiles, stream=None):
     """Row-major codes and scales into the operand layout of mxfp4_linear."""
-    _check("damoe_mxfp4_pack", lib().damoe_mxfp4_pack(_p(codes), _p(scales), rows, cols, _p(tiles), _stream(stream)))
+    _check("damoe_mxfp4_pack", lib().damoe_mxfp4_pack(
+        _room("codes", codes, rows * cols // 2), _room("scales", scales, rows * cols // 32), rows, cols,
+        _room("tiles", tiles, _codes_bytes(rows, cols, LAYOUT_TILE32)), _stream(stream)))
 
 
 def mxfp4_linear_workspace_size(T_max: int, N: int, K: int) -> int:
@@ -411,9 +437,13 @@ def mxfp4_linear(x, T, K, w_tiles, N, y, ws, add=None, ldx=None, ldy=None, ld_ad
     """y = add + Q(x) W^T with W in tiles (damoe_mxfp4_linear); add has y's type."""
     if add is not None and add.dtype != y.dtype:
         raise ValueError("add has y's type")
-    _check("damoe_mxfp4_linear", lib().damoe_mxfp4_linear(
-        _p(x), _dtype(x), _ld("x", x, T, K, ldx), T, K, _p(w_tiles), N, _p(add), 0 if add is None else _ld("add", add, T, N, ld_add),
-        _p(y), _dtype(y), _ld("y", y, T, N, ldy), _p(ws), ws.nbytes, _stream(stream)))
+    p_tiles = _room("w_tiles", w_tiles, _codes_bytes(N, K, LAYOUT_TILE32))
+    p_add, lda = (0, 0) if add is None else (add.data_ptr(), _ld("add", add, T, N, ld_add))
+    rc = (_lib or lib()).damoe_mxfp4_linear(
+        x.data_ptr(), _dtype(x), _ld("x", x, T, K, ldx), T, K, p_tiles, N, p_add, lda, y.data_ptr(), _dtype(y),
+        _ld("y", y, T, N, ldy), _room("ws", ws, 0), ws.nbytes, _stream(stream))
+    if rc:
+        raise DamoeError("damoe_mxfp4_linear", rc)
 
 
 def read_device_error(ws, stream=None) -> int:

@@ -126,3 +126,36 @@ def test_row_strides_that_the_binding_takes():
     assert damoe._ld("x", x[1:], 5, 40, 40) == 40 and damoe._ld("x", x[:0], 0, 40, None) == 40
     assert damoe._ld("x", x[:0].view(-1), 0, 40, 40) == 40
     assert damoe._ld("x", x[:1].expand(6, 40), 6, 40, None) == 0  # refused by the library: a stride below the columns
+
+
+def test_buffers_that_do_not_hold_the_codes():
+    rows, cols = 48, 384
+    x = torch.zeros(rows, cols)
+    for layout in (damoe.LAYOUT_ROWMAJOR, damoe.LAYOUT_FRAG16, damoe.LAYOUT_TILE32):
+        n, row = damoe.mxfp4_bytes(rows, cols, layout), layout == damoe.LAYOUT_ROWMAJOR
+        assert damoe._codes_bytes(rows, cols, layout) == n
+        codes, scales = _bytes(n), _bytes(rows * cols // 32) if row else None
+        bad = [("codes", codes[:-1], scales), ("codes", _bytes(2 * n)[::2], scales)]
+        bad += [("scales", codes, scales[:-1]), ("scales", codes, _bytes(2 * scales.numel())[::2])] if row else []
+        for name, c, s in bad:
+            with pytest.raises(ValueError, match=f"^{name}:"):
+                damoe.mxfp4_quantise(x, rows, cols, c, s, layout, stream=0)
+            with pytest.raises(ValueError, match=f"^{name}:"):
+                damoe.mxfp4_dequantise(c, s, rows, cols, x, layout, stream=0)
+    for r, c in [(1, 32), (33, 288), (31, 256), (32, 257 * 32)]:
+        assert damoe._codes_bytes(r, c, damoe.LAYOUT_TILE32) == damoe.mxfp4_bytes(r, c)
+    codes, scales, tiles = _bytes(rows * cols // 2), _bytes(rows * cols // 32), _bytes(damoe.mxfp4_bytes(rows, cols))
+    for name, a in [("codes", (codes[:-1], scales, tiles)), ("scales", (codes, scales[:-1], tiles)),
+                    ("tiles", (codes, scales, tiles[:-1]))]:
+        with pytest.raises(ValueError, match=f"^{name}:"):
+            damoe.mxfp4_pack(a[0], a[1], rows, cols, a[2], stream=0)
+    T = 3
+    y, ws = torch.zeros(T, rows), _bytes(damoe.mxfp4_linear_workspace_size(T, rows, cols))
+    with pytest.raises(ValueError, match="^w_tiles:"):
+        damoe.mxfp4_linear(x, T, cols, tiles[:-1], rows, y, ws, stream=0)
+    # A workspace with gaps counts bytes that it has not side by side.
+    with pytest.raises(ValueError, match="^ws:"):
+        damoe.mxfp4_linear(x, T, cols, tiles, rows, y, _bytes(2 * ws.numel())[::2], stream=0)
+    b = Batch()
+    with pytest.raises(ValueError, match="^ws:"):
+        b.forward(ws=_bytes(2 * b.t["ws"].numel())[::2])
