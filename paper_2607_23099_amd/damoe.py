@@ -163,6 +163,28 @@ def _stream(stream) -> int:
     return stream.cuda_stream
 
 
+_torch = None  # set by _types()
+
+
+def _stream_on(fn: str, stream, dev: int, dtype: int, rows: int = 1) -> int:
+    """The stream's handle for a call on tensors of device number `dev` (-1: the host's memory), which a kernel on
+    the current device would fault on unless it is that device.  Without rows nothing is launched."""
+    if dev < 0 or dev != _torch._C._cuda_getDevice():
+        if dtype < 0:  # what the library refuses by itself is named as it does
+            raise DamoeError(fn, -2)
+        if rows == 0:
+            return 0
+        raise ValueError(f"{fn}: tensors of the current device are wanted, not of "
+                         + (f"cuda:{dev} (torch.cuda.device makes it the current one)" if dev >= 0 else "the host"))
+    if stream is None:
+        return _torch._C._cuda_getCurrentRawStream(dev)
+    if isinstance(stream, int):
+        return stream
+    if getattr(stream, "device_index", dev) != dev:
+        raise ValueError(f"{fn}: a stream of cuda:{stream.device_index}, the tensors are on cuda:{dev}")
+    return stream.cuda_stream
+
+
 # ---------------------------------------------------------------- registry / layout
 
 def num_variants() -> int:
@@ -276,7 +298,9 @@ _INT32, _FLOAT32, _BYTES = set(), set(), set()
 
 
 def _types():
+    global _torch
     import torch
+    _torch = torch
     _BYTES.update((torch.uint8, torch.bool, torch.int8))
     _FLOAT32.add(torch.float32)
     _INT32.add(torch.int32)
@@ -289,9 +313,11 @@ def _dtype(t) -> int:
     return _DTYPES.get(t.dtype, -1)
 
 
-def _ld(name: str, t, rows: int, cols: int, ld) -> int:
+def _ld(name: str, t, rows: int, cols: int, ld, dev: int) -> int:
     """Row stride of a matrix in elements: as given, the tensor's own (2-D), or `cols`.  The elements of a row
-    lie side by side and the tensor holds rows x cols of them; any other is refused."""
+    lie side by side and the tensor holds rows x cols of them on device number `dev`; any other is refused."""
+    if t.get_device() != dev:
+        _elsewhere(name, t)
     if ld is None:
         shape = t.shape
         if len(shape) == 2:
@@ -309,6 +335,10 @@ def _ld(name: str, t, rows: int, cols: int, ld) -> int:
                      f"{t.stride()}" + ("" if ld is None else f" taken with a row stride of {ld}"))
 
 
+def _elsewhere(name: str, t):
+    raise ValueError(f"{name}: a tensor on {t.device}, others of the call are on another device")
+
+
 def _reach(t) -> int:
     """Elements from a tensor's first to its last."""
     if t.is_contiguous():
@@ -316,30 +346,34 @@ def _reach(t) -> int:
     return 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else 0
 
 
-def _list(name: str, t, types: set, n: int) -> int:
-    """Pointer of a tensor, 0 for None.  Refuses one that is not n elements side by side of one of the types: an int64 list
-    of offsets or of counts, or the gradient of a sum, whose elements are all the same one, would be taken for something
-    else, and a shorter list or output be read or written past its end."""
+def _list(name: str, t, types: set, n: int, dev: int) -> int:
+    """Pointer of a tensor on device number `dev`, 0 for None.  Refuses one that is not n elements side by side of one of
+    the types: an int64 list of offsets or of counts, or the gradient of a sum, whose elements are all the same one, would
+    be taken for something else, and a shorter list or output be read or written past its end."""
     if t is None:
         return 0
     if t.dtype in types and t.numel() >= n and t.is_contiguous():
+        if t.get_device() != dev:
+            _elsewhere(name, t)
         return t.data_ptr()
     raise ValueError(f"{name}: {n} contiguous elements of {'/'.join(str(d) for d in types)} are wanted, "
                      f"not {tuple(t.shape)} of {t.dtype}, strides {t.stride()}")
 
 
-def _room(name: str, t, n: int) -> int:
-    """Pointer of a buffer of at least n bytes side by side, 0 for None."""
+def _room(name: str, t, n: int, dev: int) -> int:
+    """Pointer of a buffer of at least n bytes side by side on device number `dev`, 0 for None."""
     if t is None:
         return 0
     if t.nbytes >= n and t.is_contiguous():
+        if t.get_device() != dev:
+            _elsewhere(name, t)
         return t.data_ptr()
     raise ValueError(f"{name}: {n} contiguous bytes are wanted, not {t.nbytes} in {tuple(t.shape)} with strides {t.stride()}")
 
 
-def _offsets(t, S: int) -> int:
+def _offsets(t, S: int, dev: int) -> int:
     """Refuses a list of offsets of another number of sequences than S: a longer one would lose its last sequences."""
-    p = _list("seq_offsets", t, _INT32, S + 1)
+    p = _list("seq_offsets", t, _INT32, S + 1, dev)
     if t is not None and t.numel() != S + 1:
         raise ValueError(f"seq_offsets: S = {S} sequences have {S + 1} offsets, not {t.numel()}")
     return p
@@ -354,10 +388,12 @@ def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, se
     """Balance loss, z-loss, counts and mean probabilities of a routed batch (damoe_router_loss)."""
     if not _DTYPES:
         _types()
-    p_ids, p_mask, p_off = _list("ids", ids, _INT32, T * k), _list("mask", mask, _BYTES, T), _offsets(seq_offsets, S)
+    dt, dev = _DTYPES.get(logits.dtype, -1), logits.get_device()
+    p_ids, p_mask = _list("ids", ids, _INT32, T * k, dev), _list("mask", mask, _BYTES, T, dev)
+    p_off = _offsets(seq_offsets, S, dev)
     try:
-        p_loss, p_counts = _list("loss", loss, _FLOAT32, 3), _list("counts", counts, _INT32, S * E)
-        p_probs, p_tokens = _list("probs", probs, _FLOAT32, S * E), _list("tokens", tokens, _INT32, S + 2)
+        p_loss, p_counts = _list("loss", loss, _FLOAT32, 3, dev), _list("counts", counts, _INT32, S * E, dev)
+        p_probs, p_tokens = _list("probs", probs, _FLOAT32, S * E, dev), _list("tokens", tokens, _INT32, S + 2, dev)
     except ValueError:  # what the library refuses by itself is named as it does
         if ids is None and T > 0:
             raise DamoeError("damoe_router_loss", -1) from None
@@ -365,8 +401,9 @@ def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, se
             raise DamoeError("damoe_router_loss", -3) from None
         raise
     rc = (_lib or lib()).damoe_router_loss(
-        logits.data_ptr(), _DTYPES.get(logits.dtype, -1), _ld("logits", logits, T, E, ld), p_ids, p_mask, p_off, T, E, k, S,
-        score, alpha, z_coef, p_loss, p_counts, p_probs, p_tokens, _room("ws", ws, 0), ws.nbytes, _stream(stream))
+        logits.data_ptr(), dt, _ld("logits", logits, T, E, ld, dev), p_ids, p_mask, p_off, T, E, k, S, score, alpha, z_coef,
+        p_loss, p_counts, p_probs, p_tokens, _room("ws", ws, 0, dev), ws.nbytes,
+        _stream_on("damoe_router_loss", stream, dev, dt))
     if rc:
         raise DamoeError("damoe_router_loss", rc)
 
@@ -379,15 +416,18 @@ def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None
         _types()
     if dlogits.dtype != logits.dtype:
         raise ValueError("dlogits has the logits' type")
-    p_ids, p_mask, p_off = _list("ids", ids, _INT32, T * k), _list("mask", mask, _BYTES, T), _offsets(seq_offsets, S)
-    p_w, p_dw, p_dloss = _list("w", w, _FLOAT32, T * k), _list("dw", dw, _FLOAT32, T * k), _list("dloss", dloss, _FLOAT32, 1)
+    dt, dev = _DTYPES.get(logits.dtype, -1), logits.get_device()
+    p_ids, p_mask = _list("ids", ids, _INT32, T * k, dev), _list("mask", mask, _BYTES, T, dev)
+    p_off, p_dloss = _offsets(seq_offsets, S, dev), _list("dloss", dloss, _FLOAT32, 1, dev)
+    p_w, p_dw = _list("w", w, _FLOAT32, T * k, dev), _list("dw", dw, _FLOAT32, T * k, dev)
     if T > 0:
-        p_counts, p_tokens = _list("counts", counts, _INT32, S * E), _list("tokens", tokens, _INT32, S + 2)
+        p_counts, p_tokens = _list("counts", counts, _INT32, S * E, dev), _list("tokens", tokens, _INT32, S + 2, dev)
     else:  # without tokens neither is read
         p_counts, p_tokens = _p(counts), _p(tokens)
     rc = (_lib or lib()).damoe_router_loss_grad(
-        logits.data_ptr(), _DTYPES.get(logits.dtype, -1), _ld("logits", logits, T, E, ld), p_ids, p_w, p_dw, p_mask, p_off,
-        p_counts, p_tokens, T, E, k, S, score, alpha, z_coef, p_dloss, dlogits.data_ptr(), _ld("dlogits", dlogits, T, E, ldd), _stream(stream))
+        logits.data_ptr(), dt, _ld("logits", logits, T, E, ld, dev), p_ids, p_w, p_dw, p_mask, p_off, p_counts, p_tokens, T,
+        E, k, S, score, alpha, z_coef, p_dloss, dlogits.data_ptr(), _ld("dlogits", dlogits, T, E, ldd, dev),
+        _stream_on("damoe_router_loss_grad", stream, dev, dt, T))
     if rc:
         raise DamoeError("damoe_router_loss_grad", rc)
 
@@ -405,28 +445,34 @@ def _codes_bytes(rows: int, cols: int, layout: int) -> int:
 
 
 def mxfp4_quantise(x, rows, cols, codes, scales=None, layout=LAYOUT_TILE32, ldx=None, stream=None):
-    p_codes = _room("codes", codes, _codes_bytes(rows, cols, layout))
-    p_scales = _room("scales", scales, rows * cols // 32) if layout == LAYOUT_ROWMAJOR else 0
-    rc = (_lib or lib()).damoe_mxfp4_quantise(x.data_ptr(), _dtype(x), rows, cols, _ld("x", x, rows, cols, ldx), layout, p_codes,
-                                              p_scales, _stream(stream))
+    dt, dev = _dtype(x), x.get_device()
+    p_codes = _room("codes", codes, _codes_bytes(rows, cols, layout), dev)
+    p_scales = _room("scales", scales, rows * cols // 32, dev) if layout == LAYOUT_ROWMAJOR else 0
+    rc = (_lib or lib()).damoe_mxfp4_quantise(x.data_ptr(), dt, rows, cols, _ld("x", x, rows, cols, ldx, dev), layout, p_codes,
+                                              p_scales, _stream_on("damoe_mxfp4_quantise", stream, dev, dt, rows))
     if rc:
         raise DamoeError("damoe_mxfp4_quantise", rc)
 
 
 def mxfp4_dequantise(codes, scales, rows, cols, x, layout=LAYOUT_TILE32, ldx=None, stream=None):
-    p_codes = _room("codes", codes, _codes_bytes(rows, cols, layout))
-    p_scales = _room("scales", scales, rows * cols // 32) if layout == LAYOUT_ROWMAJOR else 0
-    rc = (_lib or lib()).damoe_mxfp4_dequantise(p_codes, p_scales, rows, cols, layout, x.data_ptr(), _dtype(x),
-                                                _ld("x", x, rows, cols, ldx), _stream(stream))
+    dt, dev = _dtype(x), x.get_device()
+    p_codes = _room("codes", codes, _codes_bytes(rows, cols, layout), dev)
+    p_scales = _room("scales", scales, rows * cols // 32, dev) if layout == LAYOUT_ROWMAJOR else 0
+    rc = (_lib or lib()).damoe_mxfp4_dequantise(p_codes, p_scales, rows, cols, layout, x.data_ptr(), dt,
+                                                _ld("x", x, rows, cols, ldx, dev),
+                                                _stream_on("damoe_mxfp4_dequantise", stream, dev, dt, rows))
     if rc:
         raise DamoeError("damoe_mxfp4_dequantise", rc)
 
 
 def mxfp4_pack(codes, scales, rows, cols, tiles, stream=None):
     """Row-major codes and scales into the operand layout of mxfp4_linear."""
+    if not _DTYPES:
+        _types()
+    dev = codes.get_device()
     _check("damoe_mxfp4_pack", lib().damoe_mxfp4_pack(
-        _room("codes", codes, rows * cols // 2), _room("scales", scales, rows * cols // 32), rows, cols,
-        _room("tiles", tiles, _codes_bytes(rows, cols, LAYOUT_TILE32)), _stream(stream)))
+        _room("codes", codes, rows * cols // 2, dev), _room("scales", scales, rows * cols // 32, dev), rows, cols,
+        _room("tiles", tiles, _codes_bytes(rows, cols, LAYOUT_TILE32), dev), _stream_on("damoe_mxfp4_pack", stream, dev, 0, rows)))
 
 
 def mxfp4_linear_workspace_size(T_max: int, N: int, K: int) -> int:
@@ -437,11 +483,12 @@ def mxfp4_linear(x, T, K, w_tiles, N, y, ws, add=None, ldx=None, ldy=None, ld_ad
     """y = add + Q(x) W^T with W in tiles (damoe_mxfp4_linear); add has y's type."""
     if add is not None and add.dtype != y.dtype:
         raise ValueError("add has y's type")
-    p_tiles = _room("w_tiles", w_tiles, _codes_bytes(N, K, LAYOUT_TILE32))
-    p_add, lda = (0, 0) if add is None else (add.data_ptr(), _ld("add", add, T, N, ld_add))
+    dt, dev = _dtype(x), x.get_device()
+    p_tiles = _room("w_tiles", w_tiles, _codes_bytes(N, K, LAYOUT_TILE32), dev)
+    p_add, lda = (0, 0) if add is None else (add.data_ptr(), _ld("add", add, T, N, ld_add, dev))
     rc = (_lib or lib()).damoe_mxfp4_linear(
-        x.data_ptr(), _dtype(x), _ld("x", x, T, K, ldx), T, K, p_tiles, N, p_add, lda, y.data_ptr(), _dtype(y),
-        _ld("y", y, T, N, ldy), _room("ws", ws, 0), ws.nbytes, _stream(stream))
+        x.data_ptr(), dt, _ld("x", x, T, K, ldx, dev), T, K, p_tiles, N, p_add, lda, y.data_ptr(), _dtype(y),
+        _ld("y", y, T, N, ldy, dev), _room("ws", ws, 0, dev), ws.nbytes, _stream_on("damoe_mxfp4_linear", stream, dev, dt, T))
     if rc:
         raise DamoeError("damoe_mxfp4_linear", rc)
 

@@ -117,15 +117,15 @@ def test_matrices_that_do_not_hold_the_rows():
 def test_row_strides_that_the_binding_takes():
     """What holds the rows is taken, whatever its form: the stride that the library is given."""
     x = torch.zeros(6, 40)
-    assert damoe._ld("x", x, 6, 40, None) == 40 and damoe._ld("x", x, 5, 32, None) == 40
-    assert damoe._ld("x", x[:, 3:35], 6, 32, None) == 40 and damoe._ld("x", x[::2], 3, 40, None) == 80
-    assert damoe._ld("x", x[2:3, :32], 1, 32, None) >= 32  # of one row, any
-    assert damoe._ld("x", x[:, :1], 6, 1, None) == 40
-    assert damoe._ld("x", x.view(-1), 6, 40, None) == 40 and damoe._ld("x", x.view(2, 3, 40), 6, 40, None) == 40
-    assert damoe._ld("x", x.view(-1)[3:], 5, 32, 40) == 40 and damoe._ld("x", x[:, 3:35], 6, 32, 40) == 40
-    assert damoe._ld("x", x[1:], 5, 40, 40) == 40 and damoe._ld("x", x[:0], 0, 40, None) == 40
-    assert damoe._ld("x", x[:0].view(-1), 0, 40, 40) == 40
-    assert damoe._ld("x", x[:1].expand(6, 40), 6, 40, None) == 0  # refused by the library: a stride below the columns
+    assert damoe._ld("x", x, 6, 40, None, -1) == 40 and damoe._ld("x", x, 5, 32, None, -1) == 40
+    assert damoe._ld("x", x[:, 3:35], 6, 32, None, -1) == 40 and damoe._ld("x", x[::2], 3, 40, None, -1) == 80
+    assert damoe._ld("x", x[2:3, :32], 1, 32, None, -1) >= 32  # of one row, any
+    assert damoe._ld("x", x[:, :1], 6, 1, None, -1) == 40
+    assert damoe._ld("x", x.view(-1), 6, 40, None, -1) == 40 and damoe._ld("x", x.view(2, 3, 40), 6, 40, None, -1) == 40
+    assert damoe._ld("x", x.view(-1)[3:], 5, 32, 40, -1) == 40 and damoe._ld("x", x[:, 3:35], 6, 32, 40, -1) == 40
+    assert damoe._ld("x", x[1:], 5, 40, 40, -1) == 40 and damoe._ld("x", x[:0], 0, 40, None, -1) == 40
+    assert damoe._ld("x", x[:0].view(-1), 0, 40, 40, -1) == 40
+    assert damoe._ld("x", x[:1].expand(6, 40), 6, 40, None, -1) == 0  # refused by the library: a stride below the columns
 
 
 def test_buffers_that_do_not_hold_the_codes():
@@ -159,3 +159,60 @@ def test_buffers_that_do_not_hold_the_codes():
     b = Batch()
     with pytest.raises(ValueError, match="^ws:"):
         b.forward(ws=_bytes(2 * b.t["ws"].numel())[::2])
+
+
+def test_tensors_of_the_host_or_another_device():
+    """A kernel would fault on memory that is not the current device's."""
+    b = Batch()
+    for call in (b.forward, b.backward):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    T, N, K = 5, 64, 96
+    x, y = torch.zeros(T, K), torch.zeros(T, N)
+    tiles, ws = _bytes(damoe.mxfp4_bytes(N, K)), _bytes(damoe.mxfp4_linear_workspace_size(T, N, K))
+    codes, scales = _bytes(T * K // 2), _bytes(T * K // 32)
+    calls = [lambda x=x, rows=T, **kw: damoe.mxfp4_quantise(x, rows, K, codes, scales, damoe.LAYOUT_ROWMAJOR, **kw),
+             lambda x=x, rows=T, **kw: damoe.mxfp4_dequantise(codes, scales, rows, K, x, damoe.LAYOUT_ROWMAJOR, **kw),
+             lambda x=x, rows=T, **kw: damoe.mxfp4_linear(x, rows, K, tiles, N, y, ws, **kw)]
+    for call in calls + [lambda rows=T, **kw: damoe.mxfp4_pack(codes, scales, rows, K, _bytes(4352), **kw)]:
+        for kw in (dict(stream=0), {}):
+            with pytest.raises(ValueError, match="current device"):
+                call(**kw)
+        call(rows=0, stream=0)  # without rows, nothing is launched
+    for call in calls:
+        with pytest.raises(damoe.DamoeError, match="unsupported"):
+            call(x=x.half(), stream=0)
+
+
+@pytest.mark.gpu
+def test_one_tensor_of_the_host_among_the_device_s():
+    """Refused, whichever it is; the same call without it runs."""
+    b = Batch()
+    b.t = {n: t.cuda() for n, t in b.t.items()}
+    for call, names in [(b.forward, "logits ids loss counts tokens ws mask seq_offsets probs"),
+                        (b.backward, "logits ids counts tokens mask seq_offsets dlogits w dw dloss")]:
+        call()
+        for n in names.split():
+            with pytest.raises(ValueError, match="device"):
+                call(**{n: b.t[n].cpu()})
+    T, N, K = 5, 64, 96
+    t = dict(x=torch.zeros(T, K), w=_bytes(damoe.mxfp4_bytes(N, K)), y=torch.zeros(T, N), add=torch.zeros(T, N),
+             ws=_bytes(damoe.mxfp4_linear_workspace_size(T, N, K)))
+    t = {n: v.cuda() for n, v in t.items()}
+
+    def linear(**kw):
+        a = {**t, **kw}
+        damoe.mxfp4_linear(a["x"], T, K, a["w"], N, a["y"], a["ws"], add=a["add"])
+
+    linear()
+    for n in t:
+        with pytest.raises(ValueError, match="device"):
+            linear(**{n: t[n].cpu()})
+    codes, scales = _bytes(T * K // 2).cuda(), _bytes(T * K // 32).cuda()
+    for c, s in [(codes.cpu(), scales), (codes, scales.cpu())]:
+        for call in (lambda: damoe.mxfp4_quantise(t["x"], T, K, c, s, damoe.LAYOUT_ROWMAJOR),
+                     lambda: damoe.mxfp4_dequantise(c, s, T, K, t["x"], damoe.LAYOUT_ROWMAJOR),
+                     lambda: damoe.mxfp4_pack(c, s, T, K, _bytes(4352).cuda())):
+            with pytest.raises(ValueError, match="device"):
+                call()
+    torch.cuda.synchronize()
