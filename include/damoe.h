@@ -550,6 +550,16 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
                                 int32_t N, const void* add, int64_t ld_add, void* y, int32_t ydtype, int64_t ldy,
                                 void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* One of the calls with many arguments, for bindings to which each argument costs a conversion: its n arguments in order,
+ * each in 8 bytes (pointers and integers as int64, floats as double), are read before it returns.  The call's own
+ * status; DAMOE_ERR_INVALID_ARG for another number of words than it has arguments. */
+typedef enum damoe_call {
+  DAMOE_CALL_ROUTER_LOSS = 0,
+  DAMOE_CALL_ROUTER_LOSS_GRAD = 1,
+  DAMOE_CALL_MXFP4_LINEAR = 2
+} damoe_call;
+damoe_status damoe_call_words(int32_t call, const void* words /* host */, size_t n);
+
 /* Alg. 1 (Sec. III-A): the Dirichlet concentration alpha in [1e-6, 1e6] whose
  * mean Effective Experts over `samples` draws equals `target`, by bisection on
  * log(alpha) (at most `iters` halvings, stopping once the bracket is within a

@@ -216,3 +216,30 @@ def test_one_tensor_of_the_host_among_the_device_s():
             with pytest.raises(ValueError, match="device"):
                 call()
     torch.cuda.synchronize()
+
+
+def test_calls_by_words():
+    """damoe_call_words: the call's own status for its arguments in order, and a refusal of any other number of words."""
+    P, Q, big = 0x10000, 0x20000, 1 << 40  # never dereferenced: every call ends before a launch
+    call = damoe.lib().damoe_call_words
+    loss = [P, 1, 64, P, 0, 0, 8, 64, 4, 1, 0, 1.0, 0.0, P, P, 0, P, P, big, 0]
+    grad = [P, 1, 64, P, 0, 0, 0, 0, P, P, 8, 64, 4, 1, 0, 1.0, 0.0, 0, Q, 64, 0]
+    linear = [P, 0, 512, 4, 512, P, 64, 0, 0, Q, 0, 64, P, big, 0]
+    bad, unsupported, workspace = -1, -2, -3
+    # The position of an argument and a value that the call refuses there.
+    refusals = [
+        (0, damoe._LOSS_WORDS, loss, {bad: [(0, 0), (0, P + 2), (2, 63), (3, 0), (6, -1), (7, 0), (8, 17), (9, 2), (10, 2), (13, 0),
+                                            (14, 0), (16, 0), (17, 0), (17, P + 8)], unsupported: [(1, 2)], workspace: [(18, 255)]}),
+        (1, damoe._GRAD_WORDS, grad, {bad: [(0, 0), (2, 63), (4, P), (5, P), (8, 0), (9, 0), (10, -1), (11, 0), (12, 17), (13, 2),
+                                            (14, 2), (18, 0), (18, Q + 2), (19, 63)], unsupported: [(1, 2)]}),
+        (2, damoe._LINEAR_WORDS, linear, {bad: [(0, 0), (2, 511), (3, -1), (4, 0), (5, 0), (5, P + 8), (6, 0), (9, 0), (11, 63),
+                                                (12, 0), (12, P + 8)], unsupported: [(1, 2), (4, 48), (10, 2)], workspace: [(13, 0)]})]
+    for fn, pack, good, wrong in refusals:
+        for status, changes in wrong.items():
+            for i, v in changes:
+                words = pack(*good[:i], v, *good[i + 1:])
+                assert call(fn, words, len(good)) == status, (fn, i, v)
+        for n in (0, len(good) - 1, len(good) + 1):
+            assert call(fn, pack(*good), n) == bad
+        assert call(fn, None, len(good)) == bad
+    assert call(3, damoe._LINEAR_WORDS(*linear), 15) == call(-1, b"", 0) == bad
