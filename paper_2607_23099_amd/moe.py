@@ -115,13 +115,13 @@ class MxLinear:
     def __init__(self, weight, T_max: int):
         self.N, self.K = weight.shape
         self.T_max = T_max
-        n = damoe.mxfp4_bytes(self.N, self.K)
-        if n == 0:
-            raise ValueError("the weight's columns must be a multiple of 32")
+        n, ws = damoe.mxfp4_bytes(self.N, self.K), damoe.mxfp4_linear_workspace_size(T_max, self.N, self.K)
+        if n == 0 or ws == 0:
+            raise ValueError(f"no product of up to {T_max} tokens with {self.N} x {self.K} weights: the columns are a multiple of "
+                             "32, and an operand's tiles lie below 2^31 bytes")
         self.tiles = torch.empty(n, dtype=torch.uint8, device=weight.device)
         damoe.mxfp4_quantise(weight, self.N, self.K, self.tiles)
-        self.ws = torch.empty(damoe.mxfp4_linear_workspace_size(T_max, self.N, self.K), dtype=torch.uint8,
-                              device=weight.device)
+        self.ws = torch.empty(ws, dtype=torch.uint8, device=weight.device)
         torch.cuda.current_stream(weight.device).synchronize()
 
     def __call__(self, x, y=None, add=None, stream=None):

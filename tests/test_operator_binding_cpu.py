@@ -6,7 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2607_23099_amd import build, damoe
-from paper_2607_23099_amd.moe import Path
+from paper_2607_23099_amd.moe import MxLinear, Path
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -243,3 +243,13 @@ def test_calls_by_words():
             assert call(fn, pack(*good), n) == bad
         assert call(fn, None, len(good)) == bad
     assert call(3, damoe._LINEAR_WORDS(*linear), 15) == call(-1, b"", 0) == bad
+
+
+def test_products_that_the_library_does_not_have():
+    """Refused where the object is made, not at its first call."""
+    w = torch.zeros(64, 32, dtype=torch.bfloat16)
+    for weight, T_max in [(w, -1), (w, (1 << 20) + 1), (w[:, :24], 8), (w[:, :0], 8), (w[:0], 8),
+                          (w[:1].expand(1 << 20, 32).as_strided((1 << 20, 8192), (0, 0)), 8),  # 4.6 GB of tiles
+                          (w.as_strided((64, 8192), (0, 0)), 1 << 20), (w.as_strided(((1 << 20) + 1, 32), (0, 0)), 8)]:
+        with pytest.raises(ValueError, match="no product"):
+            MxLinear(weight, T_max)
