@@ -127,7 +127,10 @@ class MxLinear:
     def __call__(self, x, y=None, add=None, stream=None):
         """add + Q(x) W^T of the rows of x [T][K], into y (by default new, of add's or else x's type).  With `stream`, the
         product runs on it and a new y belongs to it, as if it were the current one: it waits for the inputs, and other
-        streams for y, by the caller."""
+        streams for y, by the caller.  The product has no gradient, so inputs that ask for one are refused outside of
+        torch.no_grad()."""
+        if (x.requires_grad or (add is not None and add.requires_grad)) and torch.is_grad_enabled():
+            raise ValueError("the product has no gradient: call it under torch.no_grad(), or with detached inputs")
         T = x.shape[0]
         if T > self.T_max:
             raise ValueError("more rows than T_max")

@@ -74,3 +74,15 @@ def test_weights_are_ready_for_every_stream(record):
     """A first call may come on any stream: the constructor ends when the tiles are there."""
     moe.MxLinear(torch.zeros(64, 32), 8)
     assert len(record["calls"]) == 1 and record["waited"] == 1
+
+
+def test_inputs_that_ask_for_a_gradient(record):
+    """It would be lost without a word."""
+    lin = moe.MxLinear(torch.zeros(64, 32, requires_grad=True), 8)  # a trained layer's weights are no input
+    x, add = torch.zeros(8, 32), torch.zeros(8, 64)
+    for kw in (dict(x=x.clone().requires_grad_()), dict(x=x, add=add.clone().requires_grad_())):
+        with pytest.raises(ValueError, match="gradient"):
+            lin(**kw)
+        with torch.no_grad():
+            assert not lin(**kw).requires_grad
+        lin(**{n: t.detach() for n, t in kw.items()})
