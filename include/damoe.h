@@ -542,8 +542,9 @@ damoe_status damoe_mxfp4_pack(const uint8_t* codes, const uint8_t* scales, int64
  *        nor ws
  *   ws   16-byte aligned, at least damoe_mxfp4_linear_workspace_size(T, N, K) bytes; nothing is kept in it.
  * Products and scales are exact (also where the two scales together leave fp32's range), sums fp32 in a fixed
- * order, subnormals kept, infinity past the range; a NaN block makes its row (x) or column (w) of y NaN.  T = 0 is a no-op; T <= DAMOE_MAX_T, N and K <= 2^20, and T ceil(K / 256) 136, N ceil(K / 256) 136
- * below 2^31 (32-bit offsets in an operand), else DAMOE_ERR_UNSUPPORTED.  Stream-ordered, capturable;
+ * order, subnormals kept, infinity past the range; a NaN block makes its row (x) or column (w) of y NaN.
+ * T = 0 is a no-op; T <= DAMOE_MAX_T, N and K <= 2^20, and T ceil(K / 256) 136, N ceil(K / 256) 136 below
+ * 2^31 (32-bit offsets in an operand), else DAMOE_ERR_UNSUPPORTED.  Stream-ordered, capturable;
  * concurrent calls need workspaces of their own, and so does every captured graph that may run beside another. */
 size_t damoe_mxfp4_linear_workspace_size(int32_t T_max, int32_t N, int32_t K);
 damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int32_t T, int32_t K, const uint8_t* w,
