@@ -34,9 +34,11 @@ constexpr int kGradThreads = 256;
 constexpr int kGradWaves = kGradThreads / kWave;
 
 // Up to kWaveTokens tokens, in sequences of up to kWaveMean in the mean, blocks are single waves of up to four tokens: a
-// block goes over its sequences in turn, 1.7 us each.  Waves / blocks of eight, all launches: 40 tokens in 28 sequences
-// 10.9 / 56 us, 512 in 512 (256 experts) 12.5 / 77, 512 in 8 12.1 / 12.9, 4096 in 64 12.8 / 12.8, one of 3969 tokens and
-// 127 of one 50 / 80; beyond, the slots of long sequences cost more (4096 in 2 15.6 / 13.1, 16384 in 512 19.4 / 15.4).
+// block of eight goes over its sequences in turn, 1.7 us each.  Waves / blocks of eight, all launches, 256 experts: 40 tokens
+// in 28 sequences 10.9 / 56 us, 512 in 512 12.5 / 77, 512 in 8 12.1 / 12.9, 4096 in 64 12.8 / 12.8, one of 3969 tokens and
+// 127 of one 50 / 80; the slots of long sequences cost more (4096 in 2 15.6 / 13.1).  The bound on the tokens is right for
+// means of 32 and more only: 16384 tokens in sequences of 1, 2, 4, 8, 32, 64 take 66 / 125, 40 / 69, 25 / 42, 21.5 / 25.6,
+// 18.8 / 14.2, 16.9 / 13.8 us, 65536 take 252 / 485, 122 / 241, 69 / 131, 49 / 74, 34 / 31, 33 / 27.
 constexpr int32_t kWaveTokens = 4096, kWaveMean = 64;
 
 bool by_waves(int32_t T, int32_t S) { return T <= kWaveTokens && T <= (int64_t)S * kWaveMean; }
