@@ -315,11 +315,9 @@ def _dtype(t) -> int:
     return _DTYPES.get(t.dtype, -1)
 
 
-def _ld(name: str, t, rows: int, cols: int, ld, dev: int) -> int:
+def _ld(name: str, t, rows: int, cols: int, ld) -> int:
     """Row stride of a matrix in elements: as given, the tensor's own (2-D), or `cols`.  The elements of a row
-    lie side by side and the tensor holds rows x cols of them on device number `dev`; any other is refused."""
-    if t.get_device() != dev:
-        _elsewhere(name, t)
+    lie side by side and the tensor holds rows x cols of them; any other is refused."""
     if ld is None:
         shape = t.shape
         if len(shape) == 2:
@@ -396,16 +394,21 @@ def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, se
     if not _DTYPES:
         _types()
     dt, dev = _DTYPES.get(logits.dtype, -1), logits.get_device()
-    p_ids, p_mask = _list("ids", ids, _INT32, T * k, dev), _list("mask", mask, _BYTES, T, dev)
-    p_off = _offsets(seq_offsets, S, dev)
-    n = S * E  # the outputs by _list's rules in one expression: a call for each takes 0.4 us more
-    if (loss is None or counts is None or tokens is None or not (
-            loss.dtype in _FLOAT32 and loss.numel() >= 3 and loss.is_contiguous() and loss.get_device() == dev
+    n = S * E  # the checks of _list and _offsets in one expression: their calls, which name what is wrong, take 0.6 us more
+    if not (loss is not None and counts is not None and tokens is not None
+            and (ids is None or ids.dtype in _INT32 and ids.numel() >= T * k and ids.is_contiguous() and ids.get_device() == dev)
+            and (mask is None or mask.dtype in _BYTES and mask.numel() >= T and mask.is_contiguous() and mask.get_device() == dev)
+            and (seq_offsets is None or seq_offsets.dtype in _INT32 and seq_offsets.numel() == S + 1
+                 and seq_offsets.is_contiguous() and seq_offsets.get_device() == dev)
+            and loss.dtype in _FLOAT32 and loss.numel() >= 3 and loss.is_contiguous() and loss.get_device() == dev
             and counts.dtype in _INT32 and counts.numel() >= n and counts.is_contiguous() and counts.get_device() == dev
             and tokens.dtype in _INT32 and tokens.numel() >= S + 2 and tokens.is_contiguous() and tokens.get_device() == dev
             and (probs is None or probs.dtype in _FLOAT32 and probs.numel() >= n and probs.is_contiguous()
                  and probs.get_device() == dev)
-            and ws.is_contiguous() and ws.get_device() == dev)):
+            and ws.is_contiguous() and ws.get_device() == dev):
+        _list("ids", ids, _INT32, T * k, dev)
+        _list("mask", mask, _BYTES, T, dev)
+        _offsets(seq_offsets, S, dev)
         # What the library refuses by itself is named as it does.
         if (ids is None and T > 0) or loss is None or counts is None or tokens is None:
             raise DamoeError("damoe_router_loss", -1)
@@ -416,9 +419,10 @@ def router_loss(logits, ids, T, E, k, loss, counts, tokens, ws, *, mask=None, se
             _list(name, t, types, m, dev)
         _room("ws", ws, 0, dev)
     rc = (_lib or lib()).damoe_call_words(0, _LOSS_WORDS(
-        logits.data_ptr(), dt, _ld("logits", logits, T, E, ld, dev), p_ids, p_mask, p_off, T, E, k, S, score, alpha, z_coef,
-        loss.data_ptr(), counts.data_ptr(), 0 if probs is None else probs.data_ptr(), tokens.data_ptr(), ws.data_ptr(), ws.nbytes,
-        _stream_on("damoe_router_loss", stream, dev, dt)), 20)
+        logits.data_ptr(), dt, _ld("logits", logits, T, E, ld), 0 if ids is None else ids.data_ptr(),
+        0 if mask is None else mask.data_ptr(), 0 if seq_offsets is None else seq_offsets.data_ptr(), T, E, k, S, score, alpha,
+        z_coef, loss.data_ptr(), counts.data_ptr(), 0 if probs is None else probs.data_ptr(), tokens.data_ptr(), ws.data_ptr(),
+        ws.nbytes, _stream_on("damoe_router_loss", stream, dev, dt)), 20)
     if rc:
         raise DamoeError("damoe_router_loss", rc)
 
@@ -433,6 +437,8 @@ def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None
         raise ValueError("dlogits has the logits' type")
     dt, dev = _DTYPES.get(logits.dtype, -1), logits.get_device()
     p_ids, p_mask = _list("ids", ids, _INT32, T * k, dev), _list("mask", mask, _BYTES, T, dev)
+    if dlogits.get_device() != dev:
+        _elsewhere("dlogits", dlogits)
     p_off, p_dloss = _offsets(seq_offsets, S, dev), _list("dloss", dloss, _FLOAT32, 1, dev)
     p_w, p_dw = _list("w", w, _FLOAT32, T * k, dev), _list("dw", dw, _FLOAT32, T * k, dev)
     if T > 0:
@@ -440,8 +446,8 @@ def router_loss_grad(logits, ids, T, E, k, counts, tokens, dlogits, *, mask=None
     else:  # without tokens neither is read
         p_counts, p_tokens = _p(counts), _p(tokens)
     rc = (_lib or lib()).damoe_call_words(1, _GRAD_WORDS(
-        logits.data_ptr(), dt, _ld("logits", logits, T, E, ld, dev), p_ids, p_w, p_dw, p_mask, p_off, p_counts, p_tokens, T,
-        E, k, S, score, alpha, z_coef, p_dloss, dlogits.data_ptr(), _ld("dlogits", dlogits, T, E, ldd, dev),
+        logits.data_ptr(), dt, _ld("logits", logits, T, E, ld), p_ids, p_w, p_dw, p_mask, p_off, p_counts, p_tokens, T,
+        E, k, S, score, alpha, z_coef, p_dloss, dlogits.data_ptr(), _ld("dlogits", dlogits, T, E, ldd),
         _stream_on("damoe_router_loss_grad", stream, dev, dt, T)), 21)
     if rc:
         raise DamoeError("damoe_router_loss_grad", rc)
@@ -463,7 +469,7 @@ def mxfp4_quantise(x, rows, cols, codes, scales=None, layout=LAYOUT_TILE32, ldx=
     dt, dev = _dtype(x), x.get_device()
     p_codes = _room("codes", codes, _codes_bytes(rows, cols, layout), dev)
     p_scales = _room("scales", scales, rows * cols // 32, dev) if layout == LAYOUT_ROWMAJOR else 0
-    rc = (_lib or lib()).damoe_mxfp4_quantise(x.data_ptr(), dt, rows, cols, _ld("x", x, rows, cols, ldx, dev), layout, p_codes,
+    rc = (_lib or lib()).damoe_mxfp4_quantise(x.data_ptr(), dt, rows, cols, _ld("x", x, rows, cols, ldx), layout, p_codes,
                                               p_scales, _stream_on("damoe_mxfp4_quantise", stream, dev, dt, rows))
     if rc:
         raise DamoeError("damoe_mxfp4_quantise", rc)
@@ -474,7 +480,7 @@ def mxfp4_dequantise(codes, scales, rows, cols, x, layout=LAYOUT_TILE32, ldx=Non
     p_codes = _room("codes", codes, _codes_bytes(rows, cols, layout), dev)
     p_scales = _room("scales", scales, rows * cols // 32, dev) if layout == LAYOUT_ROWMAJOR else 0
     rc = (_lib or lib()).damoe_mxfp4_dequantise(p_codes, p_scales, rows, cols, layout, x.data_ptr(), dt,
-                                                _ld("x", x, rows, cols, ldx, dev),
+                                                _ld("x", x, rows, cols, ldx),
                                                 _stream_on("damoe_mxfp4_dequantise", stream, dev, dt, rows))
     if rc:
         raise DamoeError("damoe_mxfp4_dequantise", rc)
@@ -499,11 +505,15 @@ def mxfp4_linear(x, T, K, w_tiles, N, y, ws, add=None, ldx=None, ldy=None, ld_ad
     if add is not None and add.dtype != y.dtype:
         raise ValueError("add has y's type")
     dt, dev = _dtype(x), x.get_device()
+    if y.get_device() != dev:
+        _elsewhere("y", y)
+    if add is not None and add.get_device() != dev:
+        _elsewhere("add", add)
     p_tiles = _room("w_tiles", w_tiles, _codes_bytes(N, K, LAYOUT_TILE32), dev)
-    p_add, lda = (0, 0) if add is None else (add.data_ptr(), _ld("add", add, T, N, ld_add, dev))
+    p_add, lda = (0, 0) if add is None else (add.data_ptr(), _ld("add", add, T, N, ld_add))
     rc = (_lib or lib()).damoe_call_words(2, _LINEAR_WORDS(
-        x.data_ptr(), dt, _ld("x", x, T, K, ldx, dev), T, K, p_tiles, N, p_add, lda, y.data_ptr(), _dtype(y),
-        _ld("y", y, T, N, ldy, dev), _room("ws", ws, 0, dev), ws.nbytes, _stream_on("damoe_mxfp4_linear", stream, dev, dt, T)), 15)
+        x.data_ptr(), dt, _ld("x", x, T, K, ldx), T, K, p_tiles, N, p_add, lda, y.data_ptr(), _dtype(y),
+        _ld("y", y, T, N, ldy), _room("ws", ws, 0, dev), ws.nbytes, _stream_on("damoe_mxfp4_linear", stream, dev, dt, T)), 15)
     if rc:
         raise DamoeError("damoe_mxfp4_linear", rc)
 

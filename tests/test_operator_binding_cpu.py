@@ -117,15 +117,15 @@ def test_matrices_that_do_not_hold_the_rows():
 def test_row_strides_that_the_binding_takes():
     """What holds the rows is taken, whatever its form: the stride that the library is given."""
     x = torch.zeros(6, 40)
-    assert damoe._ld("x", x, 6, 40, None, -1) == 40 and damoe._ld("x", x, 5, 32, None, -1) == 40
-    assert damoe._ld("x", x[:, 3:35], 6, 32, None, -1) == 40 and damoe._ld("x", x[::2], 3, 40, None, -1) == 80
-    assert damoe._ld("x", x[2:3, :32], 1, 32, None, -1) >= 32  # of one row, any
-    assert damoe._ld("x", x[:, :1], 6, 1, None, -1) == 40
-    assert damoe._ld("x", x.view(-1), 6, 40, None, -1) == 40 and damoe._ld("x", x.view(2, 3, 40), 6, 40, None, -1) == 40
-    assert damoe._ld("x", x.view(-1)[3:], 5, 32, 40, -1) == 40 and damoe._ld("x", x[:, 3:35], 6, 32, 40, -1) == 40
-    assert damoe._ld("x", x[1:], 5, 40, 40, -1) == 40 and damoe._ld("x", x[:0], 0, 40, None, -1) == 40
-    assert damoe._ld("x", x[:0].view(-1), 0, 40, 40, -1) == 40
-    assert damoe._ld("x", x[:1].expand(6, 40), 6, 40, None, -1) == 0  # refused by the library: a stride below the columns
+    assert damoe._ld("x", x, 6, 40, None) == 40 and damoe._ld("x", x, 5, 32, None) == 40
+    assert damoe._ld("x", x[:, 3:35], 6, 32, None) == 40 and damoe._ld("x", x[::2], 3, 40, None) == 80
+    assert damoe._ld("x", x[2:3, :32], 1, 32, None) >= 32  # of one row, any
+    assert damoe._ld("x", x[:, :1], 6, 1, None) == 40
+    assert damoe._ld("x", x.view(-1), 6, 40, None) == 40 and damoe._ld("x", x.view(2, 3, 40), 6, 40, None) == 40
+    assert damoe._ld("x", x.view(-1)[3:], 5, 32, 40) == 40 and damoe._ld("x", x[:, 3:35], 6, 32, 40) == 40
+    assert damoe._ld("x", x[1:], 5, 40, 40) == 40 and damoe._ld("x", x[:0], 0, 40, None) == 40
+    assert damoe._ld("x", x[:0].view(-1), 0, 40, 40) == 40
+    assert damoe._ld("x", x[:1].expand(6, 40), 6, 40, None) == 0  # refused by the library: a stride below the columns
 
 
 def test_buffers_that_do_not_hold_the_codes():
