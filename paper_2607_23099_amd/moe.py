@@ -232,7 +232,8 @@ class Path:
                      self.w, self.router_ws, stream)
 
     def prepare_loss(self, S: int = 1):
-        """Buffers of router_loss and router_loss_grad for batches of S sequences (allocates; call it once)."""
+        """Buffers of router_loss and router_loss_grad for batches of S sequences (allocates; call it once).  It waits until
+        they are cleared, so the first call may come on any stream."""
         sh, dev = self.dl.shape, self.logits.device
         self.loss_S = S
         self.loss = torch.zeros(3, device=dev)
@@ -241,6 +242,7 @@ class Path:
         self.loss_tokens = torch.zeros(S + 2, dtype=torch.int32, device=dev)
         self.loss_ws = torch.zeros(damoe.router_loss_workspace_size(self.T_max, sh.E, S), dtype=torch.uint8, device=dev)
         self.dlogits = torch.zeros_like(self.logits)
+        torch.cuda.current_stream(dev).synchronize()
 
     def _need_loss(self, T: int):
         if not self.loss_S:

@@ -86,3 +86,18 @@ def test_inputs_that_ask_for_a_gradient(record):
         with torch.no_grad():
             assert not lin(**kw).requires_grad
         lin(**{n: t.detach() for n, t in kw.items()})
+
+
+def _path(T_max=8, E=64):
+    path = moe.Path.__new__(moe.Path)
+    path.dl = type("Layer", (), {"shape": synth.Shape("streams", E=E, k=4, H=128, I=128, shape_id=9)})
+    path.T_max, path.loss_S, path.logits = T_max, 0, torch.zeros(T_max, E)
+    return path
+
+
+def test_loss_buffers_are_ready_for_every_stream(record):
+    """Clearing them late would wipe the results of a first call on another stream."""
+    path = _path()
+    path.prepare_loss(S=3)
+    assert record["waited"] == 1 and path.loss_S == 3
+    assert path.loss_counts.shape == (3, 64) and path.loss_tokens.shape == (5,)
