@@ -235,12 +235,15 @@ class Path:
         """Buffers of router_loss and router_loss_grad for batches of S sequences (allocates; call it once).  It waits until
         they are cleared, so the first call may come on any stream."""
         sh, dev = self.dl.shape, self.logits.device
+        ws = damoe.router_loss_workspace_size(self.T_max, sh.E, S)
+        if ws == 0:
+            raise ValueError(f"no loss of up to {self.T_max} tokens in {S} sequences")
         self.loss_S = S
         self.loss = torch.zeros(3, device=dev)
         self.loss_counts = torch.zeros((S, sh.E), dtype=torch.int32, device=dev)
         self.loss_probs = torch.zeros((S, sh.E), device=dev)
         self.loss_tokens = torch.zeros(S + 2, dtype=torch.int32, device=dev)
-        self.loss_ws = torch.zeros(damoe.router_loss_workspace_size(self.T_max, sh.E, S), dtype=torch.uint8, device=dev)
+        self.loss_ws = torch.zeros(ws, dtype=torch.uint8, device=dev)
         self.dlogits = torch.zeros_like(self.logits)
         torch.cuda.current_stream(dev).synchronize()
 

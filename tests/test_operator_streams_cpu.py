@@ -101,3 +101,11 @@ def test_loss_buffers_are_ready_for_every_stream(record):
     path.prepare_loss(S=3)
     assert record["waited"] == 1 and path.loss_S == 3
     assert path.loss_counts.shape == (3, 64) and path.loss_tokens.shape == (5,)
+
+
+@pytest.mark.parametrize("S", [0, -1, (1 << 20) + 1])
+def test_loss_of_a_number_of_sequences_that_the_library_does_not_take(record, S):
+    path = _path()
+    with pytest.raises(ValueError, match="sequences"):
+        path.prepare_loss(S)
+    assert path.loss_S == 0
