@@ -65,3 +65,30 @@ def test_a_layer_quantised_on_a_side_stream():
         assert _owner(torch, t) == side.cuda_stream
         assert torch.equal(t, want.w[n])
     assert got.layer.layout == damoe.LAYOUT_FRAG16
+
+
+def test_products_captured_with_results_of_their_own():
+    """A shared expert whose results the captured calls allocate, replayed among eager calls of the same objects, and calls
+    without rows."""
+    torch = torch_cuda()
+    from paper_2607_23099_amd.moe import MxLinear
+    g = torch.Generator().manual_seed(3)
+    T, H, I = 40, 512, 256
+    up = MxLinear((torch.randn((I, H), generator=g) / H ** 0.5).cuda(), T)
+    down = MxLinear((torch.randn((H, I), generator=g) / I ** 0.5).cuda(), T)
+    xs = [torch.randn((T, H), generator=g).to(torch.bfloat16).cuda() for _ in range(3)]
+    want = [down(up(x)) for x in xs]
+    for lin, n in ((up, I), (down, H)):
+        assert lin(torch.zeros((0, lin.K), dtype=torch.bfloat16, device="cuda")).shape == (0, n)
+    x = xs[0].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = down(up(x))
+    for rep in range(4):
+        x.copy_(xs[rep % 3])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[rep % 3]), rep
+        assert torch.equal(down(up(xs[0])), want[0])
+        torch.cuda.synchronize()

@@ -1,11 +1,18 @@
 """Which stream owns the memory that MxLinear and quantise_layer allocate (no GPU: the library's calls are recorded)."""
 import contextlib
+import os
 
 import pytest
 
 torch = pytest.importorskip("torch")
 
-from paper_2607_23099_amd import damoe, moe, synth
+from paper_2607_23099_amd import build, damoe, moe, synth
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(damoe.LIB_PATH):
+        build.build_damoe()
 
 
 class Side:
