@@ -23,6 +23,10 @@
  *   damoe_mxfp4_quantise   bf16 or fp32 rows to MXFP4, in the expert layer's layouts
  *                          or as an operand of damoe_mxfp4_linear, the product of
  *                          MXFP4 weights with activations quantised in the call
+ *   damoe_sort_rows        rows sorted by expert, and back with the gates applied
+ *                          (damoe_combine_rows) with that sum's gradient
+ *   damoe_adapters         low-rank adapters of many segments of rows beside a shared
+ *                          product; their gradient: damoe_adapters_grad
  *   damoe_tune             offline auto-tuning: Alg. 1, ddist:X sweep,
  *                          benchmark every variant, exemplar centroids
  *                          (Sec. III-A, IV-A)
@@ -72,6 +76,8 @@ typedef enum damoe_status {
 #define DAMOE_MAX_E 1024       /* experts                                  */
 #define DAMOE_MAX_K 16         /* experts per token                        */
 #define DAMOE_MAX_T (1 << 20)  /* tokens per call                          */
+#define DAMOE_MAX_RANK 128     /* rank of an adapter                       */
+#define DAMOE_MAX_COLS (1 << 20) /* columns of sorted rows, of adapters    */
 #define DAMOE_N_TILE_SIZES 5   /* token-tile sizes BM: 16, 32, 64, 128, 256 */
 
 /* Device error codes (sticky, in the workspace). */
@@ -551,13 +557,85 @@ damoe_status damoe_mxfp4_linear(const void* x, int32_t xdtype, int64_t ldx, int3
                                 int32_t N, const void* add, int64_t ld_add, void* y, int32_t ydtype, int64_t ldy,
                                 void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* Rows sorted by expert and back, for expert layers made of other products than damoe_fused_moe's, and for training.
+ * Slot j of token t has the place q = inv_perm[t k + j] of damoe_route_histogram.  A place outside [0, R) is a slot without
+ * a row (-1: masked or dropped): it is neither read nor written and adds nothing.  Other places are distinct.
+ *   x, add, y, dy       bf16 or fp32 (dtype) [T][ld], ld >= H
+ *   rows, drows         of the same type, [R][ld]; rows that no slot has are left as they were
+ *   w                   fp32 [T][k], or NULL: every gate is 1
+ * Row strides are in elements, any alignment of the element.  Sums are fp32 in the slots' order, results rounded once.
+ * A call touches H columns of a row and leaves the others.  H <= DAMOE_MAX_COLS.  T = 0 is a no-op.  Stream-ordered, no
+ * workspace, capturable.
+ *
+ *   damoe_sort_rows          rows[q] = w_tj x[t].  rows does not overlap x
+ *   damoe_combine_rows       y[t] = add[t] + sum_j w_tj rows[q]: with w = 1, sort_rows's gradient.  add may be NULL (0) or y
+ *                            itself (ld_add = ldy); y overlaps neither rows nor else add
+ *   damoe_combine_rows_grad  drows[q] = w_tj dy[t] and dw[t][j] = sum_h dy[t][h] rows[q][h] (0 for a slot without a row).
+ *                            Either output may be NULL (without dw, rows is not read); drows may be rows itself
+ *                            (ld_drows = ld_rows) and else overlaps neither rows nor dy.  The dw of sort_rows is the same
+ *                            call with x as dy and the gradient of its rows as rows */
+damoe_status damoe_sort_rows(const void* x, int32_t dtype, int64_t ldx, const float* w, const int32_t* inv_perm, int32_t T,
+                             int32_t k, int32_t H, int32_t R, void* rows, int64_t ld_rows, hipStream_t stream);
+damoe_status damoe_combine_rows(const void* rows, int32_t dtype, int64_t ld_rows, const float* w, const int32_t* inv_perm,
+                                int32_t T, int32_t k, int32_t H, int32_t R, const void* add, int64_t ld_add, void* y,
+                                int64_t ldy, hipStream_t stream);
+damoe_status damoe_combine_rows_grad(const void* dy, int32_t dtype, int64_t ldy, const void* rows, int64_t ld_rows,
+                                     const float* w, const int32_t* inv_perm, int32_t T, int32_t k, int32_t H, int32_t R,
+                                     void* drows, int64_t ld_drows, float* dw, hipStream_t stream);
+
+/* Low-rank adapters: segment l, the places [offsets[l], offsets[l + 1]), has the pair A_l, B_l and the factor s_l; place p
+ * holds the row t = perm[p].  With offsets and perm of damoe_route_histogram (k = 1, ids the tokens' adapters, negative:
+ * none) rows come in any order: adapters of many requests beside a shared product.  With the experts' offsets and
+ * perm = NULL (place p is row p) the rows of damoe_sort_rows have an adapter for each expert.
+ *   u[p] = A_l x[t]     y[t] = add[t] + s_l B_l u[p]
+ *   x        bf16 or fp32 (xdtype) [T][ldx], ldx >= K
+ *   offsets  int32 [L + 1], non-decreasing, from 0 to at most T (otherwise the results are unspecified)
+ *   perm     int32 [T], or NULL; distinct rows in [0, T) (another entry's place is left out)
+ *   a, b     bf16 or fp32 (wdtype) [L][r][K] and [L][N][r], any alignment of the element; 1 <= r <= DAMOE_MAX_RANK
+ *   scale    fp32 [L], or NULL: 1
+ *   add      NULL (0), or [T][ld_add] of y's type; it may be y itself (ld_add = ldy)
+ *   y        bf16 or fp32 (ydtype) [T][ldy], ldy >= N; rows in no segment, and columns past N, are left as they were.
+ *            Overlaps neither x, a, b nor else add
+ *   u        NULL, or fp32 [T][r] output, by places, for the gradient; places in no segment are left as they were
+ *   ws       16-byte aligned, at least damoe_adapters_workspace_size(T, L, r, K, N) bytes; nothing is kept in it
+ * Products are exact and sums fp32 in a fixed order, u is not rounded between them, y once.  A value that is not finite
+ * makes what it enters not finite, of its own rows and its own segment only.  L <= DAMOE_MAX_E, K and N <= DAMOE_MAX_COLS,
+ * T <= DAMOE_MAX_T.  T = 0 is a no-op.  Stream-ordered, allocates nothing, capturable; concurrent calls need workspaces
+ * of their own, and so does every captured graph that may run beside another. */
+size_t damoe_adapters_workspace_size(int32_t T_max, int32_t L, int32_t r, int32_t K, int32_t N);
+damoe_status damoe_adapters(const void* x, int32_t xdtype, int64_t ldx, const int32_t* perm, const int32_t* offsets,
+                            int32_t T, int32_t L, const void* a, const void* b, int32_t wdtype, int32_t r, int32_t K,
+                            int32_t N, const float* scale, const void* add, int64_t ld_add, void* y, int32_t ydtype,
+                            int64_t ldy, float* u, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradient of damoe_adapters (same x, perm, offsets, a, b, scale; u is its output) for dy, of y's type [T][ldy]:
+ *   g[p] = s_l B_l^T dy[t]     dx[t] = add[t] + A_l^T g[p]     da_l = sum_p g[p] x[t]^T     db_l = s_l sum_p dy[t] u[p]^T
+ *   add      NULL (0), or [T][ld_add] of x's type: the gradient that x has from elsewhere; it may be dx itself
+ *            (ld_add = ld_dx).  (add has none but dy, and the factors s_l are constants.)
+ *   dx       NULL, or of x's type [T][ld_dx], ld_dx >= K; rows in no segment are left as they were.  Overlaps neither x, dy,
+ *            a, b nor else add
+ *   da, db   fp32 [L][r][K] and [L][N][r]; of a segment without rows 0.  accumulate = 1 adds to what they hold
+ *   ws       as above, damoe_adapters_grad_workspace_size bytes
+ * Sums are fp32 in a fixed order.  With T = 0 da and db are 0 (accumulate = 1: a no-op). */
+size_t damoe_adapters_grad_workspace_size(int32_t T_max, int32_t L, int32_t r, int32_t K, int32_t N);
+damoe_status damoe_adapters_grad(const void* x, int32_t xdtype, int64_t ldx, const void* dy, int32_t ydtype, int64_t ldy,
+                                 const float* u, const int32_t* perm, const int32_t* offsets, int32_t T, int32_t L,
+                                 const void* a, const void* b, int32_t wdtype, int32_t r, int32_t K, int32_t N,
+                                 const float* scale, const void* add, int64_t ld_add, void* dx, int64_t ld_dx, float* da,
+                                 float* db, int32_t accumulate, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* One of the calls with many arguments, for bindings to which each argument costs a conversion: its n arguments in order,
  * each in 8 bytes (pointers and integers as int64, floats as double), are read before it returns.  The call's own
  * status; DAMOE_ERR_INVALID_ARG for another number of words than it has arguments. */
 typedef enum damoe_call {
   DAMOE_CALL_ROUTER_LOSS = 0,
   DAMOE_CALL_ROUTER_LOSS_GRAD = 1,
-  DAMOE_CALL_MXFP4_LINEAR = 2
+  DAMOE_CALL_MXFP4_LINEAR = 2,
+  DAMOE_CALL_SORT_ROWS = 3,
+  DAMOE_CALL_COMBINE_ROWS = 4,
+  DAMOE_CALL_COMBINE_ROWS_GRAD = 5,
+  DAMOE_CALL_ADAPTERS = 6,
+  DAMOE_CALL_ADAPTERS_GRAD = 7
 } damoe_call;
 damoe_status damoe_call_words(int32_t call, const void* words /* host */, size_t n);
 

@@ -1,0 +1,261 @@
+// Rows sorted by expert and back: damoe_sort_rows, damoe_combine_rows and the gradient of the latter.
+//
+// With q(t, j) = inv_perm[t k + j] the place of slot j of token t:
+//   sort     rows[q(t, j)] = w_tj x_t          combine     y_t = add_t + sum_j w_tj rows[q(t, j)]
+//   combine's gradient: drows[q(t, j)] = w_tj dy_t, dw_tj = <dy_t, rows[q(t, j)]>
+// Each is memory bound: a few operations for 16 bytes.  All of them go by tokens, so that the token's side (x, y, dy) is
+// read or written once and only the sorted side k times, and so that no two waves touch one element.
+#include "vec.h"
+
+namespace damoe {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+
+struct RowArgs {
+  const void* x;  // the token's side: x, add or dy
+  int64_t ldx;
+  const float* w;
+  const int32_t* inv_perm;
+  void* rows;     // the sorted side
+  int64_t ldr;
+  void* out;      // y or drows
+  int64_t ldo;
+  float* dw;
+  int32_t T, k, H, R;
+  int32_t chunks;  // pieces of 64 x 16 bytes of a row
+};
+
+// The token's slots, one a lane: place (-1 where there is none) and factor.
+struct Slots {
+  int place = -1;
+  float factor = 1.f;
+
+  __device__ __forceinline__ Slots(const RowArgs& a, int64_t t, int lane) {
+    if (lane < a.k) {
+      place = a.inv_perm[t * a.k + lane];
+      if (a.w) factor = a.w[t * a.k + lane];
+      if ((uint32_t)place >= (uint32_t)a.R) place = -1;
+    }
+  }
+  __device__ __forceinline__ int at(int j) const { return __builtin_amdgcn_readlane(place, j); }
+  __device__ __forceinline__ float weight(int j) const {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, factor), j));
+  }
+};
+
+// A wave's piece of work: 64 x 16 bytes of a token's row.
+template <class F>
+__device__ __forceinline__ void by_pieces(const RowArgs& a, F f) {
+  const int64_t n = (int64_t)a.T * a.chunks, stride = (int64_t)gridDim.x * kWaves;
+  int64_t i = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (; i < n; i += stride) {
+    const int64_t t = i / a.chunks;
+    f(t, (int)(i - t * a.chunks));
+  }
+}
+
+template <bool BF>
+__device__ __forceinline__ uint4 scaled(uint4 v, float w) {
+  float f[Elem<BF>::kPer16];
+  unpack16<BF>(v, f);
+#pragma unroll
+  for (float& e : f) e *= w;
+  return pack16<BF>(f);
+}
+
+template <bool BF>
+__global__ void __launch_bounds__(kThreads) k_sort_rows(RowArgs a) {
+  typedef typename Elem<BF>::T T;
+  const int lane = threadIdx.x & 63;
+  by_pieces(a, [&](int64_t t, int chunk) {
+    const Slots s(a, t, lane);
+    const int c = (chunk * kWave + lane) * Elem<BF>::kPer16, n = a.H - c;
+    if (n <= 0) return;
+    const uint4 v = load_some<BF>(static_cast<const T*>(a.x) + t * a.ldx + c, n);
+    for (int j = 0; j < a.k; ++j) {
+      const int q = s.at(j);
+      if (q < 0) continue;
+      store_some<BF>(static_cast<T*>(a.rows) + (int64_t)q * a.ldr + c, n, a.w ? scaled<BF>(v, s.weight(j)) : v);
+    }
+  });
+}
+
+// Slots in order, in fp32; one rounding at the end.
+template <bool BF>
+__global__ void __launch_bounds__(kThreads) k_combine_rows(RowArgs a) {
+  typedef typename Elem<BF>::T T;
+  constexpr int P = Elem<BF>::kPer16;
+  const int lane = threadIdx.x & 63;
+  by_pieces(a, [&](int64_t t, int chunk) {
+    const Slots s(a, t, lane);
+    const int c = (chunk * kWave + lane) * P, n = a.H - c;
+    if (n <= 0) return;
+    uint4 v[DAMOE_MAX_K];
+#pragma unroll
+    for (int j = 0; j < DAMOE_MAX_K; ++j) {
+      if (j < a.k && s.at(j) >= 0) v[j] = load_some<BF>(static_cast<const T*>(a.rows) + (int64_t)s.at(j) * a.ldr + c, n);
+    }
+    float sum[P] = {};
+    if (a.x) unpack16<BF>(load_some<BF>(static_cast<const T*>(a.x) + t * a.ldx + c, n), sum);
+#pragma unroll
+    for (int j = 0; j < DAMOE_MAX_K; ++j) {
+      if (j >= a.k || s.at(j) < 0) continue;
+      float f[P];
+      unpack16<BF>(v[j], f);
+      const float w = s.weight(j);
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum[i] = fmaf(w, f[i], sum[i]);
+    }
+    store_some<BF>(static_cast<T*>(a.out) + t * a.ldo + c, n, pack16<BF>(sum));
+  });
+}
+
+// A block takes `per` slots of a token over its whole row: each lane's products in fp32, then the wave's lanes by
+// exchanges, then the waves in order.
+template <bool BF>
+__global__ void __launch_bounds__(kThreads) k_combine_rows_grad(RowArgs a, int32_t per) {
+  typedef typename Elem<BF>::T T;
+  constexpr int P = Elem<BF>::kPer16;
+  __shared__ float part[kWaves][DAMOE_MAX_K];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (a.k + per - 1) / per;
+  for (int64_t b = blockIdx.x; b < (int64_t)a.T * groups; b += gridDim.x) {
+    const int64_t t = b / groups;
+    const int j0 = (int)(b - t * groups) * per, n_j = min(per, a.k - j0);
+    const Slots s(a, t, lane);
+    float acc[DAMOE_MAX_K] = {};
+    for (int chunk = wave; chunk < a.chunks; chunk += kWaves) {
+      const int c = (chunk * kWave + lane) * P, n = a.H - c;
+      if (n <= 0) continue;
+      const uint4 d = load_some<BF>(static_cast<const T*>(a.x) + t * a.ldx + c, n);
+      uint4 v[DAMOE_MAX_K];
+      if (a.dw) {
+#pragma unroll
+        for (int j = 0; j < DAMOE_MAX_K; ++j) {
+          if (j < n_j && s.at(j0 + j) >= 0)
+            v[j] = load_some<BF>(static_cast<const T*>(a.rows) + (int64_t)s.at(j0 + j) * a.ldr + c, n);
+        }
+      }
+      float f[P];
+      unpack16<BF>(d, f);
+#pragma unroll
+      for (int j = 0; j < DAMOE_MAX_K; ++j) {
+        if (j >= n_j || s.at(j0 + j) < 0) continue;
+        if (a.dw) {
+          float g[P];
+          unpack16<BF>(v[j], g);
+#pragma unroll
+          for (int i = 0; i < P; ++i) acc[j] = fmaf(f[i], g[i], acc[j]);
+        }
+        if (a.out) {
+          const int64_t at = (int64_t)s.at(j0 + j) * a.ldo + c;
+          store_some<BF>(static_cast<T*>(a.out) + at, n, a.w ? scaled<BF>(d, s.weight(j0 + j)) : d);
+        }
+      }
+    }
+    if (!a.dw) continue;
+#pragma unroll
+    for (int j = 0; j < DAMOE_MAX_K; ++j) {
+      if (j >= n_j) continue;
+      float v = acc[j];
+#pragma unroll
+      for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+      if (lane == 0) part[wave][j] = v;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < n_j) {
+      float v = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) v += part[i][threadIdx.x];
+      a.dw[t * a.k + j0 + threadIdx.x] = v;
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- launches
+
+// Blocks of a launch at most; beyond them they go on in strides.
+constexpr int64_t kMaxBlocks = 1 << 22;
+
+bool shape_ok(int32_t T, int32_t k, int32_t H, int32_t R) {
+  return T >= 0 && T <= DAMOE_MAX_T && k >= 1 && k <= DAMOE_MAX_K && H >= 1 && R >= 0;
+}
+
+damoe_status check(int32_t T, int32_t k, int32_t H, int32_t R, int32_t dtype) {
+  if (!shape_ok(T, k, H, R)) return DAMOE_ERR_INVALID_ARG;
+  if (dtype != DAMOE_BF16 && dtype != DAMOE_F32) return DAMOE_ERR_UNSUPPORTED;
+  return H > DAMOE_MAX_COLS ? DAMOE_ERR_UNSUPPORTED : DAMOE_OK;
+}
+
+// A matrix whose rows are at least as long as the call's, at its element's alignment.
+bool matrix_ok(const void* p, int64_t ld, int32_t H, int32_t dtype) {
+  return p && ld >= H && reinterpret_cast<uintptr_t>(p) % (dtype == DAMOE_BF16 ? 2 : 4) == 0;
+}
+
+bool words_ok(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+int32_t chunks_of(int32_t H, int32_t dtype) {
+  const int32_t n = kWave * (dtype == DAMOE_BF16 ? 8 : 4);
+  return (H + n - 1) / n;
+}
+
+unsigned blocks_for(int64_t n) { return (unsigned)std::max<int64_t>(1, std::min(kMaxBlocks, n)); }
+
+damoe_status last() { return hipGetLastError() == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP; }
+
+}  // namespace
+}  // namespace damoe
+
+using namespace damoe;
+
+extern "C" {
+
+damoe_status damoe_sort_rows(const void* x, int32_t dtype, int64_t ldx, const float* w, const int32_t* inv_perm, int32_t T,
+                             int32_t k, int32_t H, int32_t R, void* rows, int64_t ld_rows, hipStream_t stream) {
+  if (const damoe_status s = check(T, k, H, R, dtype)) return s;
+  if (T == 0 || R == 0) return DAMOE_OK;
+  if (!matrix_ok(x, ldx, H, dtype) || !matrix_ok(rows, ld_rows, H, dtype) || !inv_perm || !words_ok(inv_perm) || !words_ok(w))
+    return DAMOE_ERR_INVALID_ARG;
+  RowArgs a{x, ldx, w, inv_perm, rows, ld_rows, nullptr, 0, nullptr, T, k, H, R, chunks_of(H, dtype)};
+  const dim3 grid(blocks_for(((int64_t)T * a.chunks + kWaves - 1) / kWaves));
+  if (dtype == DAMOE_BF16) hipLaunchKernelGGL(k_sort_rows<true>, grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL(k_sort_rows<false>, grid, dim3(kThreads), 0, stream, a);
+  return last();
+}
+
+damoe_status damoe_combine_rows(const void* rows, int32_t dtype, int64_t ld_rows, const float* w, const int32_t* inv_perm,
+                                int32_t T, int32_t k, int32_t H, int32_t R, const void* add, int64_t ld_add, void* y, int64_t ldy,
+                                hipStream_t stream) {
+  if (const damoe_status s = check(T, k, H, R, dtype)) return s;
+  if (T == 0) return DAMOE_OK;
+  if ((R > 0 && !matrix_ok(rows, ld_rows, H, dtype)) || !matrix_ok(y, ldy, H, dtype) || (add && !matrix_ok(add, ld_add, H, dtype)) ||
+      (add == y && ld_add != ldy) || !inv_perm || !words_ok(inv_perm) || !words_ok(w))
+    return DAMOE_ERR_INVALID_ARG;
+  RowArgs a{add, ld_add, w, inv_perm, const_cast<void*>(rows), ld_rows, y, ldy, nullptr, T, k, H, R, chunks_of(H, dtype)};
+  const dim3 grid(blocks_for(((int64_t)T * a.chunks + kWaves - 1) / kWaves));
+  if (dtype == DAMOE_BF16) hipLaunchKernelGGL(k_combine_rows<true>, grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL(k_combine_rows<false>, grid, dim3(kThreads), 0, stream, a);
+  return last();
+}
+
+damoe_status damoe_combine_rows_grad(const void* dy, int32_t dtype, int64_t ldy, const void* rows, int64_t ld_rows, const float* w,
+                                     const int32_t* inv_perm, int32_t T, int32_t k, int32_t H, int32_t R, void* drows,
+                                     int64_t ld_drows, float* dw, hipStream_t stream) {
+  if (const damoe_status s = check(T, k, H, R, dtype)) return s;
+  if (T == 0 || (!drows && !dw)) return DAMOE_OK;
+  if (!matrix_ok(dy, ldy, H, dtype) || (dw && R > 0 && !matrix_ok(rows, ld_rows, H, dtype)) ||
+      (drows && R > 0 && !matrix_ok(drows, ld_drows, H, dtype)) || (drows && drows == rows && dw && ld_drows != ld_rows) || !inv_perm ||
+      !words_ok(inv_perm) || !words_ok(w) || !words_ok(dw))
+    return DAMOE_ERR_INVALID_ARG;
+  RowArgs a{dy, ldy, w, inv_perm, const_cast<void*>(rows), ld_rows, drows, ld_drows, dw, T, k, H, R, chunks_of(H, dtype)};
+  const int32_t per = T >= 1024 ? k : 1;
+  const dim3 grid(blocks_for((int64_t)T * ((k + per - 1) / per)));
+  if (dtype == DAMOE_BF16) hipLaunchKernelGGL(k_combine_rows_grad<true>, grid, dim3(kThreads), 0, stream, a, per);
+  else hipLaunchKernelGGL(k_combine_rows_grad<false>, grid, dim3(kThreads), 0, stream, a, per);
+  return last();
+}
+
+}  // extern "C"

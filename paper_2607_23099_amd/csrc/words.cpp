@@ -43,6 +43,11 @@ extern "C" damoe_status damoe_call_words(int32_t fn, const void* words, size_t n
     case DAMOE_CALL_ROUTER_LOSS: return call(damoe_router_loss, words, n);
     case DAMOE_CALL_ROUTER_LOSS_GRAD: return call(damoe_router_loss_grad, words, n);
     case DAMOE_CALL_MXFP4_LINEAR: return call(damoe_mxfp4_linear, words, n);
+    case DAMOE_CALL_SORT_ROWS: return call(damoe_sort_rows, words, n);
+    case DAMOE_CALL_COMBINE_ROWS: return call(damoe_combine_rows, words, n);
+    case DAMOE_CALL_COMBINE_ROWS_GRAD: return call(damoe_combine_rows_grad, words, n);
+    case DAMOE_CALL_ADAPTERS: return call(damoe_adapters, words, n);
+    case DAMOE_CALL_ADAPTERS_GRAD: return call(damoe_adapters_grad, words, n);
     default: return DAMOE_ERR_INVALID_ARG;
   }
 }

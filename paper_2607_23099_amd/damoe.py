@@ -37,7 +37,9 @@ EXPORTED = [
     "damoe_table_effexp_map", "damoe_table_effexp_candidates", "damoe_noalloc_scratch_bytes",
     "damoe_moe_layer_noalloc", "damoe_router_loss_workspace_size", "damoe_router_loss", "damoe_router_loss_grad",
     "damoe_mxfp4_bytes", "damoe_mxfp4_quantise", "damoe_mxfp4_dequantise", "damoe_mxfp4_pack",
-    "damoe_mxfp4_linear_workspace_size", "damoe_mxfp4_linear", "damoe_call_words",
+    "damoe_mxfp4_linear_workspace_size", "damoe_mxfp4_linear", "damoe_call_words", "damoe_sort_rows", "damoe_combine_rows",
+    "damoe_combine_rows_grad", "damoe_adapters_workspace_size", "damoe_adapters", "damoe_adapters_grad_workspace_size",
+    "damoe_adapters_grad",
 ]
 
 
@@ -132,6 +134,15 @@ def lib() -> ctypes.CDLL:
             "damoe_mxfp4_linear_workspace_size": ([i32, i32, i32], sz),
             "damoe_call_words": ([i32, ctypes.c_char_p, sz], i32),
             "damoe_mxfp4_linear": ([vp, i32, i64, i32, i32, vp, i32, vp, i64, vp, i32, i64, vp, sz, vp], i32),
+            "damoe_sort_rows": ([vp, i32, i64, vp, vp, i32, i32, i32, i32, vp, i64, vp], i32),
+            "damoe_combine_rows": ([vp, i32, i64, vp, vp, i32, i32, i32, i32, vp, i64, vp, i64, vp], i32),
+            "damoe_combine_rows_grad": ([vp, i32, i64, vp, i64, vp, vp, i32, i32, i32, i32, vp, i64, vp, vp], i32),
+            "damoe_adapters_workspace_size": ([i32, i32, i32, i32, i32], sz),
+            "damoe_adapters": ([vp, i32, i64, vp, vp, i32, i32, vp, vp, i32, i32, i32, i32, vp, vp, i64, vp, i32, i64, vp, vp, sz,
+                                vp], i32),
+            "damoe_adapters_grad_workspace_size": ([i32, i32, i32, i32, i32], sz),
+            "damoe_adapters_grad": ([vp, i32, i64, vp, i32, i64, vp, vp, vp, i32, i32, vp, vp, i32, i32, i32, i32, vp, vp, i64, vp,
+                                     i64, vp, vp, i32, vp, sz, vp], i32),
         }
         for name, (args, res) in sigs.items():
             fn = getattr(L, name)
@@ -382,6 +393,8 @@ def _offsets(t, S: int, dev: int) -> int:
 # damoe_call_words: ctypes takes 50 to 85 ns to convert an argument, and these calls have 15 to 21 (as words: 0.8 us less,
 # what the checks of their tensors cost).
 _LOSS_WORDS, _GRAD_WORDS, _LINEAR_WORDS = (struct.Struct(f).pack for f in ("=11q2d7q", "=15q2d4q", "=15q"))
+_SORT_WORDS, _COMBINE_WORDS, _COMBINE_GRAD_WORDS, _ADAPTERS_WORDS, _ADAPTERS_GRAD_WORDS = (
+    struct.Struct(f).pack for f in ("=12q", "=14q", "=15q", "=23q", "=28q"))
 
 
 def router_loss_workspace_size(T_max: int, E: int, S: int = 1) -> int:
@@ -516,6 +529,142 @@ def mxfp4_linear(x, T, K, w_tiles, N, y, ws, add=None, ldx=None, ldy=None, ld_ad
         _ld("y", y, T, N, ldy), _room("ws", ws, 0, dev), ws.nbytes, _stream_on("damoe_mxfp4_linear", stream, dev, dt, T)), 15)
     if rc:
         raise DamoeError("damoe_mxfp4_linear", rc)
+
+
+def _matrix(name: str, t, rows: int, cols: int, ld, like, dev: int):
+    """Pointer and row stride of a matrix of `like`'s type on device number `dev`, 0 and 0 for None."""
+    if t is None:
+        return 0, 0
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name}: {like.dtype} is wanted, as the call's other matrices have it, not {t.dtype}")
+    if t.get_device() != dev:
+        _elsewhere(name, t)
+    return t.data_ptr(), _ld(name, t, rows, cols, ld)
+
+
+def _n_rows(name: str, t, cols: int) -> int:
+    """Rows of a 2-D matrix of sorted rows."""
+    if len(t.shape) != 2:
+        raise ValueError(f"{name}: a matrix of rows of {cols} is wanted, not {tuple(t.shape)}")
+    return t.shape[0]
+
+
+def sort_rows(x, T, k, H, inv_perm, rows, w=None, ldx=None, stream=None):
+    """rows[inv_perm[t k + j]] = w[t][j] x[t] (damoe_sort_rows); places at or past rows' end are left out."""
+    if not _DTYPES:
+        _types()
+    dt, dev = _DTYPES.get(x.dtype, -1), x.get_device()
+    R = _n_rows("rows", rows, H)
+    p_rows, ldr = _matrix("rows", rows, R, H, None, x, dev)
+    rc = (_lib or lib()).damoe_call_words(3, _SORT_WORDS(
+        x.data_ptr(), dt, _ld("x", x, T, H, ldx), _list("w", w, _FLOAT32, T * k, dev), _list("inv_perm", inv_perm, _INT32, T * k, dev),
+        T, k, H, R, p_rows, ldr, _stream_on("damoe_sort_rows", stream, dev, dt, T)), 12)
+    if rc:
+        raise DamoeError("damoe_sort_rows", rc)
+
+
+def combine_rows(rows, T, k, H, inv_perm, y, w=None, add=None, ldy=None, ld_add=None, stream=None):
+    """y[t] = add[t] + sum_j w[t][j] rows[inv_perm[t k + j]] (damoe_combine_rows)."""
+    if not _DTYPES:
+        _types()
+    dt, dev = _DTYPES.get(rows.dtype, -1), rows.get_device()
+    R = _n_rows("rows", rows, H)
+    p_add, lda = _matrix("add", add, T, H, ld_add, rows, dev)
+    p_y, ld = _matrix("y", y, T, H, ldy, rows, dev)
+    rc = (_lib or lib()).damoe_call_words(4, _COMBINE_WORDS(
+        rows.data_ptr(), dt, _ld("rows", rows, R, H, None), _list("w", w, _FLOAT32, T * k, dev),
+        _list("inv_perm", inv_perm, _INT32, T * k, dev), T, k, H, R, p_add, lda, p_y, ld,
+        _stream_on("damoe_combine_rows", stream, dev, dt, T)), 14)
+    if rc:
+        raise DamoeError("damoe_combine_rows", rc)
+
+
+def combine_rows_grad(dy, rows, T, k, H, inv_perm, w=None, drows=None, dw=None, ldy=None, stream=None):
+    """drows[q] = w[t][j] dy[t] and dw[t][j] = <dy[t], rows[q]> at q = inv_perm[t k + j] (damoe_combine_rows_grad); rows may be
+    None without dw."""
+    if not _DTYPES:
+        _types()
+    dt, dev = _DTYPES.get(dy.dtype, -1), dy.get_device()
+    if rows is None and dw is not None:
+        raise ValueError("rows: dw needs them")
+    R = [_n_rows(n, t, H) for n, t in (("rows", rows), ("drows", drows)) if t is not None]
+    if len(R) == 2 and R[0] != R[1]:
+        raise ValueError(f"drows: {R[1]} rows, rows has {R[0]}")
+    R = R[0] if R else 0
+    p_rows, ldr = _matrix("rows", rows, R, H, None, dy, dev)
+    p_drows, ldd = _matrix("drows", drows, R, H, None, dy, dev)
+    rc = (_lib or lib()).damoe_call_words(5, _COMBINE_GRAD_WORDS(
+        dy.data_ptr(), dt, _ld("dy", dy, T, H, ldy), p_rows, ldr, _list("w", w, _FLOAT32, T * k, dev),
+        _list("inv_perm", inv_perm, _INT32, T * k, dev), T, k, H, R, p_drows, ldd, _list("dw", dw, _FLOAT32, T * k, dev),
+        _stream_on("damoe_combine_rows_grad", stream, dev, dt, T)), 15)
+    if rc:
+        raise DamoeError("damoe_combine_rows_grad", rc)
+
+
+def adapters_workspace_size(T_max: int, L: int, r: int, K: int, N: int) -> int:
+    return int(lib().damoe_adapters_workspace_size(T_max, L, r, K, N))
+
+
+def adapters_grad_workspace_size(T_max: int, L: int, r: int, K: int, N: int) -> int:
+    return int(lib().damoe_adapters_grad_workspace_size(T_max, L, r, K, N))
+
+
+def _pairs(a, b, dev: int):
+    """Sizes and type of adapters a [L][r][K], b [L][N][r]."""
+    if len(a.shape) != 3 or len(b.shape) != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
+        raise ValueError(f"a, b: [L][r][K] and [L][N][r] are wanted, not {tuple(a.shape)} and {tuple(b.shape)}")
+    if a.dtype != b.dtype or not a.is_contiguous() or not b.is_contiguous():
+        raise ValueError(f"a, b: contiguous tensors of one type are wanted, not {a.dtype}, {b.dtype} with strides {a.stride()}, "
+                         f"{b.stride()}")
+    for name, t in (("a", a), ("b", b)):
+        if t.get_device() != dev:
+            _elsewhere(name, t)
+    return (*a.shape, b.shape[1], _DTYPES.get(a.dtype, -1))
+
+
+def adapters(x, T, a, b, offsets, y, ws, perm=None, scale=None, add=None, u=None, ldx=None, ldy=None, ld_add=None, stream=None):
+    """y[t] = add[t] + scale_l b_l (a_l x[t]) for the rows t = perm[p] of segment l, the places [offsets[l], offsets[l + 1])
+    (damoe_adapters); a [L][r][K] and b [L][N][r].  u [T][r] keeps a_l x[t] by places for the gradient."""
+    if not _DTYPES:
+        _types()
+    dt, dev = _DTYPES.get(x.dtype, -1), x.get_device()
+    L, r, K, N, wt = _pairs(a, b, dev)
+    p_add, lda = _matrix("add", add, T, N, ld_add, y, dev)
+    p_y, ld = _matrix("y", y, T, N, ldy, y, dev)
+    rc = (_lib or lib()).damoe_call_words(6, _ADAPTERS_WORDS(
+        x.data_ptr(), dt, _ld("x", x, T, K, ldx), _list("perm", perm, _INT32, T, dev), _segment_offsets(offsets, L, dev), T, L,
+        a.data_ptr(), b.data_ptr(), wt, r, K, N, _list("scale", scale, _FLOAT32, L, dev), p_add, lda, p_y, _DTYPES.get(y.dtype, -1), ld,
+        _list("u", u, _FLOAT32, T * r, dev), _room("ws", ws, 0, dev), ws.nbytes, _stream_on("damoe_adapters", stream, dev, dt, T)), 23)
+    if rc:
+        raise DamoeError("damoe_adapters", rc)
+
+
+def _segment_offsets(t, L: int, dev: int) -> int:
+    p = _list("offsets", t, _INT32, L + 1, dev)
+    if t.numel() != L + 1:
+        raise ValueError(f"offsets: {L} adapters have {L + 1} offsets, not {t.numel()}")
+    return p
+
+
+def adapters_grad(x, dy, u, T, a, b, offsets, da, db, ws, perm=None, scale=None, add=None, dx=None, accumulate=False, ldx=None,
+                  ldy=None, ld_dx=None, ld_add=None, stream=None):
+    """Gradient of adapters for dy (damoe_adapters_grad): dx = add + ..., of x's type, and da, db in fp32, of a's and b's form
+    (accumulate: added to what they hold)."""
+    if not _DTYPES:
+        _types()
+    dt, dev = _DTYPES.get(x.dtype, -1), x.get_device()
+    L, r, K, N, wt = _pairs(a, b, dev)
+    p_dy, ld = _matrix("dy", dy, T, N, ldy, dy, dev)
+    p_add, lda = _matrix("add", add, T, K, ld_add, x, dev)
+    p_dx, ldd = _matrix("dx", dx, T, K, ld_dx, x, dev)
+    rc = (_lib or lib()).damoe_call_words(7, _ADAPTERS_GRAD_WORDS(
+        x.data_ptr(), dt, _ld("x", x, T, K, ldx), p_dy, _DTYPES.get(dy.dtype, -1), ld, _list("u", u, _FLOAT32, T * r, dev),
+        _list("perm", perm, _INT32, T, dev), _segment_offsets(offsets, L, dev), T, L, a.data_ptr(), b.data_ptr(), wt, r, K, N,
+        _list("scale", scale, _FLOAT32, L, dev), p_add, lda, p_dx, ldd, _list("da", da, _FLOAT32, L * r * K, dev),
+        _list("db", db, _FLOAT32, L * N * r, dev), int(accumulate), _room("ws", ws, 0, dev), ws.nbytes,
+        _stream_on("damoe_adapters_grad", stream, dev, dt)), 28)
+    if rc:
+        raise DamoeError("damoe_adapters_grad", rc)
 
 
 def read_device_error(ws, stream=None) -> int:
