@@ -148,6 +148,76 @@ struct Raw {
   }
 };
 
+// Lanes 4 b + a hold of register h element (h, a) of a 4 x 4 block of their own; after it element (a, h).
+__device__ __forceinline__ void transpose4(uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
+  const int lane = threadIdx.x;
+  const auto exchange = [](bool upper, auto other, uint32_t& x, uint32_t& y) {
+    const uint32_t a = other(y), b = other(x);  // by all lanes
+    x = upper ? a : x, y = upper ? y : b;
+  };
+  const auto one = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true); };  // lane ^ 1
+  const auto two = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true); };  // lane ^ 2
+  exchange(lane & 1, one, r0, r1);
+  exchange(lane & 1, one, r2, r3);
+  exchange(lane & 2, two, r0, r2);
+  exchange(lane & 2, two, r1, r3);
+}
+
+constexpr int kUnit = 128;  // columns
+
+// 16 rows of a unit of columns.  As operands lane (i, g) needs row i, but 16 lanes that load from 16 rows cost the address
+// units a cycle each; four side by side that share 64 bytes cost one together.  So lane 16 g + 4 b + a loads piece a of rows
+// 4 b + h, h = 0 .. 3, and four lanes exchange what they have.  Lane (i, g) then has columns 32 g .. + 31 of row i.
+template <bool SRC>
+struct Rows16 {
+  static constexpr int kSets = SRC ? 1 : 2;  // of four pieces of 16 bytes
+  uint32_t q[kSets * 4][4];
+
+  // The lane's row number h of those that it loads.
+  static __device__ __forceinline__ int mine(int h) { return (threadIdx.x >> 2 & 3) * 4 + h; }
+
+  // at(h): the first element of row mine(h); c: the unit's first column.
+  template <class F>
+  __device__ __forceinline__ void load(const void* base, F at, int c) {
+    typedef Elem<SRC> E;
+    const int g = (threadIdx.x & 63) >> 4, a = threadIdx.x & 3;
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const uint4 v = load16_at<E::kBytes>(static_cast<const typename E::T*>(base) + (at(h) + (c + 32 * g + (4 * s + a) * E::kPer16)));
+        uint32_t(&d)[4] = q[4 * s + h];
+        d[0] = v.x, d[1] = v.y, d[2] = v.z, d[3] = v.w;
+      }
+  }
+  __device__ __forceinline__ void exchange() {
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) transpose4(q[4 * s][d], q[4 * s + 1][d], q[4 * s + 2][d], q[4 * s + 3][d]);
+  }
+  // Row i, from element `at` on, of which n columns from the lane's first are the row's; no exchange after it.
+  __device__ __forceinline__ void load_some(const void* base, int64_t at, int n) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      Raw<SRC> f;
+      f.load_some(base, at + 8 * t, n - 8 * t);
+      put(t, f);
+    }
+  }
+  // Columns 8 t .. + 7 of the lane's.
+  __device__ __forceinline__ void put(int t, const Raw<SRC>& f) {
+#pragma unroll
+    for (int j = 0; j < (SRC ? 4 : 8); ++j) q[SRC ? t : 2 * t + j / 4][j % 4] = f.q[j];
+  }
+  __device__ __forceinline__ Raw<SRC> get(int t) const {
+    Raw<SRC> f;
+#pragma unroll
+    for (int j = 0; j < (SRC ? 4 : 8); ++j) f.q[j] = q[SRC ? t : 2 * t + j / 4][j % 4];
+    return f;
+  }
+};
+
 // Eight elements of one row of an MFMA operand: lane i + 16 g has row i, and g's eight of the 32 that are multiplied.
 template <bool BF>
 struct Frag {
@@ -200,131 +270,137 @@ struct DownArgs {
   const int32_t* off;
   const float* scale;  // of a segment's sums, or NULL
   float* part;     // [parts][T][rp], or NULL: with one part, what `up` takes and u are written
-  void* ready;     // [3][T][rp] thirds in bf16, or [T][rp] fp32
+  void* ready;     // Ready, groups of places from each segment's first on
   float* u;        // [T][r] or NULL
   int32_t L, T, C, r, rp;
   int32_t places;  // of a block
-  int32_t units;   // of 64 columns that a block takes
+  int32_t units;   // of columns that a block takes
 };
 
-// Eight columns from c on of the lane's ranks, lane % 16 of each block of 16.
+// A unit of columns of RB blocks of 16 ranks from r0 on, lane (i, g)'s columns as those of Rows16.
 template <bool WB, Lie LIE, int RB>
-struct Weights8 {
-  static constexpr int kSets = LIE == kPairs ? RB / 2 : RB, kWords = LIE == kRows && WB ? 4 : 8;
-  uint32_t q[kSets][kWords];
+struct Weights {
+  static constexpr int kSets = LIE == kPairs ? RB / 2 : RB;
+  typename std::conditional<LIE == kRows, Rows16<WB>[kSets], uint32_t[kSets][4][8]>::type q;
 
-  // n of the columns are the matrix's, the others 0.
+  // The weights from the segment's first on.  `columns` of the unit are the matrix's, the others 0.
   template <bool FULL>
-  __device__ __forceinline__ void load(const DownArgs& a, int64_t slab, int r0, int i, int c, int n) {
+  __device__ __forceinline__ void load(const DownArgs& a, const void* slab, int r0, int c, int columns) {
     typedef typename Elem<WB>::T T;
     struct __attribute__((packed, aligned(2))) Two {
       uint32_t v;
     };
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
       if constexpr (LIE == kRows) {
-        Raw<WB> f;
-        const int64_t at = slab + (int64_t)min(r0 + 16 * s + i, a.r - 1) * a.C + c;
-        if constexpr (FULL) f.load(a.w, at);
-        else f.load_some(a.w, at, n);
-#pragma unroll
-        for (int j = 0; j < kWords; ++j) q[s][j] = f.q[j];
+        if constexpr (FULL) q[s].load(slab, [&](int h) { return min(r0 + 16 * s + Rows16<WB>::mine(h), a.r - 1) * a.C; }, c);
+        else q[s].load_some(slab, min(r0 + 16 * s + i, a.r - 1) * a.C + c + 32 * g, columns - 32 * g);
       } else {
         const int rho = LIE == kPairs ? min(r0 + 32 * s + 2 * i, a.r - 2) : min(r0 + 16 * s + i, a.r - 1);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const T* p = static_cast<const T*>(a.w) + slab + (int64_t)(FULL ? c + j : min(c + j, a.C - 1)) * a.r + rho;
-          if constexpr (LIE == kPairs) q[s][j] = reinterpret_cast<const Two*>(p)->v;
-          else if constexpr (WB) q[s][j] = *p;
-          else q[s][j] = __float_as_uint(*p);
-          if (!FULL && j >= n) q[s][j] = 0;
-        }
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int k = 32 * g + 8 * t + j;
+            const T* p = static_cast<const T*>(slab) + (FULL ? c + k : min(c + k, a.C - 1)) * a.r + rho;
+            uint32_t& v = q[s][t][j];
+            if constexpr (LIE == kPairs) v = reinterpret_cast<const Two*>(p)->v;
+            else if constexpr (WB) v = *p;
+            else v = __float_as_uint(*p);
+            if (!FULL && k >= columns) v = 0;
+          }
       }
     }
   }
-  template <bool BF>
-  __device__ __forceinline__ Frag<BF> get(int rb) const {
+  __device__ __forceinline__ void exchange() {
     if constexpr (LIE == kRows) {
-      Raw<WB> f;
 #pragma unroll
-      for (int j = 0; j < kWords; ++j) f.q[j] = q[rb][j];
-      return frag<BF>(f);
+      for (int s = 0; s < kSets; ++s) q[s].exchange();
+    }
+  }
+  template <bool BF>
+  __device__ __forceinline__ Frag<BF> get(int rb, int t) const {
+    if constexpr (LIE == kRows) {
+      return frag<BF>(q[rb].get(t));
     } else {
+      const uint32_t(&v)[8] = q[LIE == kPairs ? rb / 2 : rb][t];
       Frag<BF> f;
-      if constexpr (LIE == kPairs) {
-        const uint32_t(&v)[8] = q[rb / 2];
 #pragma unroll
-        for (int j = 0; j < (BF ? 4 : 8); ++j) {
+      for (int j = 0; j < (BF ? 4 : 8); ++j) {
+        if constexpr (LIE == kPairs) {
           if constexpr (BF) f.q[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], rb & 1 ? 0x07060302u : 0x05040100u);
           else f.q[j] = rb & 1 ? v[j] & 0xFFFF0000u : v[j] << 16;
+        } else {
+          if constexpr (BF) f.q[j] = v[2 * j] | v[2 * j + 1] << 16;
+          else f.q[j] = WB ? v[j] << 16 : v[j];
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < (BF ? 4 : 8); ++j) f.q[j] = BF ? q[rb][2 * j] | q[rb][2 * j + 1] << 16 : WB ? q[rb][j] << 16 : q[rb][j];
       }
       return f;
     }
   }
 };
 
-// Sums over units of 64 columns by W waves in turn, RB blocks of 16 ranks from r0 on and M of 16 places.  A unit is two MFMA
-// steps: lane (i, g) takes columns 16 g .. + 7 of it in the first and 16 g + 8 .. + 15 in the second, so that its loads of a
-// row are 32 bytes (bf16) side by side.  D units are in flight.
+// Sums over units of columns by W waves in turn, RB blocks of 16 ranks from r0 on and M of 16 places.  A unit is four MFMA
+// steps, of each lane's columns 8 t .. + 7.  D units are in flight.
 template <bool XB, bool WB, Lie LIE, int RB, int M, int W>
 struct Down {
   static constexpr bool BF = XB && WB;
   struct Unit {
-    Raw<XB> x[2][M];
-    Weights8<WB, LIE, RB> w[2];
+    Rows16<XB> x[M];
+    Weights<WB, LIE, RB> w;
   };
-  static constexpr int kRegs = sizeof(Unit) / 4, D = kRegs <= 16 ? 4 : kRegs <= 32 ? 3 : 2;
+  static constexpr int kRegs = sizeof(Unit) / 4, D = kRegs <= 32 ? 3 : kRegs <= 72 ? 2 : 1;
   floatx4 acc[M][RB];
 
   __device__ __forceinline__ void multiply(const Unit& v, bool second) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int t = 0; t < 4; ++t) {
       Frag<BF> w[RB];
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) w[rb] = v.w[h].template get<BF>(rb);
+      for (int rb = 0; rb < RB; ++rb) w[rb] = v.w.template get<BF>(rb, t);
 #pragma unroll
       for (int m = 0; m < M; ++m) {
         if (!BF && m && !second) continue;  // fp32 instructions are long: none for places that the tile does not have
-        const Frag<BF> x = frag<BF>(v.x[h][m]);
+        const Frag<BF> x = frag<BF>(v.x[m].get(t));
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) acc[m][rb] = mma(w[rb], x, acc[m][rb]);
       }
     }
   }
+  __device__ __forceinline__ void exchange(Unit& v) {
+#pragma unroll
+    for (int m = 0; m < M; ++m) v.x[m].exchange();
+    v.w.exchange();
+  }
 
   __device__ __forceinline__ void run(const DownArgs& a, const Tile& tile, int u0, int u1, int r0) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i = lane & 15, g = lane >> 4;
     const Places places(a.perm, a.off);
     const bool second = tile.hi - tile.lo > 16;
-    int64_t row[M];
-#pragma unroll
-    for (int m = 0; m < M; ++m) {
-      const int p = min(tile.lo + 16 * m + i, tile.hi - 1), t = places.row(places.load(p), p);
-      row[m] = (int64_t)((uint32_t)t < (uint32_t)a.T ? t : 0) * a.ldx;
-    }
-    const int64_t slab = (int64_t)tile.l * a.r * a.C;
+    const auto row = [&](int place) {  // its first element; of places past the end the last one's
+      const int p = min(tile.lo + place, tile.hi - 1), t = places.row(places.load(p), p);
+      return (int64_t)((uint32_t)t < (uint32_t)a.T ? t : 0) * a.ldx;
+    };
+    const char* slab = static_cast<const char*>(a.w) + (int64_t)tile.l * a.r * a.C * Elem<WB>::kBytes;
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) acc[m][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const auto load = [&](Unit& v, int u) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = u * 64 + 16 * g + 8 * h;
-#pragma unroll
-        for (int m = 0; m < M; ++m) v.x[h][m].load(a.x, row[m] + c);
-        v.w[h].template load<true>(a, slab, r0, i, c, 8);
-      }
-    };
-    const int whole = a.C / 64;  // units
+    const int whole = a.C / kUnit;  // units
     int left = min(u1, whole) - u0 - wave;
     left = left > 0 ? (left + W - 1) / W : 0;
     if (left > 0) {
+      int64_t rows[M][4];
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) rows[m][h] = row(16 * m + Rows16<XB>::mine(h));
+      const auto load = [&](Unit& v, int u) {
+        v.w.template load<true>(a, slab, r0, u * kUnit, kUnit);
+#pragma unroll
+        for (int m = 0; m < M; ++m) v.x[m].load(a.x, [&](int h) { return rows[m][h]; }, u * kUnit);
+      };
       Unit v[D];
       int u = u0 + wave;
       const int last = u + (left - 1) * W;
@@ -333,28 +409,32 @@ struct Down {
       for (u += D * W; left >= 2 * D; left -= D) {
 #pragma unroll
         for (int d = 0; d < D; ++d, u += W) {
+          exchange(v[d]);
           multiply(v[d], second);
           load(v[d], u);
         }
       }
 #pragma unroll
       for (int d = 0; d < D; ++d, u += W) {
-        if (d < left) multiply(v[d], second);
+        if (d < left) {
+          exchange(v[d]);
+          multiply(v[d], second);
+        }
         if (d + D < left) load(v[d], u);
       }
 #pragma unroll
       for (int d = 0; d < D - 1; ++d)
-        if (d + D < left) multiply(v[d], second);
+        if (d + D < left) {
+          exchange(v[d]);
+          multiply(v[d], second);
+        }
     }
     if (whole >= u0 && whole < u1 && (whole - u0) % W == wave) {
       Unit v;
+      const int c = whole * kUnit, i = lane & 15, g = lane >> 4;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = whole * 64 + 16 * g + 8 * h;
-#pragma unroll
-        for (int m = 0; m < M; ++m) v.x[h][m].load_some(a.x, row[m] + c, a.C - c);
-        v.w[h].template load<false>(a, slab, r0, i, c, a.C - c);
-      }
+      for (int m = 0; m < M; ++m) v.x[m].load_some(a.x, row(16 * m + i) + c + 32 * g, a.C - c - 32 * g);
+      v.w.template load<false>(a, slab, r0, c, a.C - c);
       multiply(v, second);
     }
   }
@@ -388,26 +468,36 @@ struct Down {
   }
 };
 
-// Rows of the sums that `up` takes: thirds in bf16 for bf16 weights, else fp32.
+// The sums as `up` takes them: thirds in bf16 for bf16 weights, else fp32, in pieces of 16 bytes.  Groups of n <= 16 places
+// have piece by piece those of their places side by side, which is how a wave loads an operand: piece b of place i lies at
+// 16 (b n + i) of its group.  Piece: 8 ranks of a third, or 4 ranks.
 template <bool WB>
-__device__ __forceinline__ void put_ready(void* ready, int64_t plane, int64_t at, floatx4 v) {
-  if constexpr (WB) {
+struct Ready {
+  static constexpr int kBytes = WB ? 6 : 4;  // of a place and rank
+
+  static __device__ __forceinline__ char* group(void* base, int p, int rp) { return static_cast<char*>(base) + (int64_t)p * rp * kBytes; }
+  static __device__ __forceinline__ int piece(int third, int rho, int rp) { return WB ? (third * rp + rho) / 8 : rho / 4; }
+
+  // Ranks rho .. + 3 (rho a multiple of 4) of place i.
+  static __device__ __forceinline__ void put(char* group, int n, int i, int rho, int rp, floatx4 v) {
 #pragma unroll
-    for (int h = 0; h < 3; ++h) {
-      uint16_t q[4];
+    for (int h = 0; h < (WB ? 3 : 1); ++h) {
+      char* p = group + 16 * (piece(h, rho, rp) * n + i);
+      if constexpr (WB) {
+        uint16_t q[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float f = v[k];
-        q[k] = take_third(f);
-        v[k] = f;
+        for (int k = 0; k < 4; ++k) {
+          float f = v[k];
+          q[k] = take_third(f);
+          v[k] = f;
+        }
+        *reinterpret_cast<uint2*>(p + 2 * (rho % 8)) = uint2{q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16};
+      } else {
+        *reinterpret_cast<floatx4*>(p) = v;
       }
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(ready) + h * plane + at) =
-          uint2{q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16};
     }
-  } else {
-    *reinterpret_cast<floatx4*>(static_cast<float*>(ready) + at) = v;
   }
-}
+};
 
 constexpr int kDownWaves = 8;
 
@@ -416,7 +506,7 @@ template <bool XB, bool WB, Lie LIE, int RB, int M>
 __global__ void __launch_bounds__(kDownWaves* kWave) k_adapter_down(DownArgs a) {
   typedef Down<XB, WB, LIE, RB, M, kDownWaves> D;
   extern __shared__ floatx4 red[];
-  const int u0 = blockIdx.y * a.units, u1 = min(u0 + a.units, (a.C + 63) / 64);
+  const int u0 = blockIdx.y * a.units, u1 = min(u0 + a.units, (a.C + kUnit - 1) / kUnit);
   const int r0 = blockIdx.z * 16 * RB;
   Tile tile;
   if (!find_tile<false>(a.off, a.L, a.T, a.places, blockIdx.x, tile)) return;
@@ -440,28 +530,16 @@ __global__ void __launch_bounds__(kDownWaves* kWave) k_adapter_down(DownArgs a) 
       for (int k = 0; k < 4; ++k)
         if (rho + k < a.r) a.u[(int64_t)p * a.r + rho + k] = v[k];
     }
-    put_ready<WB>(a.ready, (int64_t)a.T * a.rp, (int64_t)p * a.rp + rho, v);
+    const int i = (p - tile.lo) % 16, first = p - i;
+    Ready<WB>::put(Ready<WB>::group(a.ready, first, a.rp), min(16, tile.hi - first), i, rho, a.rp, v);
   }
-}
-
-// Sum of the parts of one value, in order, with eight loads in flight.
-__device__ __forceinline__ float add_parts(const float* p, int64_t apart, int n) {
-  float v = 0.f;
-  for (int k = 0; k < n; k += 8) {
-    float q[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = k + j < n ? p[(k + j) * apart] : 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v += q[j];
-  }
-  return v;
 }
 
 // ---------------------------------------------------------------- up
 
 struct UpArgs {
   const float* part;  // [parts][T][rp] (JOIN), joined here
-  const void* ready;  // else: [3][T][rp] thirds in bf16, or [T][rp] fp32
+  void* ready;        // else: Ready
   int32_t parts;
   float* u;           // JOIN: NULL, or the joined sums [T][r]
   const void* w;      // B [L][C][r], or A [L][r][C]
@@ -472,23 +550,21 @@ struct UpArgs {
   int64_t lda;
   void* y;
   int64_t ldy;
+  char* spare;        // not JOIN: kSpare bytes that nothing reads
   int32_t L, T, C, r, rp, places;
 };
 
-constexpr int kUpCols = 64;  // columns of a wave
+constexpr size_t kSpare = 64 * 16;
 
-// The sums of 16 places as MFMA operands, and the weights that they meet: RB blocks of 16 ranks, or (RB = 0) 8 ranks.
-// bf16 weights: three thirds, whose products are exact, an operand each; of 16 ranks two in one operand over the same weights
-// twice, of 8 ranks all three.  fp32: instruction j multiplies rank kPer g + j of lane (i, g).
+// The sums of 16 places as MFMA operands: RB blocks of 16 ranks, or (RB = 0) 8 ranks.  bf16 weights: three thirds, whose
+// products are exact, an operand each; of 16 ranks two in one operand over the same weights twice, of 8 ranks all three.
+// fp32: instruction j multiplies rank kPer g + j of lane (i, g).
 template <bool WB, int RB>
 struct Sums {
-  static constexpr int kPlanes = WB ? 3 : 1;
-  static constexpr int kPer = WB ? 8 : RB ? 4 * RB : 2;         // ranks of a lane in an operand
-  static constexpr int kBlocks = WB && RB > 2 ? RB / 2 : 1;     // operands for the ranks
+  static constexpr int kPer = WB ? 8 : RB ? 4 * RB : 2;            // ranks of a lane in an operand
+  static constexpr int kBlocks = WB && RB > 2 ? RB / 2 : 1;        // operands for the ranks
   static constexpr int kOps = !WB ? 1 : RB >= 2 ? 3 : RB ? 2 : 1;  // of each: for the thirds
   static constexpr int kWords = WB ? 4 : kPer;
-  static constexpr int kStride = 16 * (RB ? RB : 1) + (WB ? 8 : 4);  // in LDS, of a place
-  typedef typename std::conditional<WB, uint16_t, float>::type T;
   uint32_t q[kBlocks][kOps][kWords];
 
   // First rank of lane group g in block kb.
@@ -501,175 +577,223 @@ struct Sums {
     return RB >= 2 ? h : RB ? 2 * h + g / 2 : g;
   }
 
-  // Row p of planes `plane` elements apart, rows of `stride`.
-  __device__ __forceinline__ void load(const T* base, int64_t plane, int64_t p, int stride, int g) {
+  // Place i (at most n - 1) of a group of n.
+  __device__ __forceinline__ void load(const char* group, int n, int i, int rp, int g) {
 #pragma unroll
     for (int kb = 0; kb < kBlocks; ++kb)
 #pragma unroll
       for (int h = 0; h < kOps; ++h) {
-        const T* s = base + min(third(h, g), kPlanes - 1) * plane + p * stride + rank(kb, g);
+        const int rho = rank(kb, g), b = Ready<WB>::piece(min(third(h, g), 2), rho, rp);
         if constexpr (kWords == 2) {
-          const uint2 v = *reinterpret_cast<const uint2*>(s);
+          const uint2 v = *reinterpret_cast<const uint2*>(group + 16 * (b * n + i) + 4 * (rho % 4));
           q[kb][h][0] = v.x, q[kb][h][1] = v.y;
         } else {
 #pragma unroll
-          for (int e = 0; e < kWords; e += 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(s + (WB ? 0 : e));
-            q[kb][h][e] = v.x, q[kb][h][e + 1] = v.y, q[kb][h][e + 2] = v.z, q[kb][h][e + 3] = v.w;
+          for (int e = 0; e < kWords / 4; ++e) {
+            const uint4 v = *reinterpret_cast<const uint4*>(group + 16 * ((b + e) * n + i));
+            uint32_t* d = &q[kb][h][4 * e];
+            d[0] = v.x, d[1] = v.y, d[2] = v.z, d[3] = v.w;
           }
         }
       }
   }
-  static __device__ __forceinline__ void put(T* lds, int places, int p, int rho, float v) {
-    if constexpr (WB) {
-#pragma unroll
-      for (int h = 0; h < 3; ++h) lds[(h * places + p) * kStride + rho] = take_third(v);
+};
+
+// N elements side by side, 8 or 16 bytes.
+template <bool YB, int N>
+struct Side {
+  typedef Elem<YB> E;
+  static constexpr int kWords = N * E::kBytes / 4;
+  uint32_t q[kWords];
+
+  __device__ __forceinline__ void load(const typename E::T* p) {
+    if constexpr (kWords == 4) {
+      const uint4 v = load16_at<E::kBytes>(p);
+      q[0] = v.x, q[1] = v.y, q[2] = v.z, q[3] = v.w;
     } else {
-      lds[p * kStride + rho] = v;
+      __builtin_memcpy(q, p, sizeof q);
+    }
+  }
+  __device__ __forceinline__ void store(typename E::T* p) const {
+    if constexpr (kWords == 4) store16_at<E::kBytes>(p, uint4{q[0], q[1], q[2], q[3]});
+    else __builtin_memcpy(p, q, sizeof q);
+  }
+  // The first n elements are the row's; the others are 0, or left.
+  __device__ __forceinline__ void load_some(const typename E::T* p, int n) {
+    if (n >= N) return load(p);
+#pragma unroll
+    for (uint32_t& e : q) e = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < n) {
+        if constexpr (YB) q[j / 2] |= (uint32_t)p[j] << (16 * (j & 1));
+        else q[j] = __float_as_uint(p[j]);
+      }
+  }
+  __device__ __forceinline__ void store_some(typename E::T* p, int n) const {
+    if (n >= N) return store(p);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < n) {
+        if constexpr (YB) p[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+        else p[j] = __uint_as_float(q[j]);
+      }
+  }
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (YB) return __uint_as_float(j & 1 ? q[j / 2] & 0xFFFF0000u : q[j / 2] << 16);
+    else return __uint_as_float(q[j]);
+  }
+  __device__ __forceinline__ void put(const float (&f)[N]) {
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) {
+      if constexpr (YB) q[j] = pack_bf16x2(f[2 * j], f[2 * j + 1]);
+      else q[j] = __float_as_uint(f[j]);
     }
   }
 };
 
-template <bool WB, int RB>
-struct UpWeights {
-  typedef Sums<WB, RB> S;
-  uint32_t q[4][S::kBlocks][S::kWords];
-
-  // Ranks of column c; ACROSS: `apart` elements from one to the next.  Ranks from r on are 0.
-  template <bool ACROSS>
-  static __device__ __forceinline__ void ranks(uint32_t (&q)[S::kWords], const void* base, int64_t i, int64_t apart, int n) {
-    typedef Elem<WB> E;
-    const typename E::T* p = static_cast<const typename E::T*>(base) + i;
-    if (!ACROSS && n >= S::kPer) {
-      if constexpr (S::kWords == 2) {
-        q[0] = __float_as_uint(p[0]), q[1] = __float_as_uint(p[1]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < S::kWords; e += 4) {
-          const uint4 v = load16_at<E::kBytes>(p + (WB ? 0 : e));
-          q[e] = v.x, q[e + 1] = v.y, q[e + 2] = v.z, q[e + 3] = v.w;
-        }
-      }
-      return;
-    }
-    uint32_t v[S::kPer];
-#pragma unroll
-    for (int j = 0; j < S::kPer; ++j) {  // past the last rank: that one again, and not used
-      const typename E::T* at = p + (ACROSS ? min(j, n - 1) * apart : min(j, n - 1));
-      if constexpr (WB) v[j] = *at;
-      else v[j] = __float_as_uint(*at);
-      if (j >= n) v[j] = 0;
-    }
-#pragma unroll
-    for (int e = 0; e < S::kWords; ++e) q[e] = WB ? v[2 * e % S::kPer] | v[(2 * e + 1) % S::kPer] << 16 : v[e % S::kPer];
-  }
-
-  // Four MFMA blocks of 16 columns from c0 on: row i of block 2 q + m is column 32 q + 8 (i / 4) + 4 m + i % 4, so that a
-  // lane's results of a pair are eight columns side by side of its place.
-  template <bool ACROSS>
-  __device__ __forceinline__ void load(const UpArgs& a, int64_t slab, int c0) {
-    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int c = min(c0 + 32 * (b / 2) + 8 * (i / 4) + 4 * (b & 1) + i % 4, a.C - 1);
-#pragma unroll
-      for (int kb = 0; kb < S::kBlocks; ++kb) {
-        const int rho = S::rank(kb, g);
-        ranks<ACROSS>(q[b][kb], a.w, slab + (ACROSS ? (int64_t)rho * a.C + c : (int64_t)c * a.r + rho), a.C, a.r - rho);
-      }
-    }
-  }
-};
-
-// 16 places by 64 columns of a wave: what is added, the product, the result.
+// 16 places by 16 NB columns of a wave.  MFMA b has column NB i + b as its column i, so that lane (i, g) has NB columns side by
+// side of places 4 g .. + 3, and 16 lanes 16 NB: rows are read and written in pieces of 128 to 256 bytes.
 template <bool YB, bool WB, int RB>
 struct Up {
   typedef Sums<WB, RB> S;
   typedef Elem<YB> E;
   typedef typename E::T Y;
-  static constexpr int P = 8 / E::kPer16;  // 16-byte pieces of eight columns
-  S u;
-  uint4 add[2][P];
+  // 8 blocks of 128 fp32 ranks would take all registers.
+  static constexpr int NB = !WB && RB == 8 ? 4 : E::kPer16, kCols = 16 * NB;
 
-  // FULL: all of the wave's columns are the matrix's and there is something to add (or `zero`, a buffer that is read and not
-  // used); t is a row.
-  template <bool FULL>
-  __device__ __forceinline__ void load_add(const UpArgs& a, const void* zero, int t, int c0) {
-    const int g = (threadIdx.x & 63) >> 4;
-    const void* base = FULL && !a.add ? zero : a.add;
-    const int64_t row = FULL && !a.add ? 0 : t * a.lda;
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int h = 0; h < P; ++h) {
-        const int c = c0 + 32 * q + 8 * g + h * E::kPer16, n = a.C - c;
-        const Y* p = static_cast<const Y*>(base) + row + (FULL && !a.add ? 0 : c);
-        if constexpr (FULL) {
-          add[q][h] = load16_at<E::kBytes>(p);
+  // The weights of the wave's columns from c0 on, 0 for ranks from r on.
+  struct Weights {
+    uint32_t q[NB][S::kBlocks][S::kWords];
+
+    // n ranks from element i on; ACROSS: `apart` elements from one to the next.
+    template <bool ACROSS>
+    static __device__ __forceinline__ void ranks(uint32_t (&q)[S::kWords], const void* base, int64_t i, int64_t apart, int n) {
+      typedef Elem<WB> F;
+      const typename F::T* p = static_cast<const typename F::T*>(base) + i;
+      if (!ACROSS && n >= S::kPer) {
+        if constexpr (S::kWords == 2) {
+          q[0] = __float_as_uint(p[0]), q[1] = __float_as_uint(p[1]);
         } else {
-          add[q][h] = uint4{0, 0, 0, 0};
-          if (a.add && t >= 0 && n > 0) add[q][h] = load_some<YB>(p, n);
+#pragma unroll
+          for (int e = 0; e < S::kWords; e += 4) {
+            const uint4 v = load16_at<F::kBytes>(p + (WB ? 0 : e));
+            q[e] = v.x, q[e + 1] = v.y, q[e + 2] = v.z, q[e + 3] = v.w;
+          }
+        }
+        return;
+      }
+      uint32_t v[S::kPer];
+#pragma unroll
+      for (int j = 0; j < S::kPer; ++j) {  // past the last rank: that one again, and not used
+        const typename F::T* at = p + (ACROSS ? min(j, n - 1) * apart : min(j, n - 1));
+        if constexpr (WB) v[j] = *at;
+        else v[j] = __float_as_uint(*at);
+        if (j >= n) v[j] = 0;
+      }
+#pragma unroll
+      for (int e = 0; e < S::kWords; ++e) q[e] = WB ? v[2 * e % S::kPer] | v[(2 * e + 1) % S::kPer] << 16 : v[e % S::kPer];
+    }
+
+    template <bool ACROSS>
+    __device__ __forceinline__ void load(const UpArgs& a, int l, int c0) {
+      const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+      const int64_t slab = (int64_t)l * a.r * a.C;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int c = min(c0 + NB * i + b, a.C - 1);
+#pragma unroll
+        for (int kb = 0; kb < S::kBlocks; ++kb) {
+          const int rho = S::rank(kb, g);
+          ranks<ACROSS>(q[b][kb], a.w, slab + (ACROSS ? (int64_t)rho * a.C + c : (int64_t)c * a.r + rho), a.C, a.r - rho);
         }
       }
+    }
+  };
+
+  S u;
+  Side<YB, NB> add[4];
+  int t[4];  // rows of places 4 g .. + 3, -1: none
+
+  // Lane by lane the row of place i of the group, -1: none.
+  __device__ __forceinline__ void rows(int row) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = __shfl(row, 4 * g + e);
+  }
+  // FULL: all of the wave's columns are the matrix's.  `zero`: a buffer that is read where there is nothing to add, and not used.
+  template <bool FULL>
+  __device__ __forceinline__ void load_add(const UpArgs& a, const void* zero, int c0) {
+    const int c = c0 + NB * (threadIdx.x & 15), n = a.C - c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (FULL) {
+        const Y* base = static_cast<const Y*>(a.add ? a.add : zero);
+        add[e].load(base + (a.add ? max(t[e], 0) * a.lda + c : 0));
+      } else {
+        add[e] = Side<YB, NB>{};
+        if (a.add && t[e] >= 0 && n > 0) add[e].load_some(static_cast<const Y*>(a.add) + t[e] * a.lda + c, n);
+      }
+    }
   }
 
-  // Row t, if it is one, is add + s times the product.
+  // The rows are add + s times the product.
   template <bool FULL>
-  __device__ __forceinline__ void work(const UpArgs& a, const UpWeights<WB, RB>& w, int t, int c0, float s) {
-    const int g = (threadIdx.x & 63) >> 4;
-    floatx4 acc[4];
+  __device__ __forceinline__ void work(const UpArgs& a, const Weights& w, int c0, float s) {
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    floatx4 acc[NB];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) acc[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < NB; ++b) acc[b] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int kb = 0; kb < S::kBlocks; ++kb)
 #pragma unroll
       for (int h = 0; h < S::kOps; ++h) {
+        const uint32_t(&v)[S::kWords] = u.q[kb][h];
         if constexpr (WB) {
           const bool none = S::third(h, g) >= 3;
-          const uint32_t(&v)[S::kWords] = u.q[kb][h];
           const uint4 f = none ? uint4{0, 0, 0, 0} : uint4{v[0], v[1], v[2], v[3]};
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
+          for (int b = 0; b < NB; ++b) {
             const uint32_t(&x)[S::kWords] = w.q[b][kb];
-            acc[b] = mfma16x16x32(uint4{x[0], x[1], x[2], x[3]}, f, acc[b]);
+            acc[b] = mfma16x16x32(f, uint4{x[0], x[1], x[2], x[3]}, acc[b]);
           }
         } else {
 #pragma unroll
           for (int j = 0; j < S::kWords; ++j)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) acc[b] = mma4(w.q[b][kb][j], u.q[kb][h][j], acc[b]);
+            for (int b = 0; b < NB; ++b) acc[b] = mma4(v[j], w.q[b][kb][j], acc[b]);
         }
       }
-    if (t < 0) return;
+    const int c = c0 + NB * i;
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
+    for (int e = 0; e < 4; ++e) {
+      if (!FULL && (t[e] < 0 || c >= a.C)) continue;
+      float f[NB];
 #pragma unroll
-      for (int h = 0; h < P; ++h) {
-        const int c = c0 + 32 * q + 8 * g + h * E::kPer16, n = a.C - c;
-        if (!FULL && n <= 0) continue;
-        float f[E::kPer16];
-        unpack16<YB>(FULL && !a.add ? uint4{0, 0, 0, 0} : add[q][h], f);
-#pragma unroll
-        for (int e = 0; e < E::kPer16; ++e) f[e] = fmaf(s, acc[2 * q + (h * E::kPer16 + e) / 4][(h * E::kPer16 + e) % 4], f[e]);
-        Y* p = static_cast<Y*>(a.y) + t * a.ldy + c;
-        if constexpr (FULL) store16_at<E::kBytes>(p, pack16<YB>(f));
-        else store_some<YB>(p, n, pack16<YB>(f));
-      }
+      for (int b = 0; b < NB; ++b) f[b] = fmaf(s, acc[b][e], FULL && !a.add ? 0.f : add[e].get(b));
+      Side<YB, NB> v;
+      v.put(f);
+      Y* p = static_cast<Y*>(a.y) + t[e] * a.ldy + c;
+      // The store is there for places without a row too, so that the wait for the next loads can count it.
+      if constexpr (FULL) v.store(t[e] < 0 ? reinterpret_cast<Y*>(a.spare + 16 * lane) : p);
+      else v.store_some(p, a.C - c);
+    }
   }
 };
 
 // JOIN: at most 16 places, whose parts are added here, in LDS for the block's waves.
 template <bool YB, bool WB, bool ACROSS, int RB, bool JOIN>
 __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
-  typedef Sums<WB, RB> S;
-  __shared__ __align__(16) typename S::T lds[JOIN ? S::kPlanes * 16 * S::kStride : 8];
+  typedef Up<YB, WB, RB> U;
+  typedef Ready<WB> R;
+  constexpr int kRanks = RB ? 16 * RB : 16;
+  __shared__ __align__(16) char lds[JOIN ? 16 * kRanks * R::kBytes : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 15, g = lane >> 4;
   Tile tile;
   if (!find_tile<false>(a.off, a.L, a.T, a.places, blockIdx.x, tile)) return;
-  const int c0 = (blockIdx.y * kUpWaves + wave) * kUpCols;
-  const bool full = c0 + kUpCols <= a.C;
-  const int64_t slab = (int64_t)tile.l * a.r * a.C;
+  const int c0 = (blockIdx.y * kUpWaves + wave) * U::kCols;
+  const bool full = c0 + U::kCols <= a.C;
   const float s = a.scale ? a.scale[tile.l] : 1.f;
   const Places places(a.perm, a.off);
   const auto place = [&](int step) { return places.load(min(tile.lo + 16 * step + i, tile.hi - 1)); };
@@ -677,67 +801,76 @@ __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
     const int p = tile.lo + 16 * step + i, t = places.row(loaded, p);
     return p < tile.hi && (uint32_t)t < (uint32_t)a.T ? t : -1;
   };
-  UpWeights<WB, RB> w;
+  typename U::Weights w;
   if constexpr (JOIN) {
-    const int t = row(place(0), 0);
-    w.template load<ACROSS>(a, slab, c0);
-    Up<YB, WB, RB> v;
-    v.template load_add<false>(a, nullptr, t, c0);
+    U v;
+    v.rows(row(place(0), 0));
+    w.template load<ACROSS>(a, tile.l, c0);
+    v.template load_add<false>(a, nullptr, c0);
     const int n = tile.hi - tile.lo;
-    for (int e = threadIdx.x; e < 16 * a.rp; e += kUpWaves * kWave) {
-      const int p = e / a.rp, rho = e % a.rp;
-      float f = 0.f;
+    for (int e = threadIdx.x; e < 16 * kRanks / 4; e += kUpWaves * kWave) {
+      const int p = e / (kRanks / 4), rho = 4 * (e % (kRanks / 4));
+      floatx4 f = {0.f, 0.f, 0.f, 0.f};
       if (p < n) {
-        f = add_parts(a.part + (int64_t)(tile.lo + p) * a.rp + rho, (int64_t)a.T * a.rp, a.parts);
-        if (a.u && blockIdx.y == 0 && rho < a.r) a.u[(int64_t)(tile.lo + p) * a.r + rho] = f;
+        const float* part = a.part + (int64_t)(tile.lo + p) * a.rp + rho;
+        for (int k = 0; k < a.parts; k += 4) {  // in order, four loads in flight
+          floatx4 q[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) q[j] = *reinterpret_cast<const floatx4*>(part + (int64_t)min(k + j, a.parts - 1) * a.T * a.rp);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (k + j < a.parts) f += q[j];
+        }
+        if (a.u && blockIdx.y == 0) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (rho + k < a.r) a.u[(int64_t)(tile.lo + p) * a.r + rho + k] = f[k];
+        }
       }
-      S::put(lds, 16, p, rho, f);
+      R::put(lds, 16, p, rho, kRanks, f);
     }
     __syncthreads();
-    v.u.load(lds, 16 * S::kStride, i, S::kStride, g);
-    v.template work<false>(a, w, t, c0, s);
+    v.u.load(lds, 16, i, kRanks, g);
+    v.template work<false>(a, w, c0, s);
   } else {
     if (c0 >= a.C) return;
     const int steps = (tile.hi - tile.lo + 15) / 16;
-    const auto load = [&](auto all, Up<YB, WB, RB>& v, int t, int step) {
-      v.template load_add<decltype(all)::value>(a, a.ready, decltype(all)::value ? max(t, 0) : t, c0);
-      v.u.load(static_cast<const typename S::T*>(a.ready), (int64_t)a.T * a.rp, min(tile.lo + 16 * step + i, tile.hi - 1), a.rp, g);
+    const auto load = [&](auto all, U& v, int t, int step) {
+      const int p = tile.lo + 16 * min(step, steps - 1), n = min(16, tile.hi - p);
+      v.u.load(R::group(a.ready, p, a.rp), n, min(i, n - 1), a.rp, g);
+      v.rows(t);
+      v.template load_add<decltype(all)::value>(a, a.ready, c0);
     };
     const std::true_type yes;
     const std::false_type no;
-    if (full && steps > 1) {
-      Up<YB, WB, RB> v[2];
-      int loaded[2] = {place(0), place(1)}, t[2];
-      w.template load<ACROSS>(a, slab, c0);
-      t[0] = row(loaded[0], 0);
-      load(yes, v[0], t[0], 0);
+    constexpr bool kAhead = RB < 8;  // of 128 ranks there are no registers for a second step
+    if (full && kAhead && steps > 1) {
+      U v[2];
+      int loaded[2] = {place(0), place(1)};
+      w.template load<ACROSS>(a, tile.l, c0);
+      load(yes, v[0], row(loaded[0], 0), 0);
       for (int step = 0; step < steps; step += 2) {
         loaded[0] = place(step + 2);
-        t[1] = row(loaded[1], step + 1);
-        load(yes, v[1], t[1], step + 1);
-        v[0].template work<true>(a, w, t[0], c0, s);
-        if (step + 1 >= steps) break;
+        load(yes, v[1], row(loaded[1], step + 1), step + 1);
+        v[0].template work<true>(a, w, c0, s);
         loaded[1] = place(step + 3);
-        t[0] = row(loaded[0], step + 2);
-        load(yes, v[0], t[0], step + 2);
-        v[1].template work<true>(a, w, t[1], c0, s);
+        load(yes, v[0], row(loaded[0], step + 2), step + 2);
+        if (step + 1 < steps) v[1].template work<true>(a, w, c0, s);
       }
       return;
     }
     const int first = place(0);
-    w.template load<ACROSS>(a, slab, c0);
-    if (full) {
-      Up<YB, WB, RB> v;
-      const int t = row(first, 0);
-      load(yes, v, t, 0);
-      v.template work<true>(a, w, t, c0, s);
-      return;
-    }
+    w.template load<ACROSS>(a, tile.l, c0);
     for (int step = 0; step < steps; ++step) {
-      Up<YB, WB, RB> v;
-      const int t = row(place(step), step);
-      load(no, v, t, step);
-      v.template work<false>(a, w, t, c0, s);
+      U v;
+      const int t = row(step ? place(step) : first, step);
+      if (full) {
+        load(yes, v, t, step);
+        v.template work<true>(a, w, c0, s);
+      } else {
+        load(no, v, t, step);
+        v.template work<false>(a, w, c0, s);
+      }
     }
   }
 }
@@ -777,7 +910,7 @@ struct DownPlan {
 inline DownPlan down_plan(int32_t T, int32_t C) {
   DownPlan d;
   d.places = T < kManyRows ? 16 : 32;
-  const int32_t blocks = (T + d.places - 1) / d.places, units = (C + 63) / 64;
+  const int32_t blocks = (T + d.places - 1) / d.places, units = (C + kUnit - 1) / kUnit;
   d.parts = T >= kManyRows ? 1 : std::max(1, std::min(512 / std::max(blocks, 1), (units + kDownWaves - 1) / kDownWaves));
   d.units = (units + d.parts - 1) / d.parts;
   d.parts = (units + d.units - 1) / d.units;
@@ -820,9 +953,11 @@ hipError_t down(DownArgs a, const DownPlan& d, int32_t xdtype, int32_t wdtype, h
 template <bool ACROSS, bool JOIN>
 hipError_t up(UpArgs a, int32_t ydtype, int32_t wdtype, hipStream_t stream) {
   a.places = JOIN || a.T < kManyRows ? 16 : 128;
-  const dim3 grid((unsigned)most_tiles(a.T, a.L, a.places), (a.C + kUpWaves * kUpCols - 1) / (kUpWaves * kUpCols));
+  dim3 grid((unsigned)most_tiles(a.T, a.L, a.places));
   const auto go = [&](auto rb) {
     return by_types(ydtype, wdtype, [&](auto yb, auto wb) {
+      constexpr int kCols = kUpWaves * Up<decltype(yb)::value, decltype(wb)::value, decltype(rb)::value>::kCols;
+      grid.y = (a.C + kCols - 1) / kCols;
       hipLaunchKernelGGL((k_adapter_up<decltype(yb)::value, decltype(wb)::value, ACROSS, decltype(rb)::value, JOIN>), grid,
                          dim3(kUpWaves * kWave), 0, stream, a);
       return hipGetLastError();
@@ -855,7 +990,7 @@ inline size_t most_parts(int32_t T_max, int32_t C, int32_t rp) {
   size_t most = 0;
   for (const int32_t t : {kManyRows - 1, T_max}) {
     const int32_t T = std::min(t, T_max), places = down_plan(T, C).places;
-    const int32_t parts = ((C + 63) / 64 + kDownWaves - 1) / kDownWaves;
+    const int32_t parts = ((C + kUnit - 1) / kUnit + kDownWaves - 1) / kDownWaves;
     most = std::max(most, std::min((size_t)T * parts, std::max<size_t>((size_t)T, (size_t)512 * places)) * rp * 4);
   }
   return up256(most);

@@ -8,7 +8,7 @@ extern "C" {
 size_t damoe_adapters_workspace_size(int32_t T_max, int32_t L, int32_t r, int32_t K, int32_t N) {
   if (check(T_max, L, r, K, N, DAMOE_F32, DAMOE_F32, DAMOE_F32)) return 0;
   const int32_t rp = padded_rank(r);
-  return 256 + std::max(most_parts(T_max, K, rp), ready_bytes(T_max, rp));
+  return 256 + std::max(most_parts(T_max, K, rp), ready_bytes(T_max, rp) + kSpare);
 }
 
 damoe_status damoe_adapters(const void* x, int32_t xdtype, int64_t ldx, const int32_t* perm, const int32_t* offsets, int32_t T,
@@ -25,12 +25,13 @@ damoe_status damoe_adapters(const void* x, int32_t xdtype, int64_t ldx, const in
   const int32_t rp = padded_rank(r);
   const DownPlan d = down_plan(T, K);
   const bool join = T < kManyRows;
-  if (ws_bytes < (join ? part_bytes(d, T, rp) : ready_bytes(T, rp))) return DAMOE_ERR_WORKSPACE;
+  if (ws_bytes < (join ? part_bytes(d, T, rp) : ready_bytes(T, rp) + kSpare)) return DAMOE_ERR_WORKSPACE;
   float* part = join ? static_cast<float*>(ws) : nullptr;
   const DownArgs da{x, ldx, a, perm, offsets, nullptr, part, ws, u, L, T, K, r, rp, 0, 0};
   // `up` takes thirds where the weights are bf16, `down` leaves them there too.
   if (down<false>(da, d, xdtype, wdtype, stream) != hipSuccess) return DAMOE_ERR_HIP;
-  const UpArgs ua{part, ws, d.parts, u, b, scale, perm, offsets, add, ld_add, y, ldy, L, T, N, r, rp, 0};
+  const UpArgs ua{part, ws, d.parts, u, b, scale, perm, offsets, add, ld_add, y, ldy, static_cast<char*>(ws) + ready_bytes(T, rp),
+                  L, T, N, r, rp, 0};
   const hipError_t e = join ? up<false, true>(ua, ydtype, wdtype, stream) : up<false, false>(ua, ydtype, wdtype, stream);
   return e == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
 }

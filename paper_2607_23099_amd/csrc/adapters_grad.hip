@@ -8,47 +8,87 @@ constexpr int kOuterWaves = 4;
 
 // ---------------------------------------------------------------- sums
 
-// u and the joined g of every place for the kernels after it: g by places for `up` (thirds in bf16, or fp32), and both by
-// ranks for `outer`: [3][rp][Tp] thirds in bf16, or [rp][Tp] fp32.
+// Sum of the parts of one value, in order, with eight loads in flight.
+__device__ __forceinline__ float add_parts(const float* p, int64_t apart, int n) {
+  float v = 0.f;
+  for (int k = 0; k < n; k += 8) {
+    float q[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = k + j < n ? p[(k + j) * apart] : 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v += q[j];
+  }
+  return v;
+}
+
+// u and the joined g of every place for the kernels after it: g for `up` (Ready), and both by ranks for `outer`, in pieces of
+// eight places: [piece][3][rp][8] thirds in bf16, or [piece][2][rp][4] fp32.  A segment's places begin with a piece of their own.
 struct SumsArgs {
   const float* part;  // g [parts][T][rp]
   const float* u;     // [T][r]
-  void* ready;
+  const int32_t* off;
+  void* ready;        // or NULL
   void* by_rank[2];   // g, u
   int32_t bf_ready, bf_rank[2];
-  int32_t parts, T, Tp, r, rp;
+  int32_t parts, L, T, r, rp;
 };
 
 constexpr int kSumsPlaces = 32;
 
-__device__ __forceinline__ void put_thirds(void* base, bool bf, int64_t plane, int64_t at, float v) {
-  if (!bf) {
-    static_cast<float*>(base)[at] = v;
-    return;
-  }
-#pragma unroll
-  for (int h = 0; h < 3; ++h) static_cast<uint16_t*>(base)[h * plane + at] = take_third(v);
-}
+// Place of the by-rank pieces that segment l's first place, lo, has; and the pieces that there are of T places.
+__host__ __device__ __forceinline__ int first_by_rank(int lo, int l) { return (lo + 7) / 8 * 8 + 16 * l; }
+inline size_t pieces_by_rank(int32_t T, int32_t L) { return (size_t)(T + 7) / 8 + 2 * L + 8; }  // loads go up to 31 places past the last
 
 __global__ void __launch_bounds__(256) k_adapter_sums(SumsArgs a) {
-  __shared__ float tile[kMaxRank][kSumsPlaces + 1];
-  const int p0 = blockIdx.x * kSumsPlaces, which = blockIdx.y, n = min(kSumsPlaces, a.T - p0);
-  for (int e = threadIdx.x; e < n * a.rp; e += 256) {
-    const int p = e / a.rp, rho = e - p * a.rp;
-    float v = 0.f;
-    if (which == 0) {
-      const int64_t at = (int64_t)(p0 + p) * a.rp + rho;
-      v = add_parts(a.part + at, (int64_t)a.T * a.rp, a.parts);
-      if (a.ready) put_thirds(a.ready, a.bf_ready, (int64_t)a.T * a.rp, at, v);
-    } else if (rho < a.r) {
-      v = a.u[(int64_t)(p0 + p) * a.r + rho];
+  __shared__ float lds[kMaxRank][kSumsPlaces + 1];
+  const int which = blockIdx.y, quads = a.rp / 4;
+  Tile tile;
+  if (!find_tile<false>(a.off, a.L, a.T, kSumsPlaces, blockIdx.x, tile)) return;
+  const int n = tile.hi - tile.lo;
+  for (int e = threadIdx.x; e < kSumsPlaces * quads; e += 256) {
+    const int p = e / quads, rho = 4 * (e - p * quads);
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    if (p < n && which == 0) {
+      const float* part = a.part + (int64_t)(tile.lo + p) * a.rp + rho;
+      for (int k = 0; k < a.parts; ++k) v += *reinterpret_cast<const floatx4*>(part + (int64_t)k * a.T * a.rp);
+      if (a.ready) {
+        const int i = p % 16, first = tile.lo + p - i, m = min(16, tile.hi - first);
+        if (a.bf_ready) Ready<true>::put(Ready<true>::group(a.ready, first, a.rp), m, i, rho, a.rp, v);
+        else Ready<false>::put(Ready<false>::group(a.ready, first, a.rp), m, i, rho, a.rp, v);
+      }
+    } else if (p < n) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (rho + k < a.r) v[k] = a.u[(int64_t)(tile.lo + p) * a.r + rho + k];
     }
-    tile[rho][p] = v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) lds[rho + k][p] = v[k];
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < kSumsPlaces * a.rp; e += 256) {
-    const int p = e % kSumsPlaces, rho = e / kSumsPlaces;
-    if (p < n) put_thirds(a.by_rank[which], a.bf_rank[which], (int64_t)a.rp * a.Tp, (int64_t)rho * a.Tp + p0 + p, tile[rho][p]);
+  const int64_t piece = (first_by_rank(tile.lo - tile.index * kSumsPlaces, tile.l) + tile.index * kSumsPlaces) / 8;
+  for (int e = threadIdx.x; e < kSumsPlaces / 8 * a.rp; e += 256) {
+    const int b = e / a.rp, rho = e - b * a.rp;
+    if (8 * b >= n) break;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = lds[rho][8 * b + k];
+    uint4* out = static_cast<uint4*>(a.by_rank[which]) + (piece + b) * (a.bf_rank[which] ? 3 : 2) * a.rp + rho;
+    if (a.bf_rank[which]) {
+#pragma unroll
+      for (int h = 0; h < 3; ++h) {
+        uint32_t q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t lo = take_third(v[2 * k]);
+          q[k] = lo | (uint32_t)take_third(v[2 * k + 1]) << 16;
+        }
+        out[h * a.rp] = uint4{q[0], q[1], q[2], q[3]};
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        out[h * a.rp] = uint4{__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]), __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])};
+    }
   }
 }
 
@@ -63,7 +103,7 @@ struct OuterArgs {
   const int32_t* off;
   float* out;          // dA [L][r][C], or dB [L][C][r]
   float* slots;        // parts of segments of several chunks, laid out as the output
-  int32_t L, T, Tp, C, r, rp, chunk, accumulate;
+  int32_t L, T, C, r, rp, chunk, accumulate;
 };
 
 template <bool BF>
@@ -82,10 +122,10 @@ __device__ __forceinline__ bool counts(uint32_t mask, int g, int k) { return mas
 // MFMA j has column P i + j as row i.  The next step's rows are loaded while one is multiplied.  Lanes past the last column
 // take the last P again; SMALL: there are fewer than P, each is loaded for itself.
 template <bool BF, bool ACROSS, int RB, bool SMALL>
-__global__ void __launch_bounds__(kOuterWaves* kWave, BF && RB > 1 ? 1 : 2) k_adapter_outer(OuterArgs a) {
+__global__ void __launch_bounds__(kOuterWaves* kWave, 2) k_adapter_outer(OuterArgs a) {
   typedef OuterTile<BF> O;
   typedef typename Elem<BF>::T X;
-  constexpr int P = O::kPer, F = BF ? 3 : 1;
+  constexpr int P = O::kPer, F = BF ? 3 : 2;
   constexpr int kPlane = 64 * 4 + 4;  // floats of a wave's MFMA in LDS
   __shared__ __align__(16) float sums[kOuterWaves * P * kPlane];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -101,12 +141,13 @@ __global__ void __launch_bounds__(kOuterWaves* kWave, BF && RB > 1 ? 1 : 2) k_ad
     for (int rb = 0; rb < RB; ++rb) acc[j][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
   struct Rows {
     uint4 v[8];
-    Raw<BF> u[RB][F];
+    uint4 u[RB][F];
     uint32_t mask;  // of places
   };
   const Places places(a.perm, a.off);
   constexpr int kStep = 32 * kOuterWaves;
   const int first = tile.lo + 32 * wave, steps = first < tile.hi ? (tile.hi - first + kStep - 1) / kStep : 0;
+  const int begin = tile.lo - tile.index * a.chunk, shift = first_by_rank(begin, tile.l) - begin;
   const auto at = [&](int s) { return first + min(s, steps - 1) * kStep; };
   // Lane by lane the row of place p + lane % 32.
   const auto place = [&](int s) { return places.load(min(at(s) + (lane & 31), tile.hi - 1)); };
@@ -128,7 +169,8 @@ __global__ void __launch_bounds__(kOuterWaves* kWave, BF && RB > 1 ? 1 : 2) k_ad
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-      for (int h = 0; h < F; ++h) s.u[rb][h].load(a.by_rank, ((int64_t)h * a.rp + r0 + 16 * rb + i) * a.Tp + p + 8 * g);
+      for (int h = 0; h < F; ++h)
+        s.u[rb][h] = static_cast<const uint4*>(a.by_rank)[((int64_t)((p + shift) / 8 + g) * F + h) * a.rp + r0 + 16 * rb + i];
   };
   const auto work = [&](Rows& s) {
     if (s.mask != ~0u) {  // nothing of places that do not count: their rows are others', their factors were never written
@@ -138,34 +180,37 @@ __global__ void __launch_bounds__(kOuterWaves* kWave, BF && RB > 1 ? 1 : 2) k_ad
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int h = 0; h < F; ++h)
+        for (int h = 0; h < F; ++h) {
+          uint32_t* q = reinterpret_cast<uint32_t*>(&s.u[rb][h]);
 #pragma unroll
-          for (int d = 0; d < (BF ? 4 : 8); ++d) {
-            if constexpr (BF) s.u[rb][h].q[d] &= (counts(s.mask, g, 2 * d) ? 0xFFFFu : 0u) | (counts(s.mask, g, 2 * d + 1) ? 0xFFFF0000u : 0u);
-            else s.u[rb][h].q[d] = counts(s.mask, g, d) ? s.u[rb][h].q[d] : 0u;
+          for (int d = 0; d < 4; ++d) {
+            if constexpr (BF) q[d] &= (counts(s.mask, g, 2 * d) ? 0xFFFFu : 0u) | (counts(s.mask, g, 2 * d + 1) ? 0xFFFF0000u : 0u);
+            else q[d] = counts(s.mask, g, 4 * h + d) ? q[d] : 0u;
           }
+        }
     }
     if constexpr (BF) {
       // Dword d of place k holds its columns 2 d and 2 d + 1; operand j wants column j of all places.
+      uint4 x[P];
 #pragma unroll
       for (int d = 0; d < P / 2; ++d) {
-        uint32_t q[8];
+        uint32_t q[8], lo[4], hi[4];
 #pragma unroll
         for (int k = 0; k < 8; ++k) q[k] = d == 0 ? s.v[k].x : d == 1 ? s.v[k].y : d == 2 ? s.v[k].z : s.v[k].w;
-        Frag<true> lo, hi;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          lo.q[k] = __builtin_amdgcn_perm(q[2 * k + 1], q[2 * k], 0x05040100u);
-          hi.q[k] = __builtin_amdgcn_perm(q[2 * k + 1], q[2 * k], 0x07060302u);
+          lo[k] = __builtin_amdgcn_perm(q[2 * k + 1], q[2 * k], 0x05040100u);
+          hi[k] = __builtin_amdgcn_perm(q[2 * k + 1], q[2 * k], 0x07060302u);
         }
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int h = 0; h < F; ++h) {
-            acc[2 * d][rb] = mma(lo, frag<true>(s.u[rb][h]), acc[2 * d][rb]);
-            acc[2 * d + 1][rb] = mma(hi, frag<true>(s.u[rb][h]), acc[2 * d + 1][rb]);
-          }
+        x[2 * d] = uint4{lo[0], lo[1], lo[2], lo[3]}, x[2 * d + 1] = uint4{hi[0], hi[1], hi[2], hi[3]};
       }
+      // A sum's instructions are P RB apart, longer than one takes.
+#pragma unroll
+      for (int h = 0; h < F; ++h)
+#pragma unroll
+        for (int j = 0; j < P; ++j)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) acc[j][rb] = mfma16x16x32(x[j], s.u[rb][h], acc[j][rb]);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -173,7 +218,7 @@ __global__ void __launch_bounds__(kOuterWaves* kWave, BF && RB > 1 ? 1 : 2) k_ad
 #pragma unroll
         for (int j = 0; j < P; ++j)
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb) acc[j][rb] = mma4(q[j], s.u[rb][0].q[k], acc[j][rb]);
+          for (int rb = 0; rb < RB; ++rb) acc[j][rb] = mma4(q[j], reinterpret_cast<const uint32_t*>(&s.u[rb][k / 4])[k % 4], acc[j][rb]);
       }
     }
   };
@@ -189,10 +234,9 @@ __global__ void __launch_bounds__(kOuterWaves* kWave, BF && RB > 1 ? 1 : 2) k_ad
       loaded[0] = place(step + 2);
       load(s[1], loaded[1], step + 1);
       work(s[0]);
-      if (step + 1 >= steps) break;
       loaded[1] = place(step + 3);
       load(s[0], loaded[0], step + 2);
-      work(s[1]);
+      if (step + 1 < steps) work(s[1]);
     }
   }
   // The waves' sums in order, through LDS, where threads side by side take elements side by side of the output.  Lane (i, g)
@@ -256,7 +300,7 @@ int32_t outer_chunk(int32_t T, int32_t C, int32_t dtype) {
   const int32_t cols = dtype == DAMOE_BF16 ? OuterTile<true>::kCols : OuterTile<false>::kCols;
   const int32_t tiles = (C + cols - 1) / cols;
   const int32_t chunks = std::max(1, std::min((T + 127) / 128, 512 / tiles));
-  return (T + chunks - 1) / chunks;
+  return ((T + chunks - 1) / chunks + 31) / 32 * 32;  // whole steps
 }
 
 // Slots of `outer`: a segment of n > 1 chunks has more than (n - 1) chunk places, so n is at most twice the chunks they fill.
@@ -283,11 +327,8 @@ hipError_t outer(const OuterArgs& a, int32_t dtype, bool across, hipStream_t str
   return across ? ranked(false_type{}, true_type{}) : ranked(false_type{}, false_type{});
 }
 
-// Rows of what `sums` lays out by ranks: loads of `outer` go up to 31 places past the last.
-int32_t row_by_rank(int32_t T) { return (T + 7) / 8 * 8 + 64; }
-
 // By ranks; slots.
-size_t rank_bytes(int32_t T, int32_t rp) { return up256((size_t)row_by_rank(T) * rp * 6); }
+size_t rank_bytes(int32_t T, int32_t L, int32_t rp) { return up256(pieces_by_rank(T, L) * rp * 48); }
 size_t slot_bytes(int64_t slots, int32_t r, int32_t C) { return up256((size_t)slots * r * C * 4); }
 
 // The most that slots_of is: there are never more chunks than 128-place ones, nor than the blocks allow.
@@ -306,7 +347,7 @@ extern "C" {
 size_t damoe_adapters_grad_workspace_size(int32_t T_max, int32_t L, int32_t r, int32_t K, int32_t N) {
   if (check(T_max, L, r, K, N, DAMOE_F32, DAMOE_F32, DAMOE_F32)) return 0;
   const int32_t rp = padded_rank(r);
-  return 256 + most_parts(T_max, N, rp) + ready_bytes(T_max, rp) + 2 * rank_bytes(T_max, rp) + slot_bytes(most_slots(T_max, K), r, K) +
+  return 256 + most_parts(T_max, N, rp) + ready_bytes(T_max, rp) + kSpare + 2 * rank_bytes(T_max, L, rp) + slot_bytes(most_slots(T_max, K), r, K) +
          slot_bytes(most_slots(T_max, N), r, N);
 }
 
@@ -338,25 +379,25 @@ damoe_status damoe_adapters_grad(const void* x, int32_t xdtype, int64_t ldx, con
     };
     float* part = reinterpret_cast<float*>(piece(part_bytes(d, T, rp)));
     void* ready = piece(ready_bytes(T, rp));
-    void* g_rank = piece(rank_bytes(T, rp));
-    void* u_rank = piece(rank_bytes(T, rp));
+    char* spare = piece(kSpare);
+    void* g_rank = piece(rank_bytes(T, L, rp));
+    void* u_rank = piece(rank_bytes(T, L, rp));
     slots_a = reinterpret_cast<float*>(piece(slot_bytes(slots_of(T, ck), r, K)));
     slots_b = reinterpret_cast<float*>(piece(slot_bytes(slots_of(T, cn), r, N)));
     if (ws_bytes < end) return DAMOE_ERR_WORKSPACE;
-    const int32_t Tp = row_by_rank(T);
     const DownArgs ga{dy, ldy, b, perm, offsets, scale, part, nullptr, nullptr, L, T, N, r, rp, 0, 0};
     if (down<true>(ga, d, ydtype, wdtype, stream) != hipSuccess) return DAMOE_ERR_HIP;
-    const SumsArgs sa{part, u, dx ? ready : nullptr, {g_rank, u_rank}, wdtype == DAMOE_BF16, {xdtype == DAMOE_BF16, ydtype == DAMOE_BF16},
-                      d.parts, T, Tp, r, rp};
-    hipLaunchKernelGGL(k_adapter_sums, dim3((T + kSumsPlaces - 1) / kSumsPlaces, 2), dim3(256), 0, stream, sa);
+    const SumsArgs sa{part, u, offsets, dx ? ready : nullptr, {g_rank, u_rank}, wdtype == DAMOE_BF16,
+                      {xdtype == DAMOE_BF16, ydtype == DAMOE_BF16}, d.parts, L, T, r, rp};
+    hipLaunchKernelGGL(k_adapter_sums, dim3((unsigned)most_tiles(T, L, kSumsPlaces), 2), dim3(256), 0, stream, sa);
     if (hipGetLastError() != hipSuccess) return DAMOE_ERR_HIP;
     // dB first: it reads what `down` has just read.
-    const OuterArgs ob{dy, ldy, u_rank, scale, perm, offsets, db, slots_b, L, T, Tp, N, r, rp, cn, accumulate};
+    const OuterArgs ob{dy, ldy, u_rank, scale, perm, offsets, db, slots_b, L, T, N, r, rp, cn, accumulate};
     if (outer(ob, ydtype, true, stream) != hipSuccess) return DAMOE_ERR_HIP;
-    const OuterArgs oa{x, ldx, g_rank, nullptr, perm, offsets, da, slots_a, L, T, Tp, K, r, rp, ck, accumulate};
+    const OuterArgs oa{x, ldx, g_rank, nullptr, perm, offsets, da, slots_a, L, T, K, r, rp, ck, accumulate};
     if (outer(oa, xdtype, false, stream) != hipSuccess) return DAMOE_ERR_HIP;
     if (dx) {
-      const UpArgs xa{nullptr, ready, 1, nullptr, a, nullptr, perm, offsets, add, ld_add, dx, ld_dx, L, T, K, r, rp, 0};
+      const UpArgs xa{nullptr, ready, 1, nullptr, a, nullptr, perm, offsets, add, ld_add, dx, ld_dx, spare, L, T, K, r, rp, 0};
       if (up<true, false>(xa, xdtype, wdtype, stream) != hipSuccess) return DAMOE_ERR_HIP;
     }
   }
