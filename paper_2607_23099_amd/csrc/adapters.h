@@ -177,7 +177,7 @@ struct Rows16 {
   static __device__ __forceinline__ int mine(int h) { return (threadIdx.x >> 2 & 3) * 4 + h; }
 
   // at(h): the first element of row mine(h); c: the unit's first column.
-  template <class F>
+  template <bool NT = false, class F>
   __device__ __forceinline__ void load(const void* base, F at, int c) {
     typedef Elem<SRC> E;
     const int g = (threadIdx.x & 63) >> 4, a = threadIdx.x & 3;
@@ -185,7 +185,7 @@ struct Rows16 {
     for (int s = 0; s < kSets; ++s)
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        const uint4 v = load16_at<E::kBytes>(static_cast<const typename E::T*>(base) + (at(h) + (c + 32 * g + (4 * s + a) * E::kPer16)));
+        const uint4 v = load16_at<E::kBytes, NT>(static_cast<const typename E::T*>(base) + (at(h) + (c + 32 * g + (4 * s + a) * E::kPer16)));
         uint32_t(&d)[4] = q[4 * s + h];
         d[0] = v.x, d[1] = v.y, d[2] = v.z, d[3] = v.w;
       }
@@ -399,7 +399,7 @@ struct Down {
       const auto load = [&](Unit& v, int u) {
         v.w.template load<true>(a, slab, r0, u * kUnit, kUnit);
 #pragma unroll
-        for (int m = 0; m < M; ++m) v.x[m].load(a.x, [&](int h) { return rows[m][h]; }, u * kUnit);
+        for (int m = 0; m < M; ++m) v.x[m].template load<LIE == kRows>(a.x, [&](int h) { return rows[m][h]; }, u * kUnit);
       };
       Unit v[D];
       int u = u0 + wave;
@@ -412,6 +412,7 @@ struct Down {
           exchange(v[d]);
           multiply(v[d], second);
           load(v[d], u);
+          __builtin_amdgcn_sched_barrier(0);  // or the loads are put behind the next unit's work
         }
       }
 #pragma unroll
@@ -599,7 +600,7 @@ struct Sums {
   }
 };
 
-// N elements side by side, 8 or 16 bytes.
+// N elements side by side, of 8 to 32 bytes (stores: up to 16).
 template <bool YB, int N>
 struct Side {
   typedef Elem<YB> E;
@@ -607,9 +608,12 @@ struct Side {
   uint32_t q[kWords];
 
   __device__ __forceinline__ void load(const typename E::T* p) {
-    if constexpr (kWords == 4) {
-      const uint4 v = load16_at<E::kBytes>(p);
-      q[0] = v.x, q[1] = v.y, q[2] = v.z, q[3] = v.w;
+    if constexpr (kWords >= 4) {
+#pragma unroll
+      for (int h = 0; h < kWords; h += 4) {
+        const uint4 v = load16_at<E::kBytes>(p + h / 4 * E::kPer16);
+        q[h] = v.x, q[h + 1] = v.y, q[h + 2] = v.z, q[h + 3] = v.w;
+      }
     } else {
       __builtin_memcpy(q, p, sizeof q);
     }
@@ -699,6 +703,28 @@ struct Up {
     __device__ __forceinline__ void load(const UpArgs& a, int l, int c0) {
       const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
       const int64_t slab = (int64_t)l * a.r * a.C;
+      if (ACROSS && c0 + kCols <= a.C) {  // the lane's columns of a rank are side by side
+#pragma unroll
+        for (int kb = 0; kb < S::kBlocks; ++kb) {
+          const int rho = S::rank(kb, g), n = a.r - rho;
+          Side<WB, NB> v[S::kPer];
+#pragma unroll
+          for (int j = 0; j < S::kPer; ++j)
+            v[j].load(static_cast<const typename Elem<WB>::T*>(a.w) + slab + (int64_t)(rho + min(j, n - 1)) * a.C + c0 + NB * i);
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < S::kWords; ++e) {
+              if constexpr (WB) {
+                const uint32_t two = __builtin_amdgcn_perm(v[2 * e + 1].q[b / 2], v[2 * e].q[b / 2], b & 1 ? 0x07060302u : 0x05040100u);
+                q[b][kb][e] = two & ((2 * e < n ? 0xFFFFu : 0u) | (2 * e + 1 < n ? 0xFFFF0000u : 0u));
+              } else {
+                q[b][kb][e] = e < n ? v[e].q[b] : 0u;
+              }
+            }
+        }
+        return;
+      }
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const int c = min(c0 + NB * i + b, a.C - 1);
