@@ -350,7 +350,7 @@ struct Down {
     Rows16<XB> x[M];
     Weights<WB, LIE, RB> w;
   };
-  static constexpr int kRegs = sizeof(Unit) / 4, D = kRegs <= 32 ? 3 : kRegs <= 72 ? 2 : 1;
+  static constexpr int kRegs = sizeof(Unit) / 4, D = W > 8 ? (kRegs <= 32 ? 2 : 1) : kRegs <= 32 ? 3 : kRegs <= 72 ? 2 : 1;
   floatx4 acc[M][RB];
 
   __device__ __forceinline__ void multiply(const Unit& v, bool second) {
@@ -699,10 +699,79 @@ struct Up {
       for (int e = 0; e < S::kWords; ++e) q[e] = WB ? v[2 * e % S::kPer] | v[(2 * e + 1) % S::kPer] << 16 : v[e % S::kPer];
     }
 
+    // Columns of ranks: 16 lanes that load from a column each would cost the address units 16 times.  The wave reads runs of
+    // the lanes' columns, 256 bytes from 16 lanes, and its operands come from LDS; CB of a lane's NB columns at a time.
+    static constexpr int kPadded = WB ? (RB ? 16 * RB : 8) : 4 * S::kPer, kColumn = kPadded * Elem<WB>::kBytes;
+    static constexpr bool kStaged = kColumn <= 256;
+    static constexpr int CB = kColumn * NB <= 256 ? NB : 256 / kColumn, kRun = CB * kColumn + 16;  // 16 bytes against bank conflicts
+    static constexpr int kLds = kStaged ? 16 * kRun : 16;  // bytes of a wave
+
+    __device__ __forceinline__ void load_runs(const UpArgs& a, int64_t slab, int c0, char* lds) {
+      typedef Elem<WB> F;
+      typedef typename F::T T;
+      const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+      const T* w = static_cast<const T*>(a.w) + slab + (int64_t)c0 * a.r;
+#pragma unroll
+      for (int b0 = 0; b0 < NB; b0 += CB) {
+        if (a.r % F::kPer16 == 0) {
+          const int pieces = a.r / F::kPer16, run = CB * pieces;  // of 16 bytes; at most 16 a run
+          const float per_run = 1.f / run, per_column = 1.f / pieces;
+          uint4 v[4];
+          int to[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {  // past the last one that one again
+            const int e = min(64 * y + lane, 16 * run - 1);
+            const int lane_of = (int)((e + 0.5f) * per_run), k = e - lane_of * run, column = (int)((k + 0.5f) * per_column);
+            v[y] = load16_at<F::kBytes>(w + (NB * lane_of + b0) * a.r + k * F::kPer16);
+            to[y] = lane_of * kRun + column * kColumn + (k - column * pieces) * 16;
+          }
+#pragma unroll
+          for (int y = 0; y < 4; ++y) *reinterpret_cast<uint4*>(lds + to[y]) = v[y];
+        } else {
+          const int run = CB * a.r;
+#pragma unroll 4
+          for (int e = lane; e < 16 * run; e += 64) {
+            const int lane_of = e / run, k = e - lane_of * run, column = k / a.r;
+            *reinterpret_cast<T*>(lds + lane_of * kRun + column * kColumn + (k - column * a.r) * F::kBytes) =
+                w[(NB * lane_of + b0) * a.r + k];
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int b = 0; b < CB; ++b)
+#pragma unroll
+          for (int kb = 0; kb < S::kBlocks; ++kb) {
+            const int rho = S::rank(kb, g), n = a.r - rho;
+            uint32_t(&d)[S::kWords] = q[b0 + b][kb];
+            const char* from = lds + i * kRun + b * kColumn + rho * F::kBytes;
+            if constexpr (S::kWords == 2) {
+              const uint2 v = *reinterpret_cast<const uint2*>(from);
+              d[0] = v.x, d[1] = v.y;
+            } else {
+#pragma unroll
+              for (int e = 0; e < S::kWords; e += 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(from + 4 * e);
+                d[e] = v.x, d[e + 1] = v.y, d[e + 2] = v.z, d[e + 3] = v.w;
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < S::kWords; ++e) {
+              if constexpr (WB) d[e] &= (2 * e < n ? 0xFFFFu : 0u) | (2 * e + 1 < n ? 0xFFFF0000u : 0u);
+              else d[e] = e < n ? d[e] : 0u;
+            }
+          }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+
+    // lds: kLds bytes of the wave.
     template <bool ACROSS>
-    __device__ __forceinline__ void load(const UpArgs& a, int l, int c0) {
+    __device__ __forceinline__ void load(const UpArgs& a, int l, int c0, char* lds) {
       const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
       const int64_t slab = (int64_t)l * a.r * a.C;
+      if constexpr (!ACROSS && kStaged) {
+        if (c0 + kCols <= a.C) return load_runs(a, slab, c0, lds);
+      }
       if (ACROSS && c0 + kCols <= a.C) {  // the lane's columns of a rank are side by side
 #pragma unroll
         for (int kb = 0; kb < S::kBlocks; ++kb) {
@@ -814,6 +883,7 @@ __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
   typedef Ready<WB> R;
   constexpr int kRanks = RB ? 16 * RB : 16;
   __shared__ __align__(16) char lds[JOIN ? 16 * kRanks * R::kBytes : 16];
+  __shared__ __align__(16) char runs[ACROSS ? 16 : kUpWaves * U::Weights::kLds];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 15, g = lane >> 4;
   Tile tile;
@@ -828,10 +898,11 @@ __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
     return p < tile.hi && (uint32_t)t < (uint32_t)a.T ? t : -1;
   };
   typename U::Weights w;
+  char* mine = runs + (ACROSS ? 0 : wave * U::Weights::kLds);
   if constexpr (JOIN) {
     U v;
     v.rows(row(place(0), 0));
-    w.template load<ACROSS>(a, tile.l, c0);
+    w.template load<ACROSS>(a, tile.l, c0, mine);
     v.template load_add<false>(a, nullptr, c0);
     const int n = tile.hi - tile.lo;
     for (int e = threadIdx.x; e < 16 * kRanks / 4; e += kUpWaves * kWave) {
@@ -873,7 +944,7 @@ __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
     if (full && kAhead && steps > 1) {
       U v[2];
       int loaded[2] = {place(0), place(1)};
-      w.template load<ACROSS>(a, tile.l, c0);
+      w.template load<ACROSS>(a, tile.l, c0, mine);
       load(yes, v[0], row(loaded[0], 0), 0);
       for (int step = 0; step < steps; step += 2) {
         loaded[0] = place(step + 2);
@@ -886,7 +957,7 @@ __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
       return;
     }
     const int first = place(0);
-    w.template load<ACROSS>(a, tile.l, c0);
+    w.template load<ACROSS>(a, tile.l, c0, mine);
     for (int step = 0; step < steps; ++step) {
       U v;
       const int t = row(step ? place(step) : first, step);
