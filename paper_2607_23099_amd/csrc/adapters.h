@@ -18,6 +18,7 @@
 // step between, so that its value is there when the next rows are asked for.
 #pragma once
 
+#include "adapters_args.h"
 #include "vec.h"
 
 namespace damoe {
@@ -261,21 +262,6 @@ __device__ __forceinline__ uint16_t take_third(float& v) {
 // How the weights lie for `down`: rows of columns (A), or columns of ranks (B), there read one rank a lane, or (bf16, r even)
 // two side by side, which are the same row of two blocks of 16 ranks.
 enum Lie { kRows, kAcross, kPairs };
-
-struct DownArgs {
-  const void* x;   // rows that are contracted (x, dy)
-  int64_t ldx;
-  const void* w;   // A [L][r][C], or B [L][C][r]
-  const int32_t* perm;
-  const int32_t* off;
-  const float* scale;  // of a segment's sums, or NULL
-  float* part;     // [parts][T][rp], or NULL: with one part, what `up` takes and u are written
-  void* ready;     // Ready, groups of places from each segment's first on
-  float* u;        // [T][r] or NULL
-  int32_t L, T, C, r, rp;
-  int32_t places;  // of a block
-  int32_t units;   // of columns that a block takes
-};
 
 // A unit of columns of RB blocks of 16 ranks from r0 on, lane (i, g)'s columns as those of Rows16.
 template <bool WB, Lie LIE, int RB>
@@ -537,23 +523,6 @@ __global__ void __launch_bounds__(kDownWaves* kWave) k_adapter_down(DownArgs a) 
 }
 
 // ---------------------------------------------------------------- up
-
-struct UpArgs {
-  const float* part;  // [parts][T][rp] (JOIN), joined here
-  void* ready;        // else: Ready
-  int32_t parts;
-  float* u;           // JOIN: NULL, or the joined sums [T][r]
-  const void* w;      // B [L][C][r], or A [L][r][C]
-  const float* scale;
-  const int32_t* perm;
-  const int32_t* off;
-  const void* add;
-  int64_t lda;
-  void* y;
-  int64_t ldy;
-  char* spare;        // not JOIN: kSpare bytes that nothing reads
-  int32_t L, T, C, r, rp, places;
-};
 
 constexpr size_t kSpare = 64 * 16;
 
@@ -876,13 +845,70 @@ struct Up {
   }
 };
 
-// JOIN: at most 16 places, whose parts are added here, in LDS for the block's waves.
-template <bool YB, bool WB, bool ACROSS, int RB, bool JOIN>
+// A tile of at most 16 places whose parts are added here, in LDS for the block's waves; c0: the wave's columns.  `first`: the
+// block that keeps u.
+template <bool YB, bool WB, bool ACROSS, int RB>
+struct UpJoin {
+  typedef Up<YB, WB, RB> U;
+  typedef Ready<WB> R;
+  static constexpr int kRanks = RB ? 16 * RB : 16, kSums = 16 * kRanks * R::kBytes;
+  static constexpr int kRuns = ACROSS ? 0 : U::Weights::kLds;  // bytes of LDS for a wave, behind kSums of the block
+
+  static __device__ __forceinline__ void run(const UpArgs& a, const Tile& tile, int c0, bool first, char* lds) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = lane & 15, g = lane >> 4;
+    const float s = a.scale ? a.scale[tile.l] : 1.f;
+    const Places places(a.perm, a.off);
+    const int p = min(tile.lo + i, tile.hi - 1), row = places.row(places.load(p), p);
+    U v;
+    typename U::Weights w;
+    if (c0 < a.C) {
+      w.template load<ACROSS>(a, tile.l, c0, lds + kSums + wave * kRuns);
+      v.rows(tile.lo + i < tile.hi && (uint32_t)row < (uint32_t)a.T ? row : -1);
+      v.template load_add<false>(a, nullptr, c0);
+    }
+    const int n = tile.hi - tile.lo;
+    for (int e = threadIdx.x; e < 16 * kRanks / 4; e += kUpWaves * kWave) {
+      const int at = e / (kRanks / 4), rho = 4 * (e % (kRanks / 4));
+      floatx4 f = {0.f, 0.f, 0.f, 0.f};
+      if (at < n) {
+        const float* part = a.part + (int64_t)(tile.lo + at) * a.rp + rho;
+        for (int k = 0; k < a.parts; k += 4) {  // in order, four loads in flight
+          floatx4 q[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) q[j] = *reinterpret_cast<const floatx4*>(part + (int64_t)min(k + j, a.parts - 1) * a.T * a.rp);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (k + j < a.parts) f += q[j];
+        }
+        if (a.u && first) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (rho + k < a.r) a.u[(int64_t)(tile.lo + at) * a.r + rho + k] = f[k];
+        }
+      }
+      R::put(lds, 16, at, rho, kRanks, f);
+    }
+    __syncthreads();
+    if (c0 >= a.C) return;
+    v.u.load(lds, 16, i, kRanks, g);
+    v.template work<false>(a, w, c0, s);
+  }
+};
+
+template <bool YB, bool WB, int RB>
+__global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up_join(UpArgs a) {
+  typedef UpJoin<YB, WB, false, RB> J;
+  __shared__ __align__(16) char lds[J::kSums + kUpWaves * J::kRuns];
+  Tile tile;
+  if (!find_tile<false>(a.off, a.L, a.T, a.places, blockIdx.x, tile)) return;
+  J::run(a, tile, (blockIdx.y * kUpWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * J::U::kCols, blockIdx.y == 0, lds);
+}
+
+template <bool YB, bool WB, bool ACROSS, int RB>
 __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
   typedef Up<YB, WB, RB> U;
   typedef Ready<WB> R;
-  constexpr int kRanks = RB ? 16 * RB : 16;
-  __shared__ __align__(16) char lds[JOIN ? 16 * kRanks * R::kBytes : 16];
   __shared__ __align__(16) char runs[ACROSS ? 16 : kUpWaves * U::Weights::kLds];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 15, g = lane >> 4;
@@ -899,75 +925,43 @@ __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
   };
   typename U::Weights w;
   char* mine = runs + (ACROSS ? 0 : wave * U::Weights::kLds);
-  if constexpr (JOIN) {
+  if (c0 >= a.C) return;
+  const int steps = (tile.hi - tile.lo + 15) / 16;
+  const auto load = [&](auto all, U& v, int t, int step) {
+    const int p = tile.lo + 16 * min(step, steps - 1), n = min(16, tile.hi - p);
+    v.u.load(R::group(a.ready, p, a.rp), n, min(i, n - 1), a.rp, g);
+    v.rows(t);
+    v.template load_add<decltype(all)::value>(a, a.ready, c0);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  constexpr bool kAhead = RB < 8;  // of 128 ranks there are no registers for a second step
+  if (full && kAhead && steps > 1) {
+    U v[2];
+    int loaded[2] = {place(0), place(1)};
+    w.template load<ACROSS>(a, tile.l, c0, mine);
+    load(yes, v[0], row(loaded[0], 0), 0);
+    for (int step = 0; step < steps; step += 2) {
+      loaded[0] = place(step + 2);
+      load(yes, v[1], row(loaded[1], step + 1), step + 1);
+      v[0].template work<true>(a, w, c0, s);
+      loaded[1] = place(step + 3);
+      load(yes, v[0], row(loaded[0], step + 2), step + 2);
+      if (step + 1 < steps) v[1].template work<true>(a, w, c0, s);
+    }
+    return;
+  }
+  const int first = place(0);
+  w.template load<ACROSS>(a, tile.l, c0, mine);
+  for (int step = 0; step < steps; ++step) {
     U v;
-    v.rows(row(place(0), 0));
-    w.template load<ACROSS>(a, tile.l, c0, mine);
-    v.template load_add<false>(a, nullptr, c0);
-    const int n = tile.hi - tile.lo;
-    for (int e = threadIdx.x; e < 16 * kRanks / 4; e += kUpWaves * kWave) {
-      const int p = e / (kRanks / 4), rho = 4 * (e % (kRanks / 4));
-      floatx4 f = {0.f, 0.f, 0.f, 0.f};
-      if (p < n) {
-        const float* part = a.part + (int64_t)(tile.lo + p) * a.rp + rho;
-        for (int k = 0; k < a.parts; k += 4) {  // in order, four loads in flight
-          floatx4 q[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) q[j] = *reinterpret_cast<const floatx4*>(part + (int64_t)min(k + j, a.parts - 1) * a.T * a.rp);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (k + j < a.parts) f += q[j];
-        }
-        if (a.u && blockIdx.y == 0) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (rho + k < a.r) a.u[(int64_t)(tile.lo + p) * a.r + rho + k] = f[k];
-        }
-      }
-      R::put(lds, 16, p, rho, kRanks, f);
-    }
-    __syncthreads();
-    v.u.load(lds, 16, i, kRanks, g);
-    v.template work<false>(a, w, c0, s);
-  } else {
-    if (c0 >= a.C) return;
-    const int steps = (tile.hi - tile.lo + 15) / 16;
-    const auto load = [&](auto all, U& v, int t, int step) {
-      const int p = tile.lo + 16 * min(step, steps - 1), n = min(16, tile.hi - p);
-      v.u.load(R::group(a.ready, p, a.rp), n, min(i, n - 1), a.rp, g);
-      v.rows(t);
-      v.template load_add<decltype(all)::value>(a, a.ready, c0);
-    };
-    const std::true_type yes;
-    const std::false_type no;
-    constexpr bool kAhead = RB < 8;  // of 128 ranks there are no registers for a second step
-    if (full && kAhead && steps > 1) {
-      U v[2];
-      int loaded[2] = {place(0), place(1)};
-      w.template load<ACROSS>(a, tile.l, c0, mine);
-      load(yes, v[0], row(loaded[0], 0), 0);
-      for (int step = 0; step < steps; step += 2) {
-        loaded[0] = place(step + 2);
-        load(yes, v[1], row(loaded[1], step + 1), step + 1);
-        v[0].template work<true>(a, w, c0, s);
-        loaded[1] = place(step + 3);
-        load(yes, v[0], row(loaded[0], step + 2), step + 2);
-        if (step + 1 < steps) v[1].template work<true>(a, w, c0, s);
-      }
-      return;
-    }
-    const int first = place(0);
-    w.template load<ACROSS>(a, tile.l, c0, mine);
-    for (int step = 0; step < steps; ++step) {
-      U v;
-      const int t = row(step ? place(step) : first, step);
-      if (full) {
-        load(yes, v, t, step);
-        v.template work<true>(a, w, c0, s);
-      } else {
-        load(no, v, t, step);
-        v.template work<false>(a, w, c0, s);
-      }
+    const int t = row(step ? place(step) : first, step);
+    if (full) {
+      load(yes, v, t, step);
+      v.template work<true>(a, w, c0, s);
+    } else {
+      load(no, v, t, step);
+      v.template work<false>(a, w, c0, s);
     }
   }
 }
@@ -1053,10 +1047,11 @@ hipError_t up(UpArgs a, int32_t ydtype, int32_t wdtype, hipStream_t stream) {
   dim3 grid((unsigned)most_tiles(a.T, a.L, a.places));
   const auto go = [&](auto rb) {
     return by_types(ydtype, wdtype, [&](auto yb, auto wb) {
-      constexpr int kCols = kUpWaves * Up<decltype(yb)::value, decltype(wb)::value, decltype(rb)::value>::kCols;
+      constexpr bool YB = decltype(yb)::value, WB = decltype(wb)::value;
+      constexpr int RB = decltype(rb)::value, kCols = kUpWaves * Up<YB, WB, RB>::kCols;
       grid.y = (a.C + kCols - 1) / kCols;
-      hipLaunchKernelGGL((k_adapter_up<decltype(yb)::value, decltype(wb)::value, ACROSS, decltype(rb)::value, JOIN>), grid,
-                         dim3(kUpWaves * kWave), 0, stream, a);
+      if constexpr (JOIN) hipLaunchKernelGGL((k_adapter_up_join<YB, WB, RB>), grid, dim3(kUpWaves * kWave), 0, stream, a);
+      else hipLaunchKernelGGL((k_adapter_up<YB, WB, ACROSS, RB>), grid, dim3(kUpWaves * kWave), 0, stream, a);
       return hipGetLastError();
     });
   };
