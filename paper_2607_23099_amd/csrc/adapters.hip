@@ -23,14 +23,14 @@ damoe_status damoe_adapters(const void* x, int32_t xdtype, int64_t ldx, const in
       reinterpret_cast<uintptr_t>(ws) % 16)
     return DAMOE_ERR_INVALID_ARG;
   const int32_t rp = padded_rank(r);
+  const DownPlan d = down_plan(T, K);
+  const bool join = T < kManyRows;
+  if (ws_bytes < (join ? part_bytes(d, T, rp) : ready_bytes(T, rp) + kSpare)) return DAMOE_ERR_WORKSPACE;
   if (adapters_few(T, L, rp, K, N, ydtype, wdtype)) {
     const DownArgs da{x, ldx, a, perm, offsets, nullptr, nullptr, nullptr, u, L, T, K, r, rp, 0, 0};
     const UpArgs ua{nullptr, nullptr, 1, nullptr, b, scale, perm, offsets, add, ld_add, y, ldy, nullptr, L, T, N, r, rp, 0};
     return adapters_in_one(da, ua, xdtype, wdtype, ydtype, stream) == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
   }
-  const DownPlan d = down_plan(T, K);
-  const bool join = T < kManyRows;
-  if (ws_bytes < (join ? part_bytes(d, T, rp) : ready_bytes(T, rp) + kSpare)) return DAMOE_ERR_WORKSPACE;
   float* part = join ? static_cast<float*>(ws) : nullptr;
   const DownArgs da{x, ldx, a, perm, offsets, nullptr, part, ws, u, L, T, K, r, rp, 0, 0};
   // `up` takes thirds where the weights are bf16, `down` leaves them there too.

@@ -549,16 +549,31 @@ def _n_rows(name: str, t, cols: int) -> int:
     return t.shape[0]
 
 
+def _simple(t, rows: int, cols: int, ld, dtype, dev: int) -> int:
+    """Row stride of a contiguous 2-D matrix that needs no other look, 0 for any other: _matrix, in a third of its time."""
+    if ld is None and t.dtype == dtype and t.is_contiguous() and t.get_device() == dev:
+        shape = t.shape
+        if len(shape) == 2 and shape[0] >= rows and shape[1] >= cols:
+            return shape[1]
+    return 0
+
+
 def sort_rows(x, T, k, H, inv_perm, rows, w=None, ldx=None, stream=None):
     """rows[inv_perm[t k + j]] = w[t][j] x[t] (damoe_sort_rows); places at or past rows' end are left out."""
     if not _DTYPES:
         _types()
-    dt, dev = _DTYPES.get(x.dtype, -1), x.get_device()
+    dt, dev, n = x.dtype, x.get_device(), T * k
     R = _n_rows("rows", rows, H)
-    p_rows, ldr = _matrix("rows", rows, R, H, None, x, dev)
+    ldr = _simple(rows, R, H, None, dt, dev) or _matrix("rows", rows, R, H, None, x, dev)[1]
+    if not (inv_perm is not None and inv_perm.dtype in _INT32 and inv_perm.numel() >= n and inv_perm.is_contiguous()
+            and inv_perm.get_device() == dev
+            and (w is None or w.dtype in _FLOAT32 and w.numel() >= n and w.is_contiguous() and w.get_device() == dev)):
+        _list("w", w, _FLOAT32, n, dev)
+        _list("inv_perm", inv_perm, _INT32, n, dev)
     rc = (_lib or lib()).damoe_call_words(3, _SORT_WORDS(
-        x.data_ptr(), dt, _ld("x", x, T, H, ldx), _list("w", w, _FLOAT32, T * k, dev), _list("inv_perm", inv_perm, _INT32, T * k, dev),
-        T, k, H, R, p_rows, ldr, _stream_on("damoe_sort_rows", stream, dev, dt, T)), 12)
+        x.data_ptr(), _DTYPES.get(dt, -1), _simple(x, T, H, ldx, dt, dev) or _ld("x", x, T, H, ldx), 0 if w is None else w.data_ptr(),
+        0 if inv_perm is None else inv_perm.data_ptr(), T, k, H, R, rows.data_ptr(), ldr,
+        _stream_on("damoe_sort_rows", stream, dev, _DTYPES.get(dt, -1), T)), 12)
     if rc:
         raise DamoeError("damoe_sort_rows", rc)
 
@@ -567,14 +582,25 @@ def combine_rows(rows, T, k, H, inv_perm, y, w=None, add=None, ldy=None, ld_add=
     """y[t] = add[t] + sum_j w[t][j] rows[inv_perm[t k + j]] (damoe_combine_rows)."""
     if not _DTYPES:
         _types()
-    dt, dev = _DTYPES.get(rows.dtype, -1), rows.get_device()
+    dt, dev, n = rows.dtype, rows.get_device(), T * k
     R = _n_rows("rows", rows, H)
-    p_add, lda = _matrix("add", add, T, H, ld_add, rows, dev)
-    p_y, ld = _matrix("y", y, T, H, ldy, rows, dev)
+    if add is None:
+        p_add = lda = 0
+    else:
+        p_add, lda = add.data_ptr(), _simple(add, T, H, ld_add, dt, dev) or _matrix("add", add, T, H, ld_add, rows, dev)[1]
+    if y is None:
+        p_y = ld = 0
+    else:
+        p_y, ld = y.data_ptr(), _simple(y, T, H, ldy, dt, dev) or _matrix("y", y, T, H, ldy, rows, dev)[1]
+    if not (inv_perm is not None and inv_perm.dtype in _INT32 and inv_perm.numel() >= n and inv_perm.is_contiguous()
+            and inv_perm.get_device() == dev
+            and (w is None or w.dtype in _FLOAT32 and w.numel() >= n and w.is_contiguous() and w.get_device() == dev)):
+        _list("w", w, _FLOAT32, n, dev)
+        _list("inv_perm", inv_perm, _INT32, n, dev)
     rc = (_lib or lib()).damoe_call_words(4, _COMBINE_WORDS(
-        rows.data_ptr(), dt, _ld("rows", rows, R, H, None), _list("w", w, _FLOAT32, T * k, dev),
-        _list("inv_perm", inv_perm, _INT32, T * k, dev), T, k, H, R, p_add, lda, p_y, ld,
-        _stream_on("damoe_combine_rows", stream, dev, dt, T)), 14)
+        rows.data_ptr(), _DTYPES.get(dt, -1), _simple(rows, R, H, None, dt, dev) or _ld("rows", rows, R, H, None),
+        0 if w is None else w.data_ptr(), 0 if inv_perm is None else inv_perm.data_ptr(), T, k, H, R, p_add, lda, p_y, ld,
+        _stream_on("damoe_combine_rows", stream, dev, _DTYPES.get(dt, -1), T)), 14)
     if rc:
         raise DamoeError("damoe_combine_rows", rc)
 
@@ -584,19 +610,31 @@ def combine_rows_grad(dy, rows, T, k, H, inv_perm, w=None, drows=None, dw=None, 
     None without dw."""
     if not _DTYPES:
         _types()
-    dt, dev = _DTYPES.get(dy.dtype, -1), dy.get_device()
+    dt, dev, n = dy.dtype, dy.get_device(), T * k
     if rows is None and dw is not None:
         raise ValueError("rows: dw needs them")
-    R = [_n_rows(n, t, H) for n, t in (("rows", rows), ("drows", drows)) if t is not None]
-    if len(R) == 2 and R[0] != R[1]:
-        raise ValueError(f"drows: {R[1]} rows, rows has {R[0]}")
-    R = R[0] if R else 0
-    p_rows, ldr = _matrix("rows", rows, R, H, None, dy, dev)
-    p_drows, ldd = _matrix("drows", drows, R, H, None, dy, dev)
+    R = 0
+    p_rows = ldr = p_drows = ldd = 0
+    if drows is not None:
+        R = _n_rows("drows", drows, H)
+        p_drows, ldd = drows.data_ptr(), _simple(drows, R, H, None, dt, dev) or _matrix("drows", drows, R, H, None, dy, dev)[1]
+    if rows is not None:
+        m = _n_rows("rows", rows, H)
+        if drows is not None and m != R:
+            raise ValueError(f"drows: {R} rows, rows has {m}")
+        R = m
+        p_rows, ldr = rows.data_ptr(), _simple(rows, R, H, None, dt, dev) or _matrix("rows", rows, R, H, None, dy, dev)[1]
+    if not (inv_perm is not None and inv_perm.dtype in _INT32 and inv_perm.numel() >= n and inv_perm.is_contiguous()
+            and inv_perm.get_device() == dev
+            and (w is None or w.dtype in _FLOAT32 and w.numel() >= n and w.is_contiguous() and w.get_device() == dev)
+            and (dw is None or dw.dtype in _FLOAT32 and dw.numel() >= n and dw.is_contiguous() and dw.get_device() == dev)):
+        _list("w", w, _FLOAT32, n, dev)
+        _list("inv_perm", inv_perm, _INT32, n, dev)
+        _list("dw", dw, _FLOAT32, n, dev)
     rc = (_lib or lib()).damoe_call_words(5, _COMBINE_GRAD_WORDS(
-        dy.data_ptr(), dt, _ld("dy", dy, T, H, ldy), p_rows, ldr, _list("w", w, _FLOAT32, T * k, dev),
-        _list("inv_perm", inv_perm, _INT32, T * k, dev), T, k, H, R, p_drows, ldd, _list("dw", dw, _FLOAT32, T * k, dev),
-        _stream_on("damoe_combine_rows_grad", stream, dev, dt, T)), 15)
+        dy.data_ptr(), _DTYPES.get(dt, -1), _simple(dy, T, H, ldy, dt, dev) or _ld("dy", dy, T, H, ldy), p_rows, ldr,
+        0 if w is None else w.data_ptr(), 0 if inv_perm is None else inv_perm.data_ptr(), T, k, H, R, p_drows, ldd,
+        0 if dw is None else dw.data_ptr(), _stream_on("damoe_combine_rows_grad", stream, dev, _DTYPES.get(dt, -1), T)), 15)
     if rc:
         raise DamoeError("damoe_combine_rows_grad", rc)
 
@@ -611,15 +649,17 @@ def adapters_grad_workspace_size(T_max: int, L: int, r: int, K: int, N: int) -> 
 
 def _pairs(a, b, dev: int):
     """Sizes and type of adapters a [L][r][K], b [L][N][r]."""
-    if len(a.shape) != 3 or len(b.shape) != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
-        raise ValueError(f"a, b: [L][r][K] and [L][N][r] are wanted, not {tuple(a.shape)} and {tuple(b.shape)}")
-    if a.dtype != b.dtype or not a.is_contiguous() or not b.is_contiguous():
-        raise ValueError(f"a, b: contiguous tensors of one type are wanted, not {a.dtype}, {b.dtype} with strides {a.stride()}, "
-                         f"{b.stride()}")
-    for name, t in (("a", a), ("b", b)):
-        if t.get_device() != dev:
-            _elsewhere(name, t)
-    return (*a.shape, b.shape[1], _DTYPES.get(a.dtype, -1))
+    sa, sb, dt = a.shape, b.shape, a.dtype
+    if len(sa) != 3 or len(sb) != 3 or sa[0] != sb[0] or sa[1] != sb[2]:
+        raise ValueError(f"a, b: [L][r][K] and [L][N][r] are wanted, not {tuple(sa)} and {tuple(sb)}")
+    if dt != b.dtype or not a.is_contiguous() or not b.is_contiguous():
+        raise ValueError(f"a, b: contiguous tensors of one type are wanted, not {dt}, {b.dtype} with strides {a.stride()}, {b.stride()}")
+    if a.get_device() != dev:
+        _elsewhere("a", a)
+    if b.get_device() != dev:
+        _elsewhere("b", b)
+    L, r, K = sa
+    return L, r, K, sb[1], _DTYPES.get(dt, -1)
 
 
 def adapters(x, T, a, b, offsets, y, ws, perm=None, scale=None, add=None, u=None, ldx=None, ldy=None, ld_add=None, stream=None):
@@ -627,14 +667,28 @@ def adapters(x, T, a, b, offsets, y, ws, perm=None, scale=None, add=None, u=None
     (damoe_adapters); a [L][r][K] and b [L][N][r].  u [T][r] keeps a_l x[t] by places for the gradient."""
     if not _DTYPES:
         _types()
-    dt, dev = _DTYPES.get(x.dtype, -1), x.get_device()
+    dt, dy, dev = x.dtype, y.dtype, x.get_device()
     L, r, K, N, wt = _pairs(a, b, dev)
-    p_add, lda = _matrix("add", add, T, N, ld_add, y, dev)
-    p_y, ld = _matrix("y", y, T, N, ldy, y, dev)
+    if add is None:
+        p_add = lda = 0
+    else:
+        p_add, lda = add.data_ptr(), _simple(add, T, N, ld_add, dy, dev) or _matrix("add", add, T, N, ld_add, y, dev)[1]
+    ld = _simple(y, T, N, ldy, dy, dev) or _matrix("y", y, T, N, ldy, y, dev)[1]
+    if not (offsets is not None and offsets.dtype in _INT32 and offsets.numel() == L + 1 and offsets.is_contiguous()
+            and offsets.get_device() == dev and ws.is_contiguous() and ws.get_device() == dev
+            and (perm is None or perm.dtype in _INT32 and perm.numel() >= T and perm.is_contiguous() and perm.get_device() == dev)
+            and (scale is None or scale.dtype in _FLOAT32 and scale.numel() >= L and scale.is_contiguous() and scale.get_device() == dev)
+            and (u is None or u.dtype in _FLOAT32 and u.numel() >= T * r and u.is_contiguous() and u.get_device() == dev)):
+        _list("perm", perm, _INT32, T, dev)
+        _segment_offsets(offsets, L, dev)
+        _list("scale", scale, _FLOAT32, L, dev)
+        _list("u", u, _FLOAT32, T * r, dev)
+        _room("ws", ws, 0, dev)
     rc = (_lib or lib()).damoe_call_words(6, _ADAPTERS_WORDS(
-        x.data_ptr(), dt, _ld("x", x, T, K, ldx), _list("perm", perm, _INT32, T, dev), _segment_offsets(offsets, L, dev), T, L,
-        a.data_ptr(), b.data_ptr(), wt, r, K, N, _list("scale", scale, _FLOAT32, L, dev), p_add, lda, p_y, _DTYPES.get(y.dtype, -1), ld,
-        _list("u", u, _FLOAT32, T * r, dev), _room("ws", ws, 0, dev), ws.nbytes, _stream_on("damoe_adapters", stream, dev, dt, T)), 23)
+        x.data_ptr(), _DTYPES.get(dt, -1), _simple(x, T, K, ldx, dt, dev) or _ld("x", x, T, K, ldx), 0 if perm is None else perm.data_ptr(),
+        offsets.data_ptr(), T, L, a.data_ptr(), b.data_ptr(), wt, r, K, N, 0 if scale is None else scale.data_ptr(), p_add, lda,
+        y.data_ptr(), _DTYPES.get(dy, -1), ld, 0 if u is None else u.data_ptr(), ws.data_ptr(), ws.nbytes,
+        _stream_on("damoe_adapters", stream, dev, _DTYPES.get(dt, -1), T)), 23)
     if rc:
         raise DamoeError("damoe_adapters", rc)
 
@@ -652,17 +706,38 @@ def adapters_grad(x, dy, u, T, a, b, offsets, da, db, ws, perm=None, scale=None,
     (accumulate: added to what they hold)."""
     if not _DTYPES:
         _types()
-    dt, dev = _DTYPES.get(x.dtype, -1), x.get_device()
+    dt, dt_y, dev = x.dtype, dy.dtype, x.get_device()
     L, r, K, N, wt = _pairs(a, b, dev)
-    p_dy, ld = _matrix("dy", dy, T, N, ldy, dy, dev)
-    p_add, lda = _matrix("add", add, T, K, ld_add, x, dev)
-    p_dx, ldd = _matrix("dx", dx, T, K, ld_dx, x, dev)
+    ld = _simple(dy, T, N, ldy, dt_y, dev) or _matrix("dy", dy, T, N, ldy, dy, dev)[1]
+    if add is None:
+        p_add = lda = 0
+    else:
+        p_add, lda = add.data_ptr(), _simple(add, T, K, ld_add, dt, dev) or _matrix("add", add, T, K, ld_add, x, dev)[1]
+    if dx is None:
+        p_dx = ldd = 0
+    else:
+        p_dx, ldd = dx.data_ptr(), _simple(dx, T, K, ld_dx, dt, dev) or _matrix("dx", dx, T, K, ld_dx, x, dev)[1]
+    n, m = L * r * K, L * r * N
+    if not (offsets is not None and offsets.dtype in _INT32 and offsets.numel() == L + 1 and offsets.is_contiguous()
+            and offsets.get_device() == dev and ws.is_contiguous() and ws.get_device() == dev and da is not None and db is not None
+            and u is not None and u.dtype in _FLOAT32 and u.numel() >= T * r and u.is_contiguous() and u.get_device() == dev
+            and da.dtype in _FLOAT32 and da.numel() >= n and da.is_contiguous() and da.get_device() == dev
+            and db.dtype in _FLOAT32 and db.numel() >= m and db.is_contiguous() and db.get_device() == dev
+            and (perm is None or perm.dtype in _INT32 and perm.numel() >= T and perm.is_contiguous() and perm.get_device() == dev)
+            and (scale is None or scale.dtype in _FLOAT32 and scale.numel() >= L and scale.is_contiguous() and scale.get_device() == dev)):
+        _list("u", u, _FLOAT32, T * r, dev)
+        _list("perm", perm, _INT32, T, dev)
+        _segment_offsets(offsets, L, dev)
+        _list("scale", scale, _FLOAT32, L, dev)
+        _list("da", da, _FLOAT32, n, dev)
+        _list("db", db, _FLOAT32, m, dev)
+        _room("ws", ws, 0, dev)
     rc = (_lib or lib()).damoe_call_words(7, _ADAPTERS_GRAD_WORDS(
-        x.data_ptr(), dt, _ld("x", x, T, K, ldx), p_dy, _DTYPES.get(dy.dtype, -1), ld, _list("u", u, _FLOAT32, T * r, dev),
-        _list("perm", perm, _INT32, T, dev), _segment_offsets(offsets, L, dev), T, L, a.data_ptr(), b.data_ptr(), wt, r, K, N,
-        _list("scale", scale, _FLOAT32, L, dev), p_add, lda, p_dx, ldd, _list("da", da, _FLOAT32, L * r * K, dev),
-        _list("db", db, _FLOAT32, L * N * r, dev), int(accumulate), _room("ws", ws, 0, dev), ws.nbytes,
-        _stream_on("damoe_adapters_grad", stream, dev, dt)), 28)
+        x.data_ptr(), _DTYPES.get(dt, -1), _simple(x, T, K, ldx, dt, dev) or _ld("x", x, T, K, ldx), dy.data_ptr(), _DTYPES.get(dt_y, -1), ld,
+        0 if u is None else u.data_ptr(), 0 if perm is None else perm.data_ptr(), offsets.data_ptr(), T, L, a.data_ptr(), b.data_ptr(),
+        wt, r, K, N, 0 if scale is None else scale.data_ptr(), p_add, lda, p_dx, ldd, 0 if da is None else da.data_ptr(),
+        0 if db is None else db.data_ptr(), int(accumulate), ws.data_ptr(), ws.nbytes,
+        _stream_on("damoe_adapters_grad", stream, dev, _DTYPES.get(dt, -1))), 28)
     if rc:
         raise DamoeError("damoe_adapters_grad", rc)
 
