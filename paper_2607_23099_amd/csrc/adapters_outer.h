@@ -14,19 +14,10 @@ inline size_t pieces_by_rank(int32_t T, int32_t L) { return (size_t)(T + 7) / 8 
 
 // Eight places' values of a rank as operands: three thirds in bf16, or two halves of four in fp32.
 __device__ __forceinline__ void thirds(const float (&v)[8], uint4 (&out)[3]) {
-  float f[8];
+  uint32_t q[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) f[k] = v[k];
-#pragma unroll
-  for (int h = 0; h < 3; ++h) {
-    uint32_t q[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t lo = take_third(f[2 * k]);
-      q[k] = lo | (uint32_t)take_third(f[2 * k + 1]) << 16;
-    }
-    out[h] = uint4{q[0], q[1], q[2], q[3]};
-  }
+  for (int k = 0; k < 8; ++k) q[k] = __float_as_uint(v[k]);
+  thirds(q, out);
 }
 __device__ __forceinline__ void thirds(const float (&v)[8], uint4 (&out)[2]) {
 #pragma unroll
