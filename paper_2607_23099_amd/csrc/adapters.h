@@ -941,65 +941,74 @@ __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up_join(UpArgs a) {
   J::run(a, tile, (blockIdx.y * kUpWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * J::U::kCols, blockIdx.y == 0, lds);
 }
 
+// A tile of any places, in steps of 16, whose sums are a.ready's; c0: the wave's columns.
 template <bool YB, bool WB, bool ACROSS, int RB>
-__global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
+struct UpStream {
   typedef Up<YB, WB, RB> U;
   typedef Ready<WB> R;
-  __shared__ __align__(16) char runs[ACROSS ? 16 : kUpWaves * U::Weights::kLds];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int i = lane & 15, g = lane >> 4;
-  Tile tile;
-  if (!find_tile<false>(a.off, a.L, a.T, a.places, blockIdx.x, tile)) return;
-  const int c0 = (blockIdx.y * kUpWaves + wave) * U::kCols;
-  const bool full = c0 + U::kCols <= a.C;
-  const float s = a.scale ? a.scale[tile.l] : 1.f;
-  const Places places(a.perm, a.off);
-  const auto place = [&](int step) { return places.load(min(tile.lo + 16 * step + i, tile.hi - 1)); };
-  const auto row = [&](int loaded, int step) {  // -1: none
-    const int p = tile.lo + 16 * step + i, t = places.row(loaded, p);
-    return p < tile.hi && (uint32_t)t < (uint32_t)a.T ? t : -1;
-  };
-  typename U::Weights w;
-  char* mine = runs + (ACROSS ? 0 : wave * U::Weights::kLds);
-  if (c0 >= a.C) return;
-  const int steps = (tile.hi - tile.lo + 15) / 16;
-  const auto load = [&](auto all, U& v, int t, int step) {
-    const int p = tile.lo + 16 * min(step, steps - 1), n = min(16, tile.hi - p);
-    v.u.load(R::group(a.ready, p, a.rp), n, min(i, n - 1), a.rp, g);
-    v.rows(t);
-    v.template load_add<decltype(all)::value>(a, a.ready, c0);
-  };
-  const std::true_type yes;
-  const std::false_type no;
-  constexpr bool kAhead = RB < 8;  // of 128 ranks there are no registers for a second step
-  if (full && kAhead && steps > 1) {
-    U v[2];
-    int loaded[2] = {place(0), place(1)};
+  static constexpr int kRuns = ACROSS ? 0 : U::Weights::kLds;  // bytes of LDS for a wave
+
+  static __device__ __forceinline__ void run(const UpArgs& a, const Tile& tile, int c0, char* mine) {
+    if (c0 >= a.C) return;
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const bool full = c0 + U::kCols <= a.C;
+    const float s = a.scale ? a.scale[tile.l] : 1.f;
+    const Places places(a.perm, a.off);
+    const auto place = [&](int step) { return places.load(min(tile.lo + 16 * step + i, tile.hi - 1)); };
+    const auto row = [&](int loaded, int step) {  // -1: none
+      const int p = tile.lo + 16 * step + i, t = places.row(loaded, p);
+      return p < tile.hi && (uint32_t)t < (uint32_t)a.T ? t : -1;
+    };
+    typename U::Weights w;
+    const int steps = (tile.hi - tile.lo + 15) / 16;
+    const auto load = [&](auto all, U& v, int t, int step) {
+      const int p = tile.lo + 16 * min(step, steps - 1), n = min(16, tile.hi - p);
+      v.u.load(R::group(a.ready, p, a.rp), n, min(i, n - 1), a.rp, g);
+      v.rows(t);
+      v.template load_add<decltype(all)::value>(a, a.ready, c0);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    constexpr bool kAhead = RB < 8;  // of 128 ranks there are no registers for a second step
+    if (full && kAhead && steps > 1) {
+      U v[2];
+      int loaded[2] = {place(0), place(1)};
+      w.template load<ACROSS>(a, tile.l, c0, mine);
+      load(yes, v[0], row(loaded[0], 0), 0);
+      for (int step = 0; step < steps; step += 2) {
+        loaded[0] = place(step + 2);
+        load(yes, v[1], row(loaded[1], step + 1), step + 1);
+        v[0].template work<true>(a, w, c0, s);
+        loaded[1] = place(step + 3);
+        load(yes, v[0], row(loaded[0], step + 2), step + 2);
+        if (step + 1 < steps) v[1].template work<true>(a, w, c0, s);
+      }
+      return;
+    }
+    const int first = place(0);
     w.template load<ACROSS>(a, tile.l, c0, mine);
-    load(yes, v[0], row(loaded[0], 0), 0);
-    for (int step = 0; step < steps; step += 2) {
-      loaded[0] = place(step + 2);
-      load(yes, v[1], row(loaded[1], step + 1), step + 1);
-      v[0].template work<true>(a, w, c0, s);
-      loaded[1] = place(step + 3);
-      load(yes, v[0], row(loaded[0], step + 2), step + 2);
-      if (step + 1 < steps) v[1].template work<true>(a, w, c0, s);
-    }
-    return;
-  }
-  const int first = place(0);
-  w.template load<ACROSS>(a, tile.l, c0, mine);
-  for (int step = 0; step < steps; ++step) {
-    U v;
-    const int t = row(step ? place(step) : first, step);
-    if (full) {
-      load(yes, v, t, step);
-      v.template work<true>(a, w, c0, s);
-    } else {
-      load(no, v, t, step);
-      v.template work<false>(a, w, c0, s);
+    for (int step = 0; step < steps; ++step) {
+      U v;
+      const int t = row(step ? place(step) : first, step);
+      if (full) {
+        load(yes, v, t, step);
+        v.template work<true>(a, w, c0, s);
+      } else {
+        load(no, v, t, step);
+        v.template work<false>(a, w, c0, s);
+      }
     }
   }
+};
+
+template <bool YB, bool WB, bool ACROSS, int RB>
+__global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up(UpArgs a) {
+  typedef UpStream<YB, WB, ACROSS, RB> S;
+  __shared__ __align__(16) char runs[ACROSS ? 16 : kUpWaves * S::kRuns];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Tile tile;
+  if (find_tile<false>(a.off, a.L, a.T, a.places, blockIdx.x, tile))
+    S::run(a, tile, (blockIdx.y * kUpWaves + wave) * S::U::kCols, runs + wave * S::kRuns);
 }
 
 // ---------------------------------------------------------------- launches
@@ -1076,10 +1085,12 @@ hipError_t down(DownArgs a, const DownPlan& d, int32_t xdtype, int32_t wdtype, h
   });
 }
 
+inline int32_t up_places(int32_t T) { return T < kManyRows ? 16 : 128; }
+
 // JOIN: from a.part, else from a.ready.
 template <bool ACROSS, bool JOIN>
 hipError_t up(UpArgs a, int32_t ydtype, int32_t wdtype, hipStream_t stream) {
-  a.places = JOIN || a.T < kManyRows ? 16 : 128;
+  a.places = JOIN ? 16 : up_places(a.T);
   dim3 grid((unsigned)most_tiles(a.T, a.L, a.places));
   const auto go = [&](auto rb) {
     return by_types(ydtype, wdtype, [&](auto yb, auto wb) {

@@ -57,8 +57,11 @@ struct OuterArgs {
 bool adapters_few(int32_t T, int32_t L, int32_t rp, int32_t K, int32_t N, int32_t ydtype, int32_t wdtype);
 hipError_t adapters_in_one(DownArgs a, const UpArgs& b, int32_t xdtype, int32_t wdtype, int32_t ydtype, hipStream_t stream);
 
-// dx, dA and dB in one launch behind `down`, which has left g's parts: for few rows, x and dy of one type.
+// dx, dA and dB in one launch.  Few rows: behind `down`, which has left g's parts, a segment is one chunk and empty ones are
+// cleared; joined: behind `sums`.
 bool adapters_grad_few(int32_t T, int32_t L, int32_t r, int32_t K, int32_t N, int32_t xdtype, int32_t ydtype);
-hipError_t adapters_grad_in_one(const OuterArgs& b, const OuterArgs& a, UpArgs x, int32_t dtype, int32_t wdtype, hipStream_t stream);
+bool adapters_grad_joined(int32_t T, int32_t L, int32_t r, int32_t K, int32_t N, int32_t xdtype, int32_t ydtype);
+hipError_t adapters_grad_in_one(const OuterArgs& b, const OuterArgs& a, UpArgs x, bool few, int32_t dtype, int32_t wdtype,
+                                hipStream_t stream);
 
 }  // namespace damoe

@@ -217,14 +217,18 @@ damoe_status damoe_adapters_grad(const void* x, int32_t xdtype, int64_t ldx, con
     const OuterArgs ob{dy, ldy, u_rank, u, 1, r, scale, perm, offsets, db, slots_b, L, T, N, r, rp, cn, accumulate};
     const OuterArgs oa{x, ldx, g_rank, part, d.parts, rp, nullptr, perm, offsets, da, slots_a, L, T, K, r, rp, ck, accumulate};
     const UpArgs xa{part, ready, d.parts, nullptr, a, nullptr, perm, offsets, add, ld_add, dx, ld_dx, spare, L, T, K, r, rp, 0};
-    if (few) return adapters_grad_in_one(ob, oa, xa, xdtype, wdtype, stream) == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
+    if (few) return adapters_grad_in_one(ob, oa, xa, true, xdtype, wdtype, stream) == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
     const SumsArgs sa{part, u, offsets, dx ? ready : nullptr, {g_rank, u_rank}, wdtype == DAMOE_BF16,
                       {xdtype == DAMOE_BF16, ydtype == DAMOE_BF16}, d.parts, L, T, r, rp};
     hipLaunchKernelGGL(k_adapter_sums, dim3((unsigned)most_tiles(T, L, kSumsPlaces), 2), dim3(256), 0, stream, sa);
     if (hipGetLastError() != hipSuccess) return DAMOE_ERR_HIP;
-    if (outer(ob, ydtype, true, stream) != hipSuccess) return DAMOE_ERR_HIP;
-    if (outer(oa, xdtype, false, stream) != hipSuccess) return DAMOE_ERR_HIP;
-    if (dx && up<true, false>(xa, xdtype, wdtype, stream) != hipSuccess) return DAMOE_ERR_HIP;
+    if (adapters_grad_joined(T, L, r, K, N, xdtype, ydtype)) {
+      if (adapters_grad_in_one(ob, oa, xa, false, xdtype, wdtype, stream) != hipSuccess) return DAMOE_ERR_HIP;
+    } else {
+      if (outer(ob, ydtype, true, stream) != hipSuccess) return DAMOE_ERR_HIP;
+      if (outer(oa, xdtype, false, stream) != hipSuccess) return DAMOE_ERR_HIP;
+      if (dx && up<true, false>(xa, xdtype, wdtype, stream) != hipSuccess) return DAMOE_ERR_HIP;
+    }
   }
   JoinArgs j{offsets, {da, db}, {slots_a, slots_b}, {(int64_t)r * K, (int64_t)r * N}, {ck, cn}, L, T, accumulate, 256};
   const int64_t all = std::max(j.size[0], j.size[1]);
