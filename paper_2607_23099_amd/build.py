@@ -12,6 +12,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -63,10 +65,21 @@ def damoe_sources():
 
 
 def build_damoe(verbose=False):
+    """The sources side by side, then one link: a minute and not four on 8 CPUs."""
     srcs = damoe_sources()
     if not srcs:
         raise RuntimeError("no sources under csrc/")
-    _link(srcs, LIB_DAMOE, extra=[f"-I{os.path.join(PKG, 'csrc')}"], verbose=verbose)
+    flags = [f for f in HIP_FLAGS if f != "-shared"] + [f"-I{INCLUDE}", f"-I{os.path.join(PKG, 'csrc')}"]
+    with tempfile.TemporaryDirectory() as tmp:
+        def compiled(src):
+            obj = os.path.join(tmp, os.path.basename(src) + ".o")
+            _run([_hipcc(), *flags, "-c", src, "-o", obj], verbose)
+            return obj
+
+        workers = min(8, int(os.environ.get("MAX_JOBS", 0)) or os.cpu_count() or 1)
+        with ThreadPoolExecutor(workers) as pool:
+            objs = list(pool.map(compiled, srcs))
+        _link(objs, LIB_DAMOE, verbose=verbose)
 
 
 def build_all(verbose=False):
