@@ -590,7 +590,7 @@ damoe_status damoe_combine_rows_grad(const void* dy, int32_t dtype, int64_t ldy,
  *   u[p] = A_l x[t]     y[t] = add[t] + s_l B_l u[p]
  *   x        bf16 or fp32 (xdtype) [T][ldx], ldx >= K
  *   offsets  int32 [L + 1], non-decreasing, from 0 to at most T (otherwise the results are unspecified)
- *   perm     int32 [T], or NULL; distinct rows in [0, T) (another entry's place is left out)
+ *   perm     int32 [T], or NULL; distinct rows in [0, T) (another entry's place is left out, and u of it is unspecified)
  *   a, b     bf16 or fp32 (wdtype) [L][r][K] and [L][N][r], any alignment of the element; 1 <= r <= DAMOE_MAX_RANK
  *   scale    fp32 [L], or NULL: 1
  *   add      NULL (0), or [T][ld_add] of y's type; it may be y itself (ld_add = ldy)

@@ -50,6 +50,7 @@ struct OuterArgs {
   const int32_t* off;
   float* out;          // dA [L][r][C], or dB [L][C][r]
   float* slots;        // parts of segments of several chunks, laid out as the output
+  int32_t n_slots;     // no more are there, whatever the offsets are
   int32_t L, T, C, r, rp, chunk, accumulate;
 };
 

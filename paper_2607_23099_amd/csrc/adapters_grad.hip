@@ -97,7 +97,7 @@ struct JoinArgs {
   float* out[2];
   const float* slots[2];
   int64_t size[2];
-  int32_t chunk[2], L, T, accumulate, per;  // per: elements of a block
+  int32_t chunk[2], n_slots[2], L, T, accumulate, per;  // per: elements of a block
 };
 
 __global__ void __launch_bounds__(256) k_adapter_join(JoinArgs a) {
@@ -110,6 +110,7 @@ __global__ void __launch_bounds__(256) k_adapter_join(JoinArgs a) {
   for (int k = lane; k < l; k += 64) before += Length(a.off, a.L, a.T, a.chunk[m], k).split();
 #pragma unroll
   for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
+  if (seg.n && before + seg.n > a.n_slots[m]) return;  // offsets that decrease
   float* out = a.out[m] + l * size;
   const float* slots = a.slots[m] + (int64_t)before * size;
   for (int64_t i = (int64_t)blockIdx.x * a.per + threadIdx.x; i < end; i += 256) {
@@ -193,6 +194,7 @@ damoe_status damoe_adapters_grad(const void* x, int32_t xdtype, int64_t ldx, con
   const int32_t rp = padded_rank(r);
   const bool few = T > 0 && adapters_grad_few(T, L, r, K, N, xdtype, ydtype);  // then a segment is one chunk
   const int32_t ck = few || !T ? std::max(T, 1) : outer_chunk(T, K, xdtype), cn = few || !T ? std::max(T, 1) : outer_chunk(T, N, ydtype);
+  const int32_t n_a = T ? (int32_t)slots_of(T, ck) : 0, n_b = T ? (int32_t)slots_of(T, cn) : 0;
   char* base = static_cast<char*>(ws);
   float *slots_a = nullptr, *slots_b = nullptr;
   if (T > 0) {
@@ -208,14 +210,14 @@ damoe_status damoe_adapters_grad(const void* x, int32_t xdtype, int64_t ldx, con
     char* spare = piece(kSpare);
     void* g_rank = piece(rank_bytes(T, L, rp));
     void* u_rank = piece(rank_bytes(T, L, rp));
-    slots_a = reinterpret_cast<float*>(piece(slot_bytes(slots_of(T, ck), r, K)));
-    slots_b = reinterpret_cast<float*>(piece(slot_bytes(slots_of(T, cn), r, N)));
+    slots_a = reinterpret_cast<float*>(piece(slot_bytes(n_a, r, K)));
+    slots_b = reinterpret_cast<float*>(piece(slot_bytes(n_b, r, N)));
     if (ws_bytes < end) return DAMOE_ERR_WORKSPACE;
     const DownArgs ga{dy, ldy, b, perm, offsets, scale, part, nullptr, nullptr, L, T, N, r, rp, 0, 0};
     if (down<true>(ga, d, ydtype, wdtype, stream) != hipSuccess) return DAMOE_ERR_HIP;
     // dB first: it reads what `down` has just read.
-    const OuterArgs ob{dy, ldy, u_rank, u, 1, r, scale, perm, offsets, db, slots_b, L, T, N, r, rp, cn, accumulate};
-    const OuterArgs oa{x, ldx, g_rank, part, d.parts, rp, nullptr, perm, offsets, da, slots_a, L, T, K, r, rp, ck, accumulate};
+    const OuterArgs ob{dy, ldy, u_rank, u, 1, r, scale, perm, offsets, db, slots_b, n_b, L, T, N, r, rp, cn, accumulate};
+    const OuterArgs oa{x, ldx, g_rank, part, d.parts, rp, nullptr, perm, offsets, da, slots_a, n_a, L, T, K, r, rp, ck, accumulate};
     const UpArgs xa{part, ready, d.parts, nullptr, a, nullptr, perm, offsets, add, ld_add, dx, ld_dx, spare, L, T, K, r, rp, 0};
     if (few) return adapters_grad_in_one(ob, oa, xa, true, xdtype, wdtype, stream) == hipSuccess ? DAMOE_OK : DAMOE_ERR_HIP;
     const SumsArgs sa{part, u, offsets, dx ? ready : nullptr, {g_rank, u_rank}, wdtype == DAMOE_BF16,
@@ -230,7 +232,7 @@ damoe_status damoe_adapters_grad(const void* x, int32_t xdtype, int64_t ldx, con
       if (dx && up<true, false>(xa, xdtype, wdtype, stream) != hipSuccess) return DAMOE_ERR_HIP;
     }
   }
-  JoinArgs j{offsets, {da, db}, {slots_a, slots_b}, {(int64_t)r * K, (int64_t)r * N}, {ck, cn}, L, T, accumulate, 256};
+  JoinArgs j{offsets, {da, db}, {slots_a, slots_b}, {(int64_t)r * K, (int64_t)r * N}, {ck, cn}, {n_a, n_b}, L, T, accumulate, 256};
   const int64_t all = std::max(j.size[0], j.size[1]);
   while ((all + j.per - 1) / j.per * L > 2048 && j.per < all) j.per *= 2;
   hipLaunchKernelGGL(k_adapter_join, dim3((unsigned)((all + j.per - 1) / j.per), L, 2), dim3(256), 0, stream, j);

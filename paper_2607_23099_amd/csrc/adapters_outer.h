@@ -174,6 +174,7 @@ struct Outer {
     }
     // The waves' sums in order, through LDS, where threads side by side take elements side by side of the output.  Lane (i, g)
     // holds rank i of each block and, of MFMA j and register e, column P (4 g + e) + j of the lanes' columns.
+    if (!tile.whole && tile.slot >= a.n_slots) return;  // offsets that decrease
     const int64_t size = (int64_t)a.r * a.C;
     float* out = tile.whole ? a.out + tile.l * size : a.slots + tile.slot * size;
     const float scale = a.scale ? a.scale[tile.l] : 1.f;

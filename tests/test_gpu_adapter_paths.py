@@ -179,3 +179,17 @@ def test_offsets_that_end_before_the_rows_or_past_them():
         c.d_off.copy_(torch.tensor([0, int(c.off[1]), T + 100000], dtype=torch.int32))
         c.forward(), c.backward()
         close(c.d_y, y.double().cpu().numpy(), np.zeros(y.shape), None, "y")
+
+
+def test_offsets_that_decrease_stay_within_the_workspace():
+    """Their results are unspecified; every place is below T, every slot one of those there are."""
+    torch = torch_cuda()
+    for T, r in ((700, 8), (2500, 8), (5000, 40)):
+        log(f"T={T} r={r}")
+        c = Case(torch, T, 64, r, 128, 256)
+        sizes = [w.numel() for w in c.ws]
+        c.ws = [torch.full((n + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda") for n in sizes]
+        c.d_off.copy_(torch.tensor([0] + [T, 0] * 32, dtype=torch.int32))
+        c.forward(), c.backward()
+        for w, n in zip(c.ws, sizes):
+            assert (w[n:] == 0xA5).all(), n

@@ -1,5 +1,6 @@
 """What the row and adapter calls refuse, in the library and in the binding (no GPU: every call ends before a launch)."""
 import os
+import random
 
 import pytest
 
@@ -174,3 +175,22 @@ def test_refusals_of_the_binding_adapters():
                     call(**{name: v})
     with pytest.raises(damoe.DamoeError, match="unsupported"):
         forward(x=good["x"].half())
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are made up: a launch has to fail")
+def test_a_workspace_of_the_named_size_is_enough_for_every_smaller_call():
+    """Of T_max rows, for T of 0 to T_max, whatever way the call takes through its kernels."""
+    rng = random.Random(1)
+    sizes = [(4096, 3, 16, 7168, 4096), (1024, 1024, 64, 64, 8192), (1 << 20, 1, 1, 1, 1), (9000, 1, 128, 300, 5000), (200, 7, 33, 8, 8)]
+    sizes += [(int(2 ** rng.uniform(0, 20)), rng.randint(1, 1024), rng.randint(1, 128), int(2 ** rng.uniform(0, 14)), int(2 ** rng.uniform(0, 14)))
+              for _ in range(40)]
+    call = damoe.lib().damoe_call_words
+    for most, L, r, K, N in sizes:
+        for d in (0, 1):
+            common = dict(L=L, r=r, K=K, N=N, ldx=K, ldy=N, xdtype=d, ydtype=d)
+            for fn, pack, good, ld, size in ((6, damoe._ADAPTERS_WORDS, ADAPTERS, dict(ld_add=N), damoe.adapters_workspace_size),
+                                             (7, damoe._ADAPTERS_GRAD_WORDS, ADAPTERS_GRAD, dict(ld_add=K, ld_dx=K), damoe.adapters_grad_workspace_size)):
+                room = size(most, L, r, K, N)
+                for T in sorted({1, most, max(1, most // 3), min(most, 1024), min(most, 1025), min(most, 4095), min(most, 4096), min(most, 129)}):
+                    words = {**good, **common, **ld, "T": T, "ws_bytes": room}
+                    assert call(fn, pack(*words.values()), len(words)) not in (BAD, UNSUPPORTED, WORKSPACE), (fn, T, most, L, r, K, N)
