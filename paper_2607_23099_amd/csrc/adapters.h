@@ -612,11 +612,12 @@ struct Side {
   static constexpr int kWords = N * E::kBytes / 4;
   uint32_t q[kWords];
 
+  template <bool NT = false>
   __device__ __forceinline__ void load(const typename E::T* p) {
     if constexpr (kWords >= 4) {
 #pragma unroll
       for (int h = 0; h < kWords; h += 4) {
-        const uint4 v = load16_at<E::kBytes>(p + h / 4 * E::kPer16);
+        const uint4 v = load16_at<E::kBytes, NT>(p + h / 4 * E::kPer16);
         q[h] = v.x, q[h + 1] = v.y, q[h + 2] = v.z, q[h + 3] = v.w;
       }
     } else {
@@ -829,7 +830,7 @@ struct Up {
     for (int e = 0; e < 4; ++e) {
       if constexpr (FULL) {
         const Y* base = static_cast<const Y*>(a.add ? a.add : zero);
-        add[e].load(base + (a.add ? max(t[e], 0) * a.lda + c : 0));
+        add[e].template load<true>(base + (a.add ? max(t[e], 0) * a.lda + c : 0));
       } else {
         add[e] = Side<YB, NB>{};
         if (a.add && t[e] >= 0 && n > 0) add[e].load_some(static_cast<const Y*>(a.add) + t[e] * a.lda + c, n);

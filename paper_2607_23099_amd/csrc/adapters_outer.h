@@ -95,9 +95,22 @@ struct Outer {
         for (int rb = 0; rb < RB; ++rb) {
           float f[8] = {};
           const float* part = a.part + min(r0 + 16 * rb + i, a.r - 1);
-          for (int n = 0; n < a.parts; ++n, part += (int64_t)a.T * a.ld) {
+          if (a.parts == 1) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] += part[(int64_t)min(p + 8 * g + k, tile.hi - 1) * a.ld];
+            for (int k = 0; k < 8; ++k) f[k] = part[(int64_t)min(p + 8 * g + k, tile.hi - 1) * a.ld];
+          }
+          for (int n = a.parts == 1 ? 1 : 0; n < a.parts; n += 4) {  // in order, four parts' loads in flight
+            float q[4][8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                q[j][k] = part[((int64_t)min(n + j, a.parts - 1) * a.T + min(p + 8 * g + k, tile.hi - 1)) * a.ld];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                if (n + j < a.parts) f[k] += q[j][k];
           }
           thirds(f, s.u[rb]);
         }
