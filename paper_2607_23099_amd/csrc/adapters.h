@@ -177,16 +177,17 @@ struct Rows16 {
   // The lane's row number h of those that it loads.
   static __device__ __forceinline__ int mine(int h) { return (threadIdx.x >> 2 & 3) * 4 + h; }
 
-  // at(h): the first element of row mine(h); c: the unit's first column.
+  // at(h): the first element of row mine(h); c: the unit's first column.  Rows from n on are 0 where none of a load's counts.
   template <bool NT = false, class F>
-  __device__ __forceinline__ void load(const void* base, F at, int c) {
+  __device__ __forceinline__ void load(const void* base, F at, int c, int n = 16) {
     typedef Elem<SRC> E;
     const int g = (threadIdx.x & 63) >> 4, a = threadIdx.x & 3;
 #pragma unroll
     for (int s = 0; s < kSets; ++s)
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        const uint4 v = load16_at<E::kBytes, NT>(static_cast<const typename E::T*>(base) + (at(h) + (c + 32 * g + (4 * s + a) * E::kPer16)));
+        uint4 v = {0, 0, 0, 0};
+        if (h < n) v = load16_at<E::kBytes, NT>(static_cast<const typename E::T*>(base) + (at(h) + (c + 32 * g + (4 * s + a) * E::kPer16)));
         uint32_t(&d)[4] = q[4 * s + h];
         d[0] = v.x, d[1] = v.y, d[2] = v.z, d[3] = v.w;
       }
@@ -421,7 +422,7 @@ struct Down {
       const auto load = [&](Unit& v, int u) {
         v.w.template load<true>(a, slab, r0, u * kUnit, kUnit);
 #pragma unroll
-        for (int m = 0; m < M; ++m) v.x[m].template load<LIE == kRows>(a.x, [&](int h) { return rows[m][h]; }, u * kUnit);
+        for (int m = 0; m < M; ++m) v.x[m].template load<LIE == kRows>(a.x, [&](int h) { return rows[m][h]; }, u * kUnit, M == 1 ? tile.hi - tile.lo : 16);
       };
       Unit v[D];
       int u = u0 + wave;
@@ -524,7 +525,11 @@ struct Ready {
 
 constexpr int kDownWaves = 8;
 
-// More than 64 ranks take a block of the grid for each 64.
+// More than 64 ranks take a block of the grid for each 64.  Bound by x, which is read past the caches (A and what `up` adds
+// keep their places in them), and by the time in which a block finds its tile and adds up its waves, of which there is one a
+// CU: 7168 rows of 7168 bf16 at rank 32 30 us (3.4 TB/s; 45 when 16 lanes loaded from 16 rows, 36 with plain loads); 4096
+// rows over 256 segments at rank 8, fp32, 27 us for as many bytes of A as of x (4.3 TB/s).  Eight waves of two units in
+// flight: sixteen of one took 39 us for 32, three units 37.
 template <bool XB, bool WB, Lie LIE, int RB, int M>
 __global__ void __launch_bounds__(kDownWaves* kWave) k_adapter_down(DownArgs a) {
   typedef Down<XB, WB, LIE, RB, M, kDownWaves> D;
@@ -882,6 +887,7 @@ struct Up {
   }
 };
 
+// Few rows: bound by the chain of a launch, the tile, the parts, the product (61 rows of 48 segments, 7168 columns, rank 16: 5.5 us).
 // A tile of at most 16 places whose parts are added here, in LDS for the block's waves; c0: the wave's columns.  `first`: the
 // block that keeps u.
 template <bool YB, bool WB, bool ACROSS, int RB>
@@ -942,7 +948,9 @@ __global__ void __launch_bounds__(kUpWaves* kWave) k_adapter_up_join(UpArgs a) {
   J::run(a, tile, (blockIdx.y * kUpWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * J::U::kCols, blockIdx.y == 0, lds);
 }
 
-// A tile of any places, in steps of 16, whose sums are a.ready's; c0: the wave's columns.
+// A tile of any places, in steps of 16, whose sums are a.ready's; c0: the wave's columns.  Bound by what is added and written:
+// 7168 rows of 4096 bf16 at rank 32 28 us (4.2 TB/s; 38 in pieces of 64 bytes), a tile of 128 places being as long as 1024
+// blocks at once allow (64 places 31 us).
 template <bool YB, bool WB, bool ACROSS, int RB>
 struct UpStream {
   typedef Up<YB, WB, RB> U;

