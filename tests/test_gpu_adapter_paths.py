@@ -193,3 +193,11 @@ def test_offsets_that_decrease_stay_within_the_workspace():
         c.forward(), c.backward()
         for w, n in zip(c.ws, sizes):
             assert (w[n:] == 0xA5).all(), n
+
+
+@pytest.mark.parametrize("T,L,r,K,N", [(2, 1, 1, 1 << 20, 9), (2, 1, 1, 9, 1 << 20), (1030, 1, 2, 1 << 17, 12), (1 << 20, 3, 2, 8, 9)])
+def test_the_longest_rows_and_the_most_of_them(T, L, r, K, N):
+    torch = torch_cuda()
+    log(f"T={T} K={K} N={N}")
+    for dtype in ("bf16", "f32"):
+        Case(torch, T, L, r, K, N, dtype, dtype, dtype).check()

@@ -218,3 +218,36 @@ def test_equal_bits_on_another_stream_and_in_a_replayed_graph():
         calls(out)
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, replayed))
+
+
+@pytest.mark.parametrize("T,k,H", [(1 << 20, 16, 1), (1 << 20, 1, 24), (1, 16, 1 << 20), (65536, 8, 40)])
+def test_the_most_tokens_and_the_longest_rows(T, k, H):
+    """Against torch: with gates of powers of two, and values of a few bits, every sum is exact."""
+    torch = torch_cuda()
+    log(f"T={T} k={k} H={H}")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    R = T * k
+    inv = torch.randperm(R, generator=g, device="cuda").to(torch.int32)
+    inv[torch.rand(R, generator=g, device="cuda") < 0.1] = -1
+    small = lambda *s: torch.randint(-4, 5, s, generator=g, device="cuda").bfloat16()
+    x, rows, add = small(T, H), small(R, H), small(T, H)
+    w = 2.0 ** torch.randint(-2, 3, (T, k), generator=g, device="cuda").float()
+    ok = inv >= 0
+    token, place = torch.arange(R, device="cuda") // k, inv.long()
+    want = torch.zeros(R, H, device="cuda")
+    want[place[ok]] = w.view(-1)[ok][:, None] * x[token[ok]].float()
+    out = torch.zeros(R, H, dtype=torch.bfloat16, device="cuda")
+    damoe.sort_rows(x, T, k, H, inv, out, w=w)
+    assert torch.equal(out.float(), want)
+    taken = torch.where(ok[:, None], rows[place.clamp_min(0)].float(), 0).view(T, k, H)
+    y = torch.empty_like(x)
+    damoe.combine_rows(rows, T, k, H, inv, y, w=w, add=add)
+    total = add.float()
+    for j in range(k):
+        total = total + w[:, j, None] * taken[:, j]
+    assert torch.equal(y, total.bfloat16())
+    dw, out2 = torch.empty(T, k, device="cuda"), torch.zeros_like(out)
+    damoe.combine_rows_grad(x, rows, T, k, H, inv, w=w, drows=out2, dw=dw)
+    assert torch.equal(out2, out)
+    for j in range(k):
+        assert torch.equal(dw[:, j], (x.float() * taken[:, j]).sum(dim=1))
