@@ -558,13 +558,20 @@ def _simple(t, rows: int, cols: int, ld, dtype, dev: int) -> int:
     return 0
 
 
+def _rows(t, cols: int, dtype, dev: int):
+    """Rows and row stride of a contiguous matrix of sorted rows, None for any other that may be one."""
+    shape = t.shape
+    if len(shape) == 2 and shape[1] >= cols and t.dtype == dtype and t.is_contiguous() and t.get_device() == dev:
+        return shape
+    return None
+
+
 def sort_rows(x, T, k, H, inv_perm, rows, w=None, ldx=None, stream=None):
     """rows[inv_perm[t k + j]] = w[t][j] x[t] (damoe_sort_rows); places at or past rows' end are left out."""
     if not _DTYPES:
         _types()
     dt, dev, n = x.dtype, x.get_device(), T * k
-    R = _n_rows("rows", rows, H)
-    ldr = _simple(rows, R, H, None, dt, dev) or _matrix("rows", rows, R, H, None, x, dev)[1]
+    R, ldr = _rows(rows, H, dt, dev) or (_n_rows("rows", rows, H), _matrix("rows", rows, rows.shape[0], H, None, x, dev)[1])
     if not (inv_perm is not None and inv_perm.dtype in _INT32 and inv_perm.numel() >= n and inv_perm.is_contiguous()
             and inv_perm.get_device() == dev
             and (w is None or w.dtype in _FLOAT32 and w.numel() >= n and w.is_contiguous() and w.get_device() == dev)):
@@ -583,7 +590,7 @@ def combine_rows(rows, T, k, H, inv_perm, y, w=None, add=None, ldy=None, ld_add=
     if not _DTYPES:
         _types()
     dt, dev, n = rows.dtype, rows.get_device(), T * k
-    R = _n_rows("rows", rows, H)
+    R, ldr = _rows(rows, H, dt, dev) or (_n_rows("rows", rows, H), _ld("rows", rows, rows.shape[0], H, None))
     if add is None:
         p_add = lda = 0
     else:
@@ -598,9 +605,8 @@ def combine_rows(rows, T, k, H, inv_perm, y, w=None, add=None, ldy=None, ld_add=
         _list("w", w, _FLOAT32, n, dev)
         _list("inv_perm", inv_perm, _INT32, n, dev)
     rc = (_lib or lib()).damoe_call_words(4, _COMBINE_WORDS(
-        rows.data_ptr(), _DTYPES.get(dt, -1), _simple(rows, R, H, None, dt, dev) or _ld("rows", rows, R, H, None),
-        0 if w is None else w.data_ptr(), 0 if inv_perm is None else inv_perm.data_ptr(), T, k, H, R, p_add, lda, p_y, ld,
-        _stream_on("damoe_combine_rows", stream, dev, _DTYPES.get(dt, -1), T)), 14)
+        rows.data_ptr(), _DTYPES.get(dt, -1), ldr, 0 if w is None else w.data_ptr(), 0 if inv_perm is None else inv_perm.data_ptr(),
+        T, k, H, R, p_add, lda, p_y, ld, _stream_on("damoe_combine_rows", stream, dev, _DTYPES.get(dt, -1), T)), 14)
     if rc:
         raise DamoeError("damoe_combine_rows", rc)
 
@@ -616,14 +622,13 @@ def combine_rows_grad(dy, rows, T, k, H, inv_perm, w=None, drows=None, dw=None, 
     R = 0
     p_rows = ldr = p_drows = ldd = 0
     if drows is not None:
-        R = _n_rows("drows", drows, H)
-        p_drows, ldd = drows.data_ptr(), _simple(drows, R, H, None, dt, dev) or _matrix("drows", drows, R, H, None, dy, dev)[1]
+        R, ldd = _rows(drows, H, dt, dev) or (_n_rows("drows", drows, H), _matrix("drows", drows, drows.shape[0], H, None, dy, dev)[1])
+        p_drows = drows.data_ptr()
     if rows is not None:
-        m = _n_rows("rows", rows, H)
+        m, ldr = _rows(rows, H, dt, dev) or (_n_rows("rows", rows, H), _matrix("rows", rows, rows.shape[0], H, None, dy, dev)[1])
         if drows is not None and m != R:
             raise ValueError(f"drows: {R} rows, rows has {m}")
-        R = m
-        p_rows, ldr = rows.data_ptr(), _simple(rows, R, H, None, dt, dev) or _matrix("rows", rows, R, H, None, dy, dev)[1]
+        R, p_rows = m, rows.data_ptr()
     if not (inv_perm is not None and inv_perm.dtype in _INT32 and inv_perm.numel() >= n and inv_perm.is_contiguous()
             and inv_perm.get_device() == dev
             and (w is None or w.dtype in _FLOAT32 and w.numel() >= n and w.is_contiguous() and w.get_device() == dev)
