@@ -401,8 +401,9 @@ struct Down {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Places places(a.perm, a.off);
     const bool second = tile.hi - tile.lo > 16;
-    const auto row = [&](int place) {  // its first element; of places past the end the last one's
-      const int p = min(tile.lo + place, tile.hi - 1), t = places.row(places.load(p), p);
+    const auto at = [&](int place) { return min(tile.lo + place, tile.hi - 1); };  // past the end the last one
+    const auto row = [&](int loaded, int place) {  // its first element
+      const int t = places.row(loaded, at(place));
       return (int64_t)((uint32_t)t < (uint32_t)a.T ? t : 0) * a.ldx;
     };
     const char* slab = static_cast<const char*>(a.w) + (int64_t)tile.l * a.r * a.C * Elem<WB>::kBytes;
@@ -414,21 +415,35 @@ struct Down {
     int left = min(u1, whole) - u0 - wave;
     left = left > 0 ? (left + W - 1) / W : 0;
     if (left > 0) {
+      int loaded[M][4];
       int64_t rows[M][4];
+      const auto load_w = [&](Unit& v, int u) { v.w.template load<true>(a, slab, r0, u * kUnit, kUnit); };
+      const auto load_x = [&](Unit& v, int u) {
 #pragma unroll
-      for (int m = 0; m < M; ++m)
-#pragma unroll
-        for (int h = 0; h < 4; ++h) rows[m][h] = row(16 * m + Rows16<XB>::mine(h));
+        for (int m = 0; m < M; ++m)
+          v.x[m].template load<LIE == kRows>(a.x, [&](int h) { return rows[m][h]; }, u * kUnit, M == 1 ? tile.hi - tile.lo : 16);
+      };
       const auto load = [&](Unit& v, int u) {
-        v.w.template load<true>(a, slab, r0, u * kUnit, kUnit);
-#pragma unroll
-        for (int m = 0; m < M; ++m) v.x[m].template load<LIE == kRows>(a.x, [&](int h) { return rows[m][h]; }, u * kUnit, M == 1 ? tile.hi - tile.lo : 16);
+        load_w(v, u);
+        load_x(v, u);
       };
       Unit v[D];
       int u = u0 + wave;
-      const int last = u + (left - 1) * W;
+      // The first weights are asked for before perm's entries have come.
 #pragma unroll
-      for (int d = 0; d < D; ++d) load(v[d], min(u + d * W, last));
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) loaded[m][h] = places.load(at(16 * m + Rows16<XB>::mine(h)));
+#pragma unroll
+      for (int d = 0; d < D; ++d)
+        if (d < left) load_w(v[d], u + d * W);
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) rows[m][h] = row(loaded[m][h], 16 * m + Rows16<XB>::mine(h));
+#pragma unroll
+      for (int d = 0; d < D; ++d)
+        if (d < left) load_x(v[d], u + d * W);
       for (u += D * W; left >= 2 * D; left -= D) {
 #pragma unroll
         for (int d = 0; d < D; ++d, u += W) {
@@ -457,7 +472,7 @@ struct Down {
       Unit v;
       const int c = whole * kUnit, i = lane & 15, g = lane >> 4;
 #pragma unroll
-      for (int m = 0; m < M; ++m) v.x[m].load_some(a.x, row(16 * m + i) + c + 32 * g, a.C - c - 32 * g);
+      for (int m = 0; m < M; ++m) v.x[m].load_some(a.x, row(places.load(at(16 * m + i)), 16 * m + i) + c + 32 * g, a.C - c - 32 * g);
       v.w.template load<false>(a, slab, r0, c, a.C - c);
       multiply(v, second);
     }
