@@ -918,6 +918,14 @@ struct UpJoin {
     const float s = a.scale ? a.scale[tile.l] : 1.f;
     const Places places(a.perm, a.off);
     const int p = min(tile.lo + i, tile.hi - 1), row = places.row(places.load(p), p);
+    const int n = tile.hi - tile.lo;
+    const auto part = [&](int e, int k) {
+      const int at = min(e / (kRanks / 4), n - 1), rho = 4 * (e % (kRanks / 4));
+      return *reinterpret_cast<const floatx4*>(a.part + ((int64_t)min(k, a.parts - 1) * a.T + tile.lo + at) * a.rp + rho);
+    };
+    floatx4 q[4];  // of the thread's first sums, asked for before the weights are waited for
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = part(threadIdx.x, j);
     U v;
     typename U::Weights w;
     if (c0 < a.C) {
@@ -925,25 +933,23 @@ struct UpJoin {
       v.rows(tile.lo + i < tile.hi && (uint32_t)row < (uint32_t)a.T ? row : -1);
       v.template load_add<false>(a, nullptr, c0);
     }
-    const int n = tile.hi - tile.lo;
     for (int e = threadIdx.x; e < 16 * kRanks / 4; e += kUpWaves * kWave) {
       const int at = e / (kRanks / 4), rho = 4 * (e % (kRanks / 4));
       floatx4 f = {0.f, 0.f, 0.f, 0.f};
-      if (at < n) {
-        const float* part = a.part + (int64_t)(tile.lo + at) * a.rp + rho;
-        for (int k = 0; k < a.parts; k += 4) {  // in order, four loads in flight
-          floatx4 q[4];
+      for (int k = 0; k < a.parts; k += 4) {  // in order, four loads in flight
+        if (k || e != (int)threadIdx.x) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) q[j] = *reinterpret_cast<const floatx4*>(part + (int64_t)min(k + j, a.parts - 1) * a.T * a.rp);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (k + j < a.parts) f += q[j];
+          for (int j = 0; j < 4; ++j) q[j] = part(e, k + j);
         }
-        if (a.u && first) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (rho + k < a.r) a.u[(int64_t)(tile.lo + at) * a.r + rho + k] = f[k];
-        }
+        for (int j = 0; j < 4; ++j)
+          if (k + j < a.parts) f += q[j];
+      }
+      if (at >= n) f = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (a.u && first && at < n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (rho + k < a.r) a.u[(int64_t)(tile.lo + at) * a.r + rho + k] = f[k];
       }
       R::put(lds, 16, at, rho, kRanks, f);
     }
