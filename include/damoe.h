@@ -598,9 +598,10 @@ damoe_status damoe_combine_rows_grad(const void* dy, int32_t dtype, int64_t ldy,
  *            Overlaps neither x, a, b nor else add
  *   u        NULL, or fp32 [T][r] output, by places, for the gradient; places in no segment are left as they were
  *   ws       16-byte aligned, at least damoe_adapters_workspace_size(T, L, r, K, N) bytes; nothing is kept in it
- * Products are exact and sums fp32 in a fixed order, u is not rounded between them, y once.  A value that is not finite
- * makes what it enters not finite, of its own rows and its own segment only.  L <= DAMOE_MAX_E, K and N <= DAMOE_MAX_COLS,
- * T <= DAMOE_MAX_T.  T = 0 is a no-op.  Stream-ordered, allocates nothing, capturable; concurrent calls need workspaces
+ * fp32 factors keep all their bits, u among them; sums are fp32 in a fixed order, and y is rounded once.  A value that is not
+ * finite makes what it enters not finite, of its own rows and its own segment only.  L <= DAMOE_MAX_E, K and
+ * N <= DAMOE_MAX_COLS, T <= DAMOE_MAX_T.  T = 0 is a no-op.  Stream-ordered, allocates nothing, capturable; concurrent calls
+ * need workspaces
  * of their own, and so does every captured graph that may run beside another. */
 size_t damoe_adapters_workspace_size(int32_t T_max, int32_t L, int32_t r, int32_t K, int32_t N);
 damoe_status damoe_adapters(const void* x, int32_t xdtype, int64_t ldx, const int32_t* perm, const int32_t* offsets,

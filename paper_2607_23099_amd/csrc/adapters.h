@@ -540,8 +540,8 @@ struct Ready {
 
 constexpr int kDownWaves = 8;
 
-// More than 64 ranks take a block of the grid for each 64.  Bound by x, which is read past the caches (A and what `up` adds
-// keep their places in them), and by the time in which a block finds its tile and adds up its waves, of which there is one a
+// More than 64 ranks take a block of the grid for each 64.  Bound by x, which is read past the caches, as what `up` adds
+// is (A keeps its place in them), and by the time in which a block finds its tile and adds up its waves, of which there is one a
 // CU: 7168 rows of 7168 bf16 at rank 32 30 us (3.4 TB/s; 45 when 16 lanes loaded from 16 rows, 36 with plain loads); 4096
 // rows over 256 segments at rank 8, fp32, 27 us for as many bytes of A as of x (4.3 TB/s).  Eight waves of two units in
 // flight: sixteen of one took 39 us for 32, three units 37.

@@ -6,7 +6,7 @@ namespace {
 
 // Few places: `down` and `up` in one launch.  A block takes a tile of at most 16 places and W x Up::kCols columns of y, and
 // has the tile's u for itself, by W waves over K; blocks of other columns make it again.  Bound by one CU's loads of A: one row
-// of 7168 to 4096 columns at rank 16 9.1 us, of 512 to 512 5.0.
+// of 7168 to 4096 columns at rank 16 9.4 us, of 512 to 512 4.5.
 template <bool XB, bool YB, bool WB, int RB, int W>
 __global__ void __launch_bounds__(W* kWave) k_adapter_both(DownArgs a, UpArgs b) {
   constexpr int kSets = RB ? RB : 1, kRanks = 16 * kSets;
@@ -52,9 +52,9 @@ __global__ void __launch_bounds__(W* kWave) k_adapter_both(DownArgs a, UpArgs b)
 }
 
 // Whether the u that blocks make again costs less than a second launch, by the bytes of A that all blocks read and that one
-// does.  Captured calls in one launch / in two, us: L = 48, r = 16, 7168 x 2048, 16 rows (7 MB) 6.9 / 8.4, 61 rows (22 MB) 12.0 /
-// 10.4; L = 4, r = 32, 2048 x 2048, 256 rows (5 MB) 9.5 / 10.5, 2048 rows (34 MB) 20.0 / 17.5; L = 8, r = 16, 4096 x 7168, 61
-// rows (10 MB) 13.7 / 10.1, one row (229 KB a block) 9.1 / 8.9, which a launch of 3 us on the host turns round.
+// does.  Captured calls in one launch / in two, us: L = 48, r = 16, 7168 x 2048, 16 rows (7 MB) 6.6 / 8.4, 61 rows (22 MB) 12.0 /
+// 9.4; L = 4, r = 32, 2048 x 2048, 256 rows (5 MB) 9.5 / 10.5, 2048 rows (34 MB) 20.0 / 17.5; L = 8, r = 16, 4096 x 7168, 61
+// rows (10 MB) 13.7 / 8.3, one row (229 KB a block) 9.4 / 8.9, which a launch of 3 us on the host turns round.
 constexpr int64_t kBothBytes = 8 << 20, kBothBlock = 256 << 10;
 
 constexpr int kBothWaves = 8;
