@@ -627,7 +627,8 @@ damoe_status damoe_adapters_grad(const void* x, int32_t xdtype, int64_t ldx, con
 
 /* One of the calls with many arguments, for bindings to which each argument costs a conversion: its n arguments in order,
  * each in 8 bytes (pointers and integers as int64, floats as double), are read before it returns.  The call's own
- * status; DAMOE_ERR_INVALID_ARG for another number of words than it has arguments. */
+ * status; DAMOE_ERR_INVALID_ARG for another number of words than it has arguments, and for an integer that its type does not
+ * hold. */
 typedef enum damoe_call {
   DAMOE_CALL_ROUTER_LOSS = 0,
   DAMOE_CALL_ROUTER_LOSS_GRAD = 1,

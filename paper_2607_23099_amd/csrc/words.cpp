@@ -1,5 +1,6 @@
 // Calls whose arguments come as words in memory.
 #include <cstring>
+#include <tuple>
 #include <utility>
 
 #include "damoe.h"
@@ -12,12 +13,16 @@ union Word {
   void* p;
 };
 
-// Argument by argument, each as the type that the callee declares.
+// Argument by argument, each as the type that the callee declares; `fits` goes where an integer has more than 32 bits.
 struct Args {
   const Word* w;
+  bool* fits;
   template <class T>
   operator T*() const { return static_cast<T*>(w->p); }
-  operator int32_t() const { return (int32_t)w->i; }
+  operator int32_t() const {
+    *fits &= w->i == (int32_t)w->i;
+    return (int32_t)w->i;
+  }
   operator int64_t() const { return w->i; }
   operator size_t() const { return (size_t)w->i; }
   operator float() const { return (float)w->f; }
@@ -25,7 +30,9 @@ struct Args {
 
 template <class... A, size_t... I>
 damoe_status apply(damoe_status (*f)(A...), const Word* w, std::index_sequence<I...>) {
-  return f(static_cast<A>(Args{w + I})...);
+  bool fits = true;
+  const std::tuple<A...> args{static_cast<A>(Args{w + I, &fits})...};
+  return fits ? std::apply(f, args) : DAMOE_ERR_INVALID_ARG;
 }
 
 template <class... A>
