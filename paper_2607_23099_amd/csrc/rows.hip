@@ -27,7 +27,8 @@ struct RowArgs {
   int32_t chunks;  // pieces of 64 x 16 bytes of a row
 };
 
-// The token's slots, one a lane: place (-1 where there is none) and factor.
+// The token's slots, one a lane: place (-1 where there is none) and factor.  at() and weight() take them from their lanes, which
+// all have to be there: what is in the registers of a lane that has left is not laid down.
 struct Slots {
   int place = -1;
   float factor = 1.f;
@@ -56,6 +57,14 @@ __device__ __forceinline__ void by_pieces(const RowArgs& a, F f) {
   }
 }
 
+// First column of the lane's 16 bytes.  Lanes past the row's end, of which none may leave (Slots), have its last piece once more:
+// they load and store what the lane does whose it is.
+template <bool BF>
+__device__ __forceinline__ int column(const RowArgs& a, int chunk, int lane) {
+  constexpr int P = Elem<BF>::kPer16;
+  return min((chunk * kWave + lane) * P, (a.H - 1) / P * P);
+}
+
 template <bool BF>
 __device__ __forceinline__ uint4 scaled(uint4 v, float w) {
   float f[Elem<BF>::kPer16];
@@ -72,8 +81,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_rows(RowArgs a) {
   const int lane = threadIdx.x & 63;
   by_pieces(a, [&](int64_t t, int chunk) {
     const Slots s(a, t, lane);
-    const int c = (chunk * kWave + lane) * Elem<BF>::kPer16, n = a.H - c;
-    if (n <= 0) return;
+    const int c = column<BF>(a, chunk, lane), n = a.H - c;
     const uint4 v = load_some<BF>(static_cast<const T*>(a.x) + t * a.ldx + c, n);
     for (int j = 0; j < a.k; ++j) {
       const int q = s.at(j);
@@ -92,8 +100,7 @@ __global__ void __launch_bounds__(kThreads) k_combine_rows(RowArgs a) {
   const int lane = threadIdx.x & 63;
   by_pieces(a, [&](int64_t t, int chunk) {
     const Slots s(a, t, lane);
-    const int c = (chunk * kWave + lane) * P, n = a.H - c;
-    if (n <= 0) return;
+    const int c = column<BF>(a, chunk, lane), n = a.H - c;
     uint4 v[DAMOE_MAX_K];
 #pragma unroll
     for (int j = 0; j < DAMOE_MAX_K; ++j) {
@@ -121,9 +128,10 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // A block takes a token over its whole row: each lane's products in fp32, then the wave's lanes by exchanges, then the waves
-// in order.  8192 tokens of 8 x 7168 bf16: 394 us, 5.1 TB/s, half of it written.
+// in order.  8192 tokens of 8 x 7168 bf16: 394 us, 5.1 TB/s, half of it written.  At most 128 registers (four waves a SIMD): with 130
+// 8192 tokens of 8 x 520 took 68 us for 55.
 template <bool BF>
-__global__ void __launch_bounds__(kThreads) k_combine_rows_grad(RowArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) k_combine_rows_grad(RowArgs a) {
   typedef typename Elem<BF>::T T;
   constexpr int P = Elem<BF>::kPer16;
   __shared__ float part[kWaves][DAMOE_MAX_K];
@@ -132,8 +140,8 @@ __global__ void __launch_bounds__(kThreads) k_combine_rows_grad(RowArgs a) {
     const Slots s(a, t, lane);
     float acc[DAMOE_MAX_K] = {};
     for (int chunk = wave; chunk < a.chunks; chunk += kWaves) {
-      const int c = (chunk * kWave + lane) * P, n = a.H - c;
-      if (n <= 0) continue;
+      const int c = column<BF>(a, chunk, lane), n = a.H - c;
+      const bool mine = c == (chunk * kWave + lane) * P;
       const uint4 d = load_some<BF>(static_cast<const T*>(a.x) + t * a.ldx + c, n);
       uint4 v[DAMOE_MAX_K];
       if (a.dw) {
@@ -148,10 +156,11 @@ __global__ void __launch_bounds__(kThreads) k_combine_rows_grad(RowArgs a) {
       for (int j = 0; j < DAMOE_MAX_K; ++j) {
         if (j >= a.k || s.at(j) < 0) continue;
         if (a.dw) {
-          float g[P];
+          float g[P], sum = acc[j];
           unpack16<BF>(v[j], g);
 #pragma unroll
-          for (int i = 0; i < P; ++i) acc[j] = fmaf(f[i], g[i], acc[j]);
+          for (int i = 0; i < P; ++i) sum = fmaf(f[i], g[i], sum);
+          acc[j] = mine ? sum : acc[j];
         }
         if (a.out) store_some<BF, true>(static_cast<T*>(a.out) + (int64_t)s.at(j) * a.ldo + c, n, a.w ? scaled<BF>(d, s.weight(j)) : d);
       }
