@@ -76,7 +76,7 @@ def build_damoe(verbose=False):
             _run([_hipcc(), *flags, "-c", src, "-o", obj], verbose)
             return obj
 
-        workers = min(8, int(os.environ.get("MAX_JOBS", 0)) or os.cpu_count() or 1)
+        workers = max(1, min(8, int(os.environ.get("MAX_JOBS") or 0) or os.cpu_count() or 1))
         with ThreadPoolExecutor(workers) as pool:
             objs = list(pool.map(compiled, srcs))
         _link(objs, LIB_DAMOE, verbose=verbose)
