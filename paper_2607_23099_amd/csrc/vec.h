@@ -43,15 +43,11 @@ template <>
 struct Elem<true> {
   typedef uint16_t T;
   static constexpr int kBytes = 2, kPer16 = 8;
-  static __device__ __forceinline__ float get(uint16_t v) { return bf16_to_f32(v); }
-  static __device__ __forceinline__ uint16_t put(float v) { return (uint16_t)pack_bf16x2(v, v); }
 };
 template <>
 struct Elem<false> {
   typedef float T;
   static constexpr int kBytes = 4, kPer16 = 4;
-  static __device__ __forceinline__ float get(float v) { return v; }
-  static __device__ __forceinline__ float put(float v) { return v; }
 };
 
 // The 16 bytes of a row from `p` on of which n elements (at least one) are the row's; the others are 0.
