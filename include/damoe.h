@@ -598,11 +598,11 @@ damoe_status damoe_combine_rows_grad(const void* dy, int32_t dtype, int64_t ldy,
  *            Overlaps neither x, a, b nor else add
  *   u        NULL, or fp32 [T][r] output, by places, for the gradient; places in no segment are left as they were
  *   ws       16-byte aligned, at least damoe_adapters_workspace_size(T, L, r, K, N) bytes; nothing is kept in it
- * fp32 factors keep all their bits, u among them; sums are fp32 in a fixed order, and y is rounded once.  A value that is not
+ * fp32 factors, u among them, keep all their bits from 2^-110 in magnitude on; what of a smaller one lies below 2^-133 counts
+ * only against fp32 factors, not against bf16 ones.  Sums are fp32 in a fixed order, and y is rounded once.  A value that is not
  * finite makes what it enters not finite, of its own rows and its own segment only.  L <= DAMOE_MAX_E, K and
  * N <= DAMOE_MAX_COLS, T <= DAMOE_MAX_T.  T = 0 is a no-op.  Stream-ordered, allocates nothing, capturable; concurrent calls
- * need workspaces
- * of their own, and so does every captured graph that may run beside another. */
+ * need workspaces of their own, and so does every captured graph that may run beside another. */
 size_t damoe_adapters_workspace_size(int32_t T_max, int32_t L, int32_t r, int32_t K, int32_t N);
 damoe_status damoe_adapters(const void* x, int32_t xdtype, int64_t ldx, const int32_t* perm, const int32_t* offsets,
                             int32_t T, int32_t L, const void* a, const void* b, int32_t wdtype, int32_t r, int32_t K,
@@ -617,7 +617,8 @@ damoe_status damoe_adapters(const void* x, int32_t xdtype, int64_t ldx, const in
  *            a, b nor else add
  *   da, db   fp32 [L][r][K] and [L][N][r]; of a segment without rows 0.  accumulate = 1 adds to what they hold
  *   ws       as above, damoe_adapters_grad_workspace_size bytes
- * Sums are fp32 in a fixed order.  With T = 0 da and db are 0 (accumulate = 1: a no-op). */
+ * Sums are fp32 in a fixed order; u, g and fp32 weights keep their bits as above.  With T = 0 da and db are 0 (accumulate = 1: a
+ * no-op). */
 size_t damoe_adapters_grad_workspace_size(int32_t T_max, int32_t L, int32_t r, int32_t K, int32_t N);
 damoe_status damoe_adapters_grad(const void* x, int32_t xdtype, int64_t ldx, const void* dy, int32_t ydtype, int64_t ldy,
                                  const float* u, const int32_t* perm, const int32_t* offsets, int32_t T, int32_t L,

@@ -250,7 +250,8 @@ __device__ __forceinline__ floatx4 mma(const Frag<false>& a, const Frag<false>& 
 }
 
 // A third of an fp32 value in bf16: the leading 8 bits of its significand, cut off and not rounded, so that the three
-// thirds add up to all 24 and the first does not overflow.  An infinity or NaN is its own first third, without others.
+// thirds add up to all 24 and the first does not overflow (from 2^-110 on: bf16's smallest step is 2^-133, and what lies below
+// it is in none).  An infinity or NaN is its own first third, without others.
 __device__ __forceinline__ uint16_t take_third(float& v) {
   const uint32_t b = __float_as_uint(v), hi = b & 0xFFFF0000u;
   const bool finite = (b & 0x7F800000u) != 0x7F800000u;
