@@ -54,7 +54,8 @@ __global__ void __launch_bounds__(W* kWave) k_adapter_both(DownArgs a, UpArgs b)
 // Whether the u that blocks make again costs less than a second launch, by the bytes of A that all blocks read and that one
 // does.  Captured calls in one launch / in two, us: L = 48, r = 16, 7168 x 2048, 16 rows (7 MB) 6.6 / 8.4, 61 rows (22 MB) 12.0 /
 // 9.4; L = 4, r = 32, 2048 x 2048, 256 rows (5 MB) 9.5 / 10.5, 2048 rows (34 MB) 20.0 / 17.5; L = 8, r = 16, 4096 x 7168, 61
-// rows (10 MB) 13.7 / 8.3, one row (229 KB a block) 9.4 / 8.9, which a launch of 3 us on the host turns round.
+// rows (10 MB) 13.7 / 8.3, one row (229 KB a block) 10.0 / 7.8, which a launch of 3 us on the host turns round (9.3 / 11.0 from
+// Python).  B and the rows are not counted: L = 1, r = 16, 64 x 4096, 2048 rows 14.4 / 14.2, 8192 rows (4 MB of A) 55.6 / 31.5.
 constexpr int64_t kBothBytes = 8 << 20, kBothBlock = 256 << 10;
 
 constexpr int kBothWaves = 8;
