@@ -238,7 +238,9 @@ __global__ void __launch_bounds__(kThreads) k_combine_rows_grad_slots(RowArgs a)
 constexpr int64_t kMaxBlocks = 1 << 22;
 
 // Bytes of rows below which combine's gradient goes by slots.  By tokens / by slots, us, k = 8: 509 x 2048 fp32 (33 MB) 17.0 /
-// 14.5, 1500 x 1024 bf16 (25 MB) 15.7 / 13.0; 700 x 2048 fp32 (46 MB) 22.4 / 31.5, 509 x 7168 bf16 (58 MB) 27.5 / 29.1.
+// 14.5, 1500 x 1024 bf16 (25 MB) 15.7 / 13.0; 700 x 2048 fp32 (46 MB) 22.4 / 31.5, 509 x 7168 bf16 (58 MB) 27.5 / 29.1.  Next to the
+// border: 340 x 7168 bf16 (39 MB) 23.2 / 20.9, 640 x 2048 fp32 (42 MB) 22.0 / 23.7, 400 x 7168 bf16 (46 MB) 24.3 / 26.9; with
+// shorter rows or fewer slots the slots stay faster (6000 x 512 bf16, 49 MB, 39.4 / 32.0).  Masked slots count as rows.
 constexpr int64_t kFewBytes = 40 << 20;
 
 bool shape_ok(int32_t T, int32_t k, int32_t H, int32_t R) {
