@@ -57,8 +57,8 @@ __device__ __forceinline__ void by_pieces(const RowArgs& a, F f) {
   }
 }
 
-// First column of the lane's 16 bytes.  Lanes past the row's end, of which none may leave (Slots), have its last piece once more:
-// they load and store what the lane does whose it is.
+// First column of the lane's 16 bytes.  Lanes past the row's end, of which none may leave (Slots), have its last piece too and
+// load and store the same there as the lane whose it is.
 template <bool BF>
 __device__ __forceinline__ int column(const RowArgs& a, int chunk, int lane) {
   constexpr int P = Elem<BF>::kPer16;
