@@ -644,12 +644,17 @@ def combine_rows_grad(dy, rows, T, k, H, inv_perm, w=None, drows=None, dw=None, 
         raise DamoeError("damoe_combine_rows_grad", rc)
 
 
+def _size_of(size, *sizes: int) -> int:
+    """A workspace size; 0, as for others that the library does not take, for sizes past 32 bits, of which ctypes drops the rest."""
+    return int(size(*sizes)) if all(-1 << 31 <= n < 1 << 31 for n in sizes) else 0
+
+
 def adapters_workspace_size(T_max: int, L: int, r: int, K: int, N: int) -> int:
-    return int(lib().damoe_adapters_workspace_size(T_max, L, r, K, N))
+    return _size_of(lib().damoe_adapters_workspace_size, T_max, L, r, K, N)
 
 
 def adapters_grad_workspace_size(T_max: int, L: int, r: int, K: int, N: int) -> int:
-    return int(lib().damoe_adapters_grad_workspace_size(T_max, L, r, K, N))
+    return _size_of(lib().damoe_adapters_grad_workspace_size, T_max, L, r, K, N)
 
 
 def _pairs(a, b, dev: int):

@@ -31,3 +31,13 @@ def test_integers_past_32_bits(fn, pack, good):
         for far in (1 << 32, -(1 << 32), 1 << 62):
             words = {**quiet, name: quiet[name] + far}
             assert call(fn, pack(*words.values()), len(words)) == BAD, (name, far)
+
+
+@pytest.mark.parametrize("size", [damoe.adapters_workspace_size, damoe.adapters_grad_workspace_size], ids=["forward", "gradient"])
+def test_workspaces_of_sizes_past_32_bits(size):
+    """0, as for any size that the calls do not take, and not the size of what is left of them."""
+    good = [100, 3, 8, 64, 48]
+    assert size(*good) > 0
+    for i in range(len(good)):
+        for far in (1 << 32, -(1 << 32), 1 << 62):
+            assert size(*good[:i], good[i] + far, *good[i + 1:]) == 0
